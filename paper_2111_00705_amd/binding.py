@@ -34,6 +34,10 @@ EXPORTS = [
     "comp_ams_get_server_scales", "comp_ams_set_markov_state", "comp_ams_get_server_selected",
     "comp_ams_message_bits", "comp_ams_get_signs", "comp_ams_step_bf16", "comp_ams_step_f16", "comp_ams_set_rand", "comp_ams_set_streaming", "comp_ams_set_tile_order", "comp_ams_set_pass_lds", "comp_ams_message_bytes", "comp_ams_pack_message",
     "comp_ams_pack_message_noalloc", "comp_ams_probe_update",
+    "comp_ams_layer_norm", "comp_ams_layer_norm_backward", "comp_ams_layer_norm_work_bytes", "comp_ams_rel_bias_softmax",
+    "comp_ams_rel_bias_softmax_backward", "comp_ams_rel_bias_work_bytes", "comp_ams_token_logprobs",
+    "comp_ams_token_logprobs_work_bytes", "comp_ams_distill", "comp_ams_distill_work_bytes", "comp_ams_distill_backward",
+    "comp_ams_distill_grad", "comp_ams_operators_last_error",
 ]
 
 
@@ -101,6 +105,21 @@ def lib():
         L.comp_ams_message_bits.argtypes = [vp, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
         L.comp_ams_last_error.argtypes = [vp]
         L.comp_ams_last_error.restype = C.c_char_p
+        i32, i64, u64, f32 = C.c_int32, C.c_int64, C.c_uint64, C.c_float
+        L.comp_ams_layer_norm.argtypes = [vp] * 6 + [i64] * 4 + [f32, i32, vp]
+        L.comp_ams_layer_norm_backward.argtypes = [vp] * 8 + [i64] * 5 + [i32, i64, i32, i32, vp, u64, vp]
+        L.comp_ams_layer_norm_work_bytes.argtypes = [i64, i64, i32, C.POINTER(u64)]
+        L.comp_ams_rel_bias_softmax.argtypes = [vp] * 4 + [i32, vp] + [i64] * 4 + [vp, vp, i64, f32, i32, i32, vp]
+        L.comp_ams_rel_bias_softmax_backward.argtypes = [vp] * 5 + [i32, vp] + [i64] * 4 + [vp, i64, f32, i32, i32, i64, i32, i32, vp, u64, vp]
+        L.comp_ams_rel_bias_work_bytes.argtypes = [i64] * 4 + [i32, i32, C.POINTER(u64)]
+        L.comp_ams_token_logprobs.argtypes = [vp] * 6 + [i64] * 3 + [i32, i32, vp, u64, vp]
+        L.comp_ams_token_logprobs_work_bytes.argtypes = [i64, i64, i32, i32, C.POINTER(u64)]
+        L.comp_ams_distill.argtypes = [vp] * 5 + [i64] * 3 + [i32, f32, i32, vp, u64, vp]
+        L.comp_ams_distill_work_bytes.argtypes = [i64, i64, i32, C.POINTER(u64)]
+        L.comp_ams_distill_backward.argtypes = [vp] * 6 + [i64] * 4 + [i32, f32, i32, vp]
+        L.comp_ams_distill_grad.argtypes = [vp] * 6 + [i64] * 4 + [i32, f32, i32, vp]
+        L.comp_ams_operators_last_error.argtypes = []
+        L.comp_ams_operators_last_error.restype = C.c_char_p
         _lib = L
     return _lib
 

@@ -3,14 +3,18 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcomp_ams.so")
-SOURCES = [os.path.join(CSRC, "comp_ams.hip")]
+OPS = os.path.join(CSRC, "ops")
+SOURCES = [os.path.join(CSRC, "comp_ams.hip"), os.path.join(OPS, "operators.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in ("device_utils.h", "blocksign_kernels.h", "topk_kernels.h", "plain_kernels.h", "launch_rules.h")] + [
     os.path.join(os.path.dirname(HERE), "include", "comp_ams.h"),
-    os.path.join(os.path.dirname(HERE), "include", "comp_ams_tuning.h")]
+    os.path.join(os.path.dirname(HERE), "include", "comp_ams_tuning.h"),
+    os.path.join(os.path.dirname(HERE), "include", "comp_ams_operators.h")] + [
+    os.path.join(OPS, f) for f in ("op_common.h", "norm_kernels.h", "bias_kernels.h", "vocab_kernels.h")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
@@ -48,10 +52,18 @@ def stale() -> bool:
 def build(force: bool = True, verbose: bool = False) -> str:
     if force or stale():
         hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-        cmd = [hipcc] + HIPCC_FLAGS + ["-o", LIB] + SOURCES
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        subprocess.run(cmd, check=True)
+        with tempfile.TemporaryDirectory() as tmp:         # the sources side by side, then one link
+            objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SOURCES]
+            cmds = [[hipcc] + [f for f in HIPCC_FLAGS if f != "-shared"] + ["-c", "-o", o, s] for s, o in zip(SOURCES, objects)]
+            if verbose:
+                for cmd in cmds:
+                    print(" ".join(cmd), flush=True)
+            running = [subprocess.Popen(cmd) for cmd in cmds]
+            codes = [p.wait() for p in running]
+            for cmd, code in zip(cmds, codes):
+                if code:
+                    raise subprocess.CalledProcessError(code, cmd)
+            subprocess.run([hipcc] + HIPCC_FLAGS + ["-o", LIB] + objects, check=True)
         build_c_caller(verbose)
     return LIB
 

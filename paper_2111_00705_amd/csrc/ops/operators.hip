@@ -1,0 +1,432 @@
+// Host side of include/comp_ams_operators.h: argument validation, the choice of kernels, launches.
+#include "../../../include/comp_ams_operators.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+#include "bias_kernels.h"
+#include "norm_kernels.h"
+#include "vocab_kernels.h"
+
+using namespace cams_ops;
+
+namespace {
+
+thread_local char g_error[512] = "";
+
+int fail(int code, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_error, sizeof g_error, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+// The status of the launches since the runtime's "last error" was clear; it is cleared again, or the caller's next HIP call
+// would trip over it.
+int launched(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(COMP_AMS_EDEVICE, "%s: launch failed: %s", what, hipGetErrorString(e));
+    return COMP_AMS_OK;
+}
+
+constexpr int64_t kMaxGrid = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxElements = (int64_t)1 << 60;    // rows * stride: offsets in bytes stay far below 2^63
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+size_t type_size(int32_t type) { return type == COMP_AMS_F32 ? 4 : 2; }
+bool known_type(int32_t type) { return type == COMP_AMS_F32 || type == COMP_AMS_BF16 || type == COMP_AMS_F16; }
+bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// Calls f with a value of the element type.
+template <typename F>
+void with_type(int32_t type, F &&f)
+{
+    if (type == COMP_AMS_F32) f(float{});
+    else if (type == COMP_AMS_BF16) f(bf16_t{});
+    else f(f16_t{});
+}
+
+#define REQUIRE(cond, ...)                                        \
+    do {                                                          \
+        if (!(cond)) return fail(COMP_AMS_EINVAL, __VA_ARGS__);   \
+    } while (0)
+
+// A strided array of rows: base pointer, alignment, stride of at least a row, offsets in range.
+#define REQUIRE_ROWS(what, name, p, rows, cols, stride, type)                                                                  \
+    do {                                                                                                                       \
+        REQUIRE((p) != nullptr || (rows) == 0, "%s: %s is NULL", what, name);                                                  \
+        REQUIRE(aligned(p, type_size(type)), "%s: %s must be %zu-byte aligned", what, name, type_size(type));                   \
+        REQUIRE((stride) >= (cols) || (rows) <= 1, "%s: the rows of %s overlap (stride %lld < %lld)", what, name,              \
+                (long long)(stride), (long long)(cols));                                                                       \
+        REQUIRE((stride) >= 0 && ((rows) <= 1 || (stride) < kMaxElements / (rows)), "%s: %s is out of range", what, name);        \
+    } while (0)
+
+// --- layer norm ---------------------------------------------------------------------------------------------------
+
+int norm_check(const char *what, int64_t rows, int64_t cols, int32_t type)
+{
+    REQUIRE(known_type(type), "%s: unknown type %d", what, type);
+    REQUIRE(rows >= 0 && rows < (int64_t)1 << 40, "%s: rows=%lld must be in [0, 2^40)", what, (long long)rows);
+    REQUIRE(cols >= 1 && cols < (int64_t)1 << 31, "%s: cols=%lld must be in [1, 2^31)", what, (long long)cols);
+    return COMP_AMS_OK;
+}
+
+// How a worker's rows are cut for the parameter gradients: chunks of rows with one set of column sums each.
+struct NormChunks {
+    int64_t rows, count;     // rows of a chunk; chunks of a worker
+};
+NormChunks norm_chunks(int64_t worker_rows, int32_t n)
+{
+    const int64_t want = std::max<int64_t>(1, ceil_div(512, n));
+    const int64_t rows = std::max<int64_t>(16, ceil_div(worker_rows, want));
+    return {rows, std::max<int64_t>(1, ceil_div(worker_rows, rows))};
+}
+
+// --- the biased softmax ---------------------------------------------------------------------------------------------
+
+int bias_check(const char *what, const int32_t *bounds, int32_t n_buckets, const int32_t *key_len, int64_t batch, int64_t heads,
+               int64_t tq, int64_t tk, int64_t offset, float scale, int32_t type, Bounds *out)
+{
+    REQUIRE(known_type(type), "%s: unknown type %d", what, type);
+    REQUIRE(n_buckets >= 1 && n_buckets <= COMP_AMS_MAX_BUCKETS, "%s: n_buckets=%d must be in [1, %d]", what, n_buckets,
+            COMP_AMS_MAX_BUCKETS);
+    REQUIRE(bounds || n_buckets == 1, "%s: bounds are NULL", what);
+    REQUIRE(batch >= 0 && heads >= 0 && tq >= 0 && tk >= 0, "%s: a size is negative", what);
+    REQUIRE(tk < (int64_t)1 << 31, "%s: tk=%lld must be below 2^31", what, (long long)tk);
+    const int64_t most = (int64_t)1 << 31;
+    REQUIRE(batch < most && heads < most && tq < most, "%s: a size is out of range", what);
+    if (batch && heads && tq)
+        REQUIRE(batch * heads < most && batch * heads * tq < most, "%s: batch*heads*tq must be below 2^31", what);
+    REQUIRE(offset > -most && offset < most, "%s: offset out of range", what);
+    REQUIRE(std::isfinite(scale), "%s: scale must be finite", what);
+    REQUIRE(aligned(key_len, 4), "%s: key_len must be 4-byte aligned", what);
+    out->n = n_buckets - 1;
+    for (int32_t q = 0; q < n_buckets - 1; ++q) {
+        REQUIRE(q == 0 || bounds[q] > bounds[q - 1], "%s: bounds must be strictly ascending (bound %d)", what, q);
+        out->at[q] = bounds[q];
+    }
+    return COMP_AMS_OK;
+}
+
+// One array of [batch][heads][tq] rows.
+int bias_strides(const char *what, const char *name, const void *p, int64_t batch, int64_t heads, int64_t tq, int64_t tk,
+                 const int64_t *st, int32_t type)
+{
+    REQUIRE(p, "%s: %s is NULL", what, name);
+    REQUIRE(aligned(p, type_size(type)), "%s: %s must be %zu-byte aligned", what, name, type_size(type));
+    const int64_t size[3] = {batch, heads, tq};
+    for (int q = 0; q < 3; ++q) {
+        if (size[q] <= 1) continue;
+        REQUIRE(st[q] >= tk, "%s: the rows of %s overlap (stride %lld < %lld)", what, name, (long long)st[q], (long long)tk);
+        REQUIRE(st[q] < kMaxElements / size[q], "%s: %s is out of range", what, name);
+    }
+    return COMP_AMS_OK;
+}
+
+int64_t bias_pieces(int64_t tq) { return ceil_div(tq, kBiasAnyRows); }
+
+// --- vocabulary rows ----------------------------------------------------------------------------------------------------
+
+int vocab_sizes(const char *what, int64_t rows, int64_t vocab, int32_t type)
+{
+    REQUIRE(known_type(type), "%s: unknown type %d", what, type);
+    REQUIRE(rows >= 0 && rows < (int64_t)1 << 31, "%s: rows=%lld must be in [0, 2^31)", what, (long long)rows);
+    REQUIRE(vocab >= 1 && vocab < (int64_t)1 << 31, "%s: vocab=%lld must be in [1, 2^31)", what, (long long)vocab);
+    return COMP_AMS_OK;
+}
+
+int vocab_check(const char *what, const void *logits, int64_t rows, int64_t vocab, int64_t stride, int32_t type)
+{
+    if (const int rc = vocab_sizes(what, rows, vocab, type)) return rc;
+    REQUIRE_ROWS(what, "logits", logits, rows, vocab, stride, type);
+    return COMP_AMS_OK;
+}
+
+int distill_check(const char *what, const void *logits, const int32_t *idx, const float *val, int64_t rows, int64_t vocab,
+                  int64_t stride, int32_t k, float temperature, int32_t type)
+{
+    if (const int rc = vocab_check(what, logits, rows, vocab, stride, type)) return rc;
+    REQUIRE(k >= 1 && k <= COMP_AMS_MAX_TOP, "%s: k=%d must be in [1, %d]", what, k, COMP_AMS_MAX_TOP);
+    REQUIRE(std::isfinite(temperature) && temperature > 0.f && std::isfinite(1.f / temperature),
+            "%s: temperature must be positive and finite", what);
+    REQUIRE((idx && val) || rows == 0, "%s: idx or val is NULL", what);
+    REQUIRE(aligned(idx, 4) && aligned(val, 4), "%s: idx and val must be 4-byte aligned", what);
+    return COMP_AMS_OK;
+}
+
+template <bool kLoss, bool kGrad>
+void launch_distill(float *loss, float *lse_out, void *dlogits, const float *dloss, const void *logits, const float *lse_in,
+                    const int32_t *idx, const float *val, const DistillArgs &a, int32_t type, hipStream_t stream)
+{
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        distill_any<T, kLoss, kGrad><<<(unsigned)std::min(a.rows, kMaxGrid), kVocabThreads, 0, stream>>>(
+            loss, lse_out, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), lse_in, idx, val, a);
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+const char *comp_ams_operators_last_error(void) { return g_error; }
+
+int comp_ams_layer_norm(void *y, float *mean, float *rstd, const void *x, const float *gain, const float *shift, int64_t rows,
+                        int64_t cols, int64_t x_stride, int64_t y_stride, float eps, int32_t type, void *hip_stream)
+{
+    const char *what = "layer_norm";
+    if (const int rc = norm_check(what, rows, cols, type)) return rc;
+    REQUIRE_ROWS(what, "x", x, rows, cols, x_stride, type);
+    REQUIRE_ROWS(what, "y", y, rows, cols, y_stride, type);
+    REQUIRE(gain, "%s: gain is NULL", what);
+    REQUIRE(aligned(gain, 4) && aligned(shift, 4) && aligned(mean, 4) && aligned(rstd, 4), "%s: gain, shift, mean and rstd must be 4-byte aligned", what);
+    REQUIRE(std::isfinite(eps) && eps >= 0.f, "%s: eps must be finite and not negative", what);
+    if (rows == 0) return COMP_AMS_OK;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const NormArgs a = {rows, cols, x_stride, y_stride, 0, eps, (float)(1.0 / (double)cols)};
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        norm_forward_any<T><<<(unsigned)std::min(rows, kMaxGrid), kNormThreads, 0, stream>>>(static_cast<T *>(y), mean, rstd,
+                                                                                          static_cast<const T *>(x), gain, shift, a);
+    });
+    return launched(what);
+}
+
+int comp_ams_layer_norm_work_bytes(int64_t rows, int64_t cols, int32_t n, uint64_t *bytes)
+{
+    const char *what = "layer_norm_work_bytes";
+    if (const int rc = norm_check(what, rows, cols, COMP_AMS_F32)) return rc;
+    REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
+    REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
+    REQUIRE(bytes, "%s: bytes is NULL", what);
+    *bytes = (uint64_t)norm_chunks(rows / n, n).count * (uint64_t)n * 2u * (uint64_t)cols * sizeof(float);
+    return COMP_AMS_OK;
+}
+
+int comp_ams_layer_norm_backward(void *dx, void *dgain, void *dshift, const void *dy, const void *x, const float *mean,
+                                 const float *rstd, const float *gain, int64_t rows, int64_t cols, int64_t dx_stride, int64_t dy_stride,
+                                 int64_t x_stride, int32_t n, int64_t grad_stride, int32_t type, int32_t grad_type, void *work,
+                                 uint64_t work_bytes, void *hip_stream)
+{
+    const char *what = "layer_norm_backward";
+    if (const int rc = norm_check(what, rows, cols, type)) return rc;
+    REQUIRE(known_type(grad_type), "%s: unknown gradient type %d", what, grad_type);
+    REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
+    REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
+    REQUIRE_ROWS(what, "x", x, rows, cols, x_stride, type);
+    REQUIRE_ROWS(what, "dy", dy, rows, cols, dy_stride, type);
+    REQUIRE_ROWS(what, "dx", dx, rows, cols, dx_stride, type);
+    REQUIRE_ROWS(what, "dgain", dgain, (int64_t)n, cols, grad_stride, grad_type);
+    REQUIRE(aligned(dshift, type_size(grad_type)), "%s: dshift must be %zu-byte aligned", what, type_size(grad_type));
+    REQUIRE(gain && ((mean && rstd) || rows == 0), "%s: mean, rstd or gain is NULL", what);
+    REQUIRE(aligned(gain, 4) && aligned(mean, 4) && aligned(rstd, 4), "%s: mean, rstd and gain must be 4-byte aligned", what);
+    uint64_t need = 0;
+    if (const int rc = comp_ams_layer_norm_work_bytes(rows, cols, n, &need)) return rc;
+    REQUIRE(work && work_bytes >= need, "%s: needs %llu bytes of work memory", what, (unsigned long long)need);
+    REQUIRE(aligned(work, 16), "%s: work must be 16-byte aligned", what);
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const NormArgs a = {rows, cols, x_stride, dx_stride, dy_stride, 0.f, (float)(1.0 / (double)cols)};
+    const NormChunks ch = norm_chunks(rows / n, n);
+    float *sums = static_cast<float *>(work);
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        // the parameter gradients first: dx may replace dy or x
+        norm_param_any<T><<<dim3((unsigned)ceil_div(cols, kNormThreads), (unsigned)ch.count, (unsigned)n), kNormThreads, 0, stream>>>(
+            sums, static_cast<const T *>(dy), static_cast<const T *>(x), mean, rstd, a, rows / n, ch.rows);
+        if (rows > 0)
+            norm_backward_any<T><<<(unsigned)std::min(rows, kMaxGrid), kNormThreads, 0, stream>>>(
+                static_cast<T *>(dx), static_cast<const T *>(dy), static_cast<const T *>(x), mean, rstd, gain, a);
+    });
+    with_type(grad_type, [&](auto t) {
+        using G = decltype(t);
+        norm_param_join<G><<<dim3((unsigned)ceil_div(2 * cols, kNormThreads), (unsigned)n), kNormThreads, 0, stream>>>(
+            static_cast<G *>(dgain), static_cast<G *>(dshift), sums, cols, (int)ch.count, grad_stride);
+    });
+    return launched(what);
+}
+
+int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const int32_t *bounds_host, int32_t n_buckets,
+                              const int32_t *key_len, int64_t batch, int64_t heads, int64_t tq, int64_t tk,
+                              const int64_t *p_strides_host, const int64_t *s_strides_host, int64_t offset, float scale,
+                              int32_t causal, int32_t type, void *hip_stream)
+{
+    const char *what = "rel_bias_softmax";
+    Bounds bounds;
+    if (const int rc = bias_check(what, bounds_host, n_buckets, key_len, batch, heads, tq, tk, offset, scale, type, &bounds)) return rc;
+    if (batch == 0 || heads == 0 || tq == 0 || tk == 0) return COMP_AMS_OK;
+    REQUIRE(p_strides_host && s_strides_host, "%s: strides are NULL", what);
+    if (const int rc = bias_strides(what, "p", p, batch, heads, tq, tk, p_strides_host, type)) return rc;
+    if (const int rc = bias_strides(what, "s", s, batch, heads, tq, tk, s_strides_host, type)) return rc;
+    REQUIRE(table && aligned(table, 4), "%s: table is NULL or not 4-byte aligned", what);
+    BiasArgs a = {};
+    a.heads = heads, a.tq = tq, a.tk = tk, a.rows = batch * heads * tq;
+    a.s_b = s_strides_host[0], a.s_h = s_strides_host[1], a.s_q = s_strides_host[2];
+    a.p_b = p_strides_host[0], a.p_h = p_strides_host[1], a.p_q = p_strides_host[2];
+    a.offset = offset, a.scale = scale, a.causal = causal != 0;
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        bias_forward_any<T><<<(unsigned)a.rows, kBiasThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+            static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a);
+    });
+    return launched(what);
+}
+
+int comp_ams_rel_bias_work_bytes(int64_t batch, int64_t heads, int64_t tq, int64_t tk, int32_t n_buckets, int32_t type, uint64_t *bytes)
+{
+    const char *what = "rel_bias_work_bytes";
+    Bounds none;
+    if (const int rc = bias_check(what, nullptr, 1, nullptr, batch, heads, tq, tk, 0, 1.f, type, &none)) return rc;
+    REQUIRE(n_buckets >= 1 && n_buckets <= COMP_AMS_MAX_BUCKETS, "%s: n_buckets=%d must be in [1, %d]", what, n_buckets, COMP_AMS_MAX_BUCKETS);
+    REQUIRE(bytes, "%s: bytes is NULL", what);
+    *bytes = (uint64_t)(batch * heads * bias_pieces(tq)) * (uint64_t)n_buckets * sizeof(float);
+    return COMP_AMS_OK;
+}
+
+int comp_ams_rel_bias_softmax_backward(void *ds, void *dtable, const void *dp, const void *p, const int32_t *bounds_host,
+                                       int32_t n_buckets, const int32_t *key_len, int64_t batch, int64_t heads, int64_t tq,
+                                       int64_t tk, const int64_t *strides_host, int64_t offset, float scale, int32_t causal,
+                                       int32_t n, int64_t grad_stride, int32_t type, int32_t grad_type, void *work,
+                                       uint64_t work_bytes, void *hip_stream)
+{
+    const char *what = "rel_bias_softmax_backward";
+    Bounds bounds;
+    if (const int rc = bias_check(what, bounds_host, n_buckets, key_len, batch, heads, tq, tk, offset, scale, type, &bounds)) return rc;
+    REQUIRE(known_type(grad_type), "%s: unknown gradient type %d", what, grad_type);
+    REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
+    REQUIRE(batch % n == 0, "%s: batch=%lld must be a multiple of n=%d", what, (long long)batch, n);
+    if (heads == 0) return COMP_AMS_OK;
+    REQUIRE(heads <= 65535, "%s: heads=%lld must be at most 65535", what, (long long)heads);
+    REQUIRE_ROWS(what, "dtable", dtable, (int64_t)n, (int64_t)n_buckets * heads, grad_stride, grad_type);
+    const bool empty = batch == 0 || tq == 0 || tk == 0;
+    uint64_t need = 0;
+    if (!empty) {
+        REQUIRE(strides_host, "%s: strides are NULL", what);
+        if (const int rc = bias_strides(what, "ds", ds, batch, heads, tq, tk, strides_host, type)) return rc;
+        if (const int rc = bias_strides(what, "dp", dp, batch, heads, tq, tk, strides_host + 3, type)) return rc;
+        if (const int rc = bias_strides(what, "p", p, batch, heads, tq, tk, strides_host + 6, type)) return rc;
+        if (const int rc = comp_ams_rel_bias_work_bytes(batch, heads, tq, tk, n_buckets, type, &need)) return rc;
+        REQUIRE(work && work_bytes >= need, "%s: needs %llu bytes of work memory", what, (unsigned long long)need);
+        REQUIRE(aligned(work, 16), "%s: work must be 16-byte aligned", what);
+    }
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    float *sums = static_cast<float *>(work);
+    const int64_t pieces = bias_pieces(tq);
+    if (!empty) {
+        BiasArgs a = {};
+        a.heads = heads, a.tq = tq, a.tk = tk, a.rows = batch * heads * tq;
+        a.o_b = strides_host[0], a.o_h = strides_host[1], a.o_q = strides_host[2];
+        a.s_b = strides_host[3], a.s_h = strides_host[4], a.s_q = strides_host[5];
+        a.p_b = strides_host[6], a.p_h = strides_host[7], a.p_q = strides_host[8];
+        a.offset = offset, a.scale = scale, a.causal = causal != 0;
+        with_type(type, [&](auto t) {
+            using T = decltype(t);
+            bias_backward_any<T><<<(unsigned)(batch * heads * pieces), kBiasAnyThreads, 0, stream>>>(
+                static_cast<T *>(ds), sums, static_cast<const T *>(dp), static_cast<const T *>(p), bounds, key_len, a, pieces);
+        });
+    }
+    with_type(grad_type, [&](auto t) {
+        using G = decltype(t);
+        bias_table_join<G><<<dim3((unsigned)n_buckets, (unsigned)heads, (unsigned)n), kWave, 0, stream>>>(
+            static_cast<G *>(dtable), sums, heads, empty ? 0 : batch / n, pieces, n_buckets, grad_stride);
+    });
+    return launched(what);
+}
+
+int comp_ams_token_logprobs_work_bytes(int64_t rows, int64_t vocab, int32_t k, int32_t type, uint64_t *bytes)
+{
+    const char *what = "token_logprobs_work_bytes";
+    if (const int rc = vocab_sizes(what, rows, vocab, type)) return rc;
+    REQUIRE(k >= 0 && k <= COMP_AMS_MAX_TOP && k <= vocab, "%s: k=%d must be in [0, min(vocab, %d)]", what, k, COMP_AMS_MAX_TOP);
+    REQUIRE(bytes, "%s: bytes is NULL", what);
+    *bytes = 0;
+    return COMP_AMS_OK;
+}
+
+int comp_ams_token_logprobs(float *logp, float *entropy, int32_t *top_idx, float *top_logp, const void *logits, const int64_t *tokens,
+                            int64_t rows, int64_t vocab, int64_t stride, int32_t k, int32_t type, void *work, uint64_t work_bytes,
+                            void *hip_stream)
+{
+    const char *what = "token_logprobs";
+    if (const int rc = vocab_check(what, logits, rows, vocab, stride, type)) return rc;
+    REQUIRE(k >= 0 && k <= COMP_AMS_MAX_TOP && k <= vocab, "%s: k=%d must be in [0, min(vocab, %d)]", what, k, COMP_AMS_MAX_TOP);
+    REQUIRE(k == 0 || (top_idx && top_logp) || rows == 0, "%s: top_idx or top_logp is NULL", what);
+    REQUIRE(!logp || tokens, "%s: logp needs tokens", what);
+    REQUIRE(aligned(logp, 4) && aligned(entropy, 4) && aligned(top_idx, 4) && aligned(top_logp, 4) && aligned(tokens, 8),
+            "%s: an array is not aligned to its elements", what);
+    uint64_t need = 0;
+    if (const int rc = comp_ams_token_logprobs_work_bytes(rows, vocab, k, type, &need)) return rc;
+    REQUIRE(need == 0 || (work && work_bytes >= need && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
+            (unsigned long long)need);
+    if (rows == 0) return COMP_AMS_OK;
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        logprobs_any<T><<<(unsigned)rows, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+            logp, entropy, top_idx, top_logp, static_cast<const T *>(logits), tokens, rows, vocab, stride, k);
+    });
+    return launched(what);
+}
+
+int comp_ams_distill_work_bytes(int64_t rows, int64_t vocab, int32_t type, uint64_t *bytes)
+{
+    const char *what = "distill_work_bytes";
+    if (const int rc = vocab_sizes(what, rows, vocab, type)) return rc;
+    REQUIRE(bytes, "%s: bytes is NULL", what);
+    *bytes = 0;
+    return COMP_AMS_OK;
+}
+
+int comp_ams_distill(float *loss, float *lse, const void *logits, const int32_t *idx, const float *val, int64_t rows, int64_t vocab,
+                     int64_t stride, int32_t k, float temperature, int32_t type, void *work, uint64_t work_bytes, void *hip_stream)
+{
+    const char *what = "distill";
+    if (const int rc = distill_check(what, logits, idx, val, rows, vocab, stride, k, temperature, type)) return rc;
+    REQUIRE(aligned(loss, 4) && aligned(lse, 4), "%s: loss and lse must be 4-byte aligned", what);
+    uint64_t need = 0;
+    if (const int rc = comp_ams_distill_work_bytes(rows, vocab, type, &need)) return rc;
+    REQUIRE(need == 0 || (work && work_bytes >= need && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
+            (unsigned long long)need);
+    if (rows == 0) return COMP_AMS_OK;
+    launch_distill<true, false>(loss, lse, nullptr, nullptr, logits, nullptr, idx, val, {rows, vocab, stride, 0, k, temperature, 1.f / temperature},
+                                type, static_cast<hipStream_t>(hip_stream));
+    return launched(what);
+}
+
+int comp_ams_distill_backward(void *dlogits, const float *dloss, const void *logits, const float *lse, const int32_t *idx,
+                              const float *val, int64_t rows, int64_t vocab, int64_t dlogits_stride, int64_t stride, int32_t k,
+                              float temperature, int32_t type, void *hip_stream)
+{
+    const char *what = "distill_backward";
+    if (const int rc = distill_check(what, logits, idx, val, rows, vocab, stride, k, temperature, type)) return rc;
+    REQUIRE_ROWS(what, "dlogits", dlogits, rows, vocab, dlogits_stride, type);
+    REQUIRE((dloss && lse) || rows == 0, "%s: dloss or lse is NULL", what);
+    REQUIRE(aligned(dloss, 4) && aligned(lse, 4), "%s: dloss and lse must be 4-byte aligned", what);
+    if (rows == 0) return COMP_AMS_OK;
+    launch_distill<false, true>(nullptr, nullptr, dlogits, dloss, logits, lse, idx, val,
+                                {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature}, type, static_cast<hipStream_t>(hip_stream));
+    return launched(what);
+}
+
+int comp_ams_distill_grad(float *loss, void *dlogits, const float *dloss, const void *logits, const int32_t *idx, const float *val,
+                          int64_t rows, int64_t vocab, int64_t dlogits_stride, int64_t stride, int32_t k, float temperature,
+                          int32_t type, void *hip_stream)
+{
+    const char *what = "distill_grad";
+    if (const int rc = distill_check(what, logits, idx, val, rows, vocab, stride, k, temperature, type)) return rc;
+    REQUIRE_ROWS(what, "dlogits", dlogits, rows, vocab, dlogits_stride, type);
+    REQUIRE(dloss || rows == 0, "%s: dloss is NULL", what);
+    REQUIRE(aligned(dloss, 4) && aligned(loss, 4), "%s: dloss and loss must be 4-byte aligned", what);
+    if (rows == 0) return COMP_AMS_OK;
+    launch_distill<true, true>(loss, nullptr, dlogits, dloss, logits, nullptr, idx, val,
+                               {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature}, type, static_cast<hipStream_t>(hip_stream));
+    return launched(what);
+}
+
+}  // extern "C"
