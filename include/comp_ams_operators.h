@@ -128,13 +128,10 @@ int comp_ams_token_logprobs_work_bytes(int64_t rows, int64_t vocab, int32_t k, i
  *   comp_ams_distill_backward  writes dz [rows][vocab] from lse and dloss
  *   comp_ams_distill_grad      both at once, for a loss whose weights (dloss) are known beforehand: one pass over the
  *                              logits; loss may be NULL
- * dlogits may be logits itself with the same stride.  work: comp_ams_distill_work_bytes() bytes for comp_ams_distill, which may be
- * 0 (then NULL will do).
+ * dlogits may be logits itself with the same stride.
  */
 int comp_ams_distill(float *loss, float *lse, const void *logits, const int32_t *idx, const float *val, int64_t rows,
-                     int64_t vocab, int64_t stride, int32_t k, float temperature, int32_t type, void *work,
-                     uint64_t work_bytes, void *hip_stream);
-int comp_ams_distill_work_bytes(int64_t rows, int64_t vocab, int32_t type, uint64_t *bytes);
+                     int64_t vocab, int64_t stride, int32_t k, float temperature, int32_t type, void *hip_stream);
 int comp_ams_distill_backward(void *dlogits, const float *dloss, const void *logits, const float *lse, const int32_t *idx,
                               const float *val, int64_t rows, int64_t vocab, int64_t dlogits_stride, int64_t stride, int32_t k,
                               float temperature, int32_t type, void *hip_stream);

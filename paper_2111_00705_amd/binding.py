@@ -36,7 +36,7 @@ EXPORTS = [
     "comp_ams_pack_message_noalloc", "comp_ams_probe_update",
     "comp_ams_layer_norm", "comp_ams_layer_norm_backward", "comp_ams_layer_norm_work_bytes", "comp_ams_rel_bias_softmax",
     "comp_ams_rel_bias_softmax_backward", "comp_ams_rel_bias_work_bytes", "comp_ams_token_logprobs",
-    "comp_ams_token_logprobs_work_bytes", "comp_ams_distill", "comp_ams_distill_work_bytes", "comp_ams_distill_backward",
+    "comp_ams_token_logprobs_work_bytes", "comp_ams_distill", "comp_ams_distill_backward",
     "comp_ams_distill_grad", "comp_ams_operators_last_error",
 ]
 
@@ -114,8 +114,7 @@ def lib():
         L.comp_ams_rel_bias_work_bytes.argtypes = [i64] * 4 + [i32, i32, C.POINTER(u64)]
         L.comp_ams_token_logprobs.argtypes = [vp] * 6 + [i64] * 3 + [i32, i32, vp, u64, vp]
         L.comp_ams_token_logprobs_work_bytes.argtypes = [i64, i64, i32, i32, C.POINTER(u64)]
-        L.comp_ams_distill.argtypes = [vp] * 5 + [i64] * 3 + [i32, f32, i32, vp, u64, vp]
-        L.comp_ams_distill_work_bytes.argtypes = [i64, i64, i32, C.POINTER(u64)]
+        L.comp_ams_distill.argtypes = [vp] * 5 + [i64] * 3 + [i32, f32, i32, vp]
         L.comp_ams_distill_backward.argtypes = [vp] * 6 + [i64] * 4 + [i32, f32, i32, vp]
         L.comp_ams_distill_grad.argtypes = [vp] * 6 + [i64] * 4 + [i32, f32, i32, vp]
         L.comp_ams_operators_last_error.argtypes = []

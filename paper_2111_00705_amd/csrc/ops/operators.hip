@@ -162,15 +162,43 @@ int distill_check(const char *what, const void *logits, const int32_t *idx, cons
     return COMP_AMS_OK;
 }
 
-template <bool kLoss, bool kGrad>
-void launch_distill(float *loss, float *lse_out, void *dlogits, const float *dloss, const void *logits, const float *lse_in,
-                    const int32_t *idx, const float *val, const DistillArgs &a, int32_t type, hipStream_t stream)
+// How a row of a vocabulary is cut for logprobs_regs, and which of its forms takes a piece.
+struct PieceShape {
+    int32_t count;           // pieces of a row; 0: the row does not fit, logprobs_any takes it
+    int64_t len;             // elements of a piece, a multiple of 64 unless there is one only
+    int32_t threads, vecs;
+};
+constexpr int kPieceThreads = 512, kPieceVecs = 8;
+
+PieceShape piece_shape(int64_t rows, int64_t vocab, int32_t type)
 {
-    with_type(type, [&](auto t) {
-        using T = decltype(t);
-        distill_any<T, kLoss, kGrad><<<(unsigned)std::min(a.rows, kMaxGrid), kVocabThreads, 0, stream>>>(
-            loss, lse_out, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), lse_in, idx, val, a);
-    });
+    const int64_t lanes = (int64_t)kPieceThreads * 16 / (int64_t)type_size(type);     // elements of one vector of every thread
+    PieceShape s = {1, vocab, kPieceThreads, 1};
+    if (vocab <= lanes / 2) {
+        s.threads = kPieceThreads / 2;
+        return s;
+    }
+    const int64_t count = ceil_div(vocab, lanes * kPieceVecs);
+    if (count > kMaxPieces || rows * count > kMaxGrid) return {0, 0, 0, 0};
+    s.count = (int32_t)count;
+    if (count > 1) s.len = ceil_div(ceil_div(vocab, count), 64) * 64;
+    s.vecs = (int32_t)ceil_div(s.len, lanes);
+    return s;
+}
+
+// f(threads, vecs) with both as compile-time constants.
+template <int kThreads, int kVecs> struct Shape {
+    static constexpr int threads = kThreads, vecs = kVecs;
+};
+template <int kThreads, int kVecs, typename F>
+void with_vecs(int vecs, F &&f)
+{
+    if constexpr (kVecs == 1) {
+        f(Shape<kThreads, 1>{});
+    } else {
+        if (vecs >= kVecs) f(Shape<kThreads, kVecs>{});
+        else with_vecs<kThreads, kVecs - 1>(vecs, f);
+    }
 }
 
 }  // namespace
@@ -346,7 +374,8 @@ int comp_ams_token_logprobs_work_bytes(int64_t rows, int64_t vocab, int32_t k, i
     if (const int rc = vocab_sizes(what, rows, vocab, type)) return rc;
     REQUIRE(k >= 0 && k <= COMP_AMS_MAX_TOP && k <= vocab, "%s: k=%d must be in [0, min(vocab, %d)]", what, k, COMP_AMS_MAX_TOP);
     REQUIRE(bytes, "%s: bytes is NULL", what);
-    *bytes = 0;
+    const PieceShape s = piece_shape(rows, vocab, type);
+    *bytes = s.count > 1 ? (uint64_t)rows * (uint64_t)s.count * ((uint64_t)k * sizeof(uint64_t) + sizeof(Piece)) : 0;
     return COMP_AMS_OK;
 }
 
@@ -366,36 +395,50 @@ int comp_ams_token_logprobs(float *logp, float *entropy, int32_t *top_idx, float
     REQUIRE(need == 0 || (work && work_bytes >= need && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
             (unsigned long long)need);
     if (rows == 0) return COMP_AMS_OK;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const PieceShape s = piece_shape(rows, vocab, type);
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        logprobs_any<T><<<(unsigned)rows, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
-            logp, entropy, top_idx, top_logp, static_cast<const T *>(logits), tokens, rows, vocab, stride, k);
+        const T *z = static_cast<const T *>(logits);
+        if (s.count == 0) {
+            logprobs_any<T><<<(unsigned)rows, kVocabThreads, 0, stream>>>(logp, entropy, top_idx, top_logp, z, tokens, rows, vocab, stride, k);
+            return;
+        }
+        uint64_t *keys = static_cast<uint64_t *>(work);
+        Piece *pieces = reinterpret_cast<Piece *>(keys + (s.count > 1 ? rows * s.count * k : 0));
+        const int groups = k <= 32 ? 64 : k <= 64 ? 128 : 256;
+        auto launch = [&](auto shape) {
+            using S = decltype(shape);
+            logprobs_regs<T, S::threads, S::vecs><<<(unsigned)(rows * s.count), S::threads, 0, stream>>>(
+                logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, groups, s.count, s.len, pieces, keys);
+        };
+        if (s.threads == kPieceThreads) with_vecs<kPieceThreads, kPieceVecs>(s.vecs, launch);
+        else launch(Shape<kPieceThreads / 2, 1>{});
+        if (s.count > 1)
+            logprobs_join<T><<<(unsigned)rows, kVocabThreads, (size_t)s.count * k * sizeof(uint64_t), stream>>>(
+                logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, s.count, pieces, keys);
     });
     return launched(what);
 }
 
-int comp_ams_distill_work_bytes(int64_t rows, int64_t vocab, int32_t type, uint64_t *bytes)
-{
-    const char *what = "distill_work_bytes";
-    if (const int rc = vocab_sizes(what, rows, vocab, type)) return rc;
-    REQUIRE(bytes, "%s: bytes is NULL", what);
-    *bytes = 0;
-    return COMP_AMS_OK;
-}
-
 int comp_ams_distill(float *loss, float *lse, const void *logits, const int32_t *idx, const float *val, int64_t rows, int64_t vocab,
-                     int64_t stride, int32_t k, float temperature, int32_t type, void *work, uint64_t work_bytes, void *hip_stream)
+                     int64_t stride, int32_t k, float temperature, int32_t type, void *hip_stream)
 {
     const char *what = "distill";
     if (const int rc = distill_check(what, logits, idx, val, rows, vocab, stride, k, temperature, type)) return rc;
     REQUIRE(aligned(loss, 4) && aligned(lse, 4), "%s: loss and lse must be 4-byte aligned", what);
-    uint64_t need = 0;
-    if (const int rc = comp_ams_distill_work_bytes(rows, vocab, type, &need)) return rc;
-    REQUIRE(need == 0 || (work && work_bytes >= need && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
-            (unsigned long long)need);
     if (rows == 0) return COMP_AMS_OK;
-    launch_distill<true, false>(loss, lse, nullptr, nullptr, logits, nullptr, idx, val, {rows, vocab, stride, 0, k, temperature, 1.f / temperature},
-                                type, static_cast<hipStream_t>(hip_stream));
+    const DistillArgs a = {rows, vocab, stride, 0, k, temperature, 1.f / temperature};
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        auto launch = [&](auto shape) {
+            using S = decltype(shape);
+            distill_forward<T, S::threads><<<(unsigned)rows, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                loss, lse, static_cast<const T *>(logits), idx, val, a);
+        };
+        if (vocab <= 4 * 256 * kVec<T>) launch(Shape<256, 0>{});
+        else launch(Shape<1024, 0>{});
+    });
     return launched(what);
 }
 
@@ -409,8 +452,16 @@ int comp_ams_distill_backward(void *dlogits, const float *dloss, const void *log
     REQUIRE((dloss && lse) || rows == 0, "%s: dloss or lse is NULL", what);
     REQUIRE(aligned(dloss, 4) && aligned(lse, 4), "%s: dloss and lse must be 4-byte aligned", what);
     if (rows == 0) return COMP_AMS_OK;
-    launch_distill<false, true>(nullptr, nullptr, dlogits, dloss, logits, lse, idx, val,
-                                {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature}, type, static_cast<hipStream_t>(hip_stream));
+    const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature};
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        const int64_t chunk = 4 * 256 * kVec<T>;
+        const int64_t pieces = std::max<int64_t>(1, std::min(ceil_div(vocab, 4 * chunk), kMaxGrid / rows));
+        const int64_t len = ceil_div(ceil_div(vocab, pieces), chunk) * chunk;
+        const int64_t count = ceil_div(vocab, len);
+        distill_gradient<T, 256><<<(unsigned)(rows * count), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(
+            static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), lse, idx, val, a, (int)count, len);
+    });
     return launched(what);
 }
 
@@ -424,8 +475,21 @@ int comp_ams_distill_grad(float *loss, void *dlogits, const float *dloss, const 
     REQUIRE(dloss || rows == 0, "%s: dloss is NULL", what);
     REQUIRE(aligned(dloss, 4) && aligned(loss, 4), "%s: dloss and loss must be 4-byte aligned", what);
     if (rows == 0) return COMP_AMS_OK;
-    launch_distill<true, true>(loss, nullptr, dlogits, dloss, logits, nullptr, idx, val,
-                               {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature}, type, static_cast<hipStream_t>(hip_stream));
+    const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature};
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        auto launch = [&](auto shape) {
+            using S = decltype(shape);
+            distill_both<T, S::threads, S::vecs><<<(unsigned)rows, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                loss, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), idx, val, a);
+        };
+        const int64_t vecs = ceil_div(vocab, kVec<T>);          // vectors of the row
+        if (vecs <= 256) launch(Shape<256, 1>{});
+        else if (vecs <= 512 * 8) with_vecs<512, 8>((int)ceil_div(vecs, 512), launch);
+        else if (vecs <= 1024 * 8) with_vecs<1024, 8>((int)ceil_div(vecs, 1024), launch);
+        else if (vecs <= 1024 * 16) launch(Shape<1024, 16>{});
+        else launch(Shape<1024, 0>{});
+    });
     return launched(what);
 }
 

@@ -301,10 +301,8 @@ def distill(logits, idx, val, temperature=1.0):
     s = _stream(logits, idx, val)
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
     lse = torch.empty_like(loss)
-    L, kind = lib(), _type(logits)
-    work, work_ptr, work_bytes = _work(L.comp_ams_distill_work_bytes, logits.device, rows, vocab, kind)
-    _check(L.comp_ams_distill(loss.data_ptr(), lse.data_ptr(), logits.data_ptr(), idx.data_ptr(), val.data_ptr(), rows, vocab, stride, k,
-                              temperature, kind, work_ptr, work_bytes, s))
+    _check(lib().comp_ams_distill(loss.data_ptr(), lse.data_ptr(), logits.data_ptr(), idx.data_ptr(), val.data_ptr(), rows, vocab, stride,
+                                  k, temperature, _type(logits), s))
     return loss, lse
 
 
