@@ -94,7 +94,7 @@ constexpr int kBiasAnyThreads = 64;
 template <typename T>
 __global__ __launch_bounds__(kBiasAnyThreads) void bias_backward_any(T *ds, float *__restrict__ work, const T *dp, const T *__restrict__ p,
                                                                      Bounds bounds, const int32_t *__restrict__ key_len, BiasArgs a,
-                                                                     int64_t pieces)
+                                                                     int64_t pieces, int64_t worker_batch)
 {
     __shared__ int32_t at[COMP_AMS_MAX_BUCKETS];
     __shared__ float slot[COMP_AMS_MAX_BUCKETS * kBiasAnyThreads];
@@ -124,24 +124,288 @@ __global__ __launch_bounds__(kBiasAnyThreads) void bias_backward_any(T *ds, floa
             or_[j] = narrow1<T>(dt * a.scale);
         }
     }
+    const int64_t b = bh / a.heads, w = b / worker_batch, parts = worker_batch * pieces;
     for (int q = 0; q <= bounds.n; ++q) {
         const float s = lanes_reduce<SumOp, kWave>(slot[q * kBiasAnyThreads + lane]);
-        if (lane == 0) work[(int64_t)blockIdx.x * (bounds.n + 1) + q] = s;
+        if (lane == 0) work[((w * a.heads + bh % a.heads) * (bounds.n + 1) + q) * parts + (b - w * worker_batch) * pieces + piece] = s;
     }
 }
 
-// work[batch][heads][pieces][buckets] -> dtable[worker][buckets][heads]; one wavefront per (bucket, head, worker), lanes in a
-// fixed order.
+// --- rows that a team of lanes holds in registers -----------------------------------------------------------------------
+
+// What query i of the workgroup's (sequence, head) sees, as keys [0, seen).
+__device__ __forceinline__ int row_seen(int64_t i, int64_t seen_by_length, const BiasArgs &a)
+{
+    int64_t seen = seen_by_length;
+    if (a.causal) seen = min(seen, max(i + a.offset + 1, (int64_t)0));
+    return (int)seen;
+}
+
+// Forward: a workgroup takes `rows_block` queries of one head and sequence, its teams in turn.  The head's bias over the relative
+// positions that occur there is laid out in LDS first, [tk + rows_block - 1] floats, so that a vector of keys finds its biases side by
+// side.
+template <typename T, int kTeam, int kVecs>
+__global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_forward(T *p, const T *s, const float *__restrict__ table, Bounds bounds,
+                                                                const int32_t *__restrict__ key_len, BiasArgs a, int pieces, int rows_block)
+{
+    constexpr int E = kVec<T>, kTeams = kTeamBlock<kTeam> / kTeam;
+    extern __shared__ float along[];
+    __shared__ float scratch[kTeamBlock<kTeam> / kWave], scratch2[kTeamBlock<kTeam> / kWave];
+    __shared__ int32_t at[COMP_AMS_MAX_BUCKETS];
+    __shared__ float of_bucket[COMP_AMS_MAX_BUCKETS];
+    const Team<kTeam> me;
+    const unsigned bh = blockIdx.x / (unsigned)pieces, piece = blockIdx.x % (unsigned)pieces;
+    const int64_t b = bh / (unsigned)a.heads, h = bh % (unsigned)a.heads;
+    const int tk = (int)a.tk, i0 = (int)piece * rows_block, i1 = min(i0 + rows_block, (int)a.tq);
+    const int64_t by_length = key_len ? min((int64_t)max(key_len[b], 0), a.tk) : a.tk;
+    const T *s0 = s + b * a.s_b + h * a.s_h;
+    T *p0 = p + b * a.p_b + h * a.p_h;
+    v4u raw[kVecs];
+    int seen = 0;
+    auto fetch = [&](int i) {
+        seen = row_seen(i, by_length, a);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) raw[v] = load_slab<T, kTeam>(s0 + i * a.s_q, v * kTeam * E, me.lane, seen);
+    };
+    int i = i0 + me.id;
+    if (i < i1) fetch(i);
+    for (int q = threadIdx.x; q <= bounds.n; q += kTeamBlock<kTeam>) {
+        if (q < bounds.n) at[q] = bounds.at[q];
+        of_bucket[q] = table[q * a.heads + h];
+    }
+    __syncthreads();
+    const int64_t first = -(int64_t)(i1 - 1) - a.offset;               // the relative position of along[0]
+    for (int x = threadIdx.x; x < tk + (i1 - i0) - 1; x += kTeamBlock<kTeam>) along[x] = of_bucket[bucket_of(first + x, at, bounds.n)];
+    __syncthreads();
+    while (i < i1) {
+        float t[kVecs][E], top = -INFINITY;
+        const int sees = seen;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            const int slab = v * kTeam * E, j = slab + me.lane * E;
+            if (slab >= sees) {
+#pragma unroll
+                for (int q = 0; q < E; ++q) t[v][q] = -INFINITY;
+                continue;
+            }
+            widen<T>(raw[v], t[v]);
+            if (slab + kTeam * E <= sees) {
+                const float *bias = along + j + (i1 - 1 - i);
+#pragma unroll
+                for (int q = 0; q < E; ++q) t[v][q] = fmaf(t[v][q], a.scale, bias[q]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < E; ++q)
+                    t[v][q] = j + q < sees ? fmaf(t[v][q], a.scale, along[j + q + (i1 - 1 - i)]) : -INFINITY;
+            }
+#pragma unroll
+            for (int q = 0; q < E; ++q) top = fmaxf(top, t[v][q]);
+        }
+        const int next = i + kTeams;
+        if (next < i1) fetch(next);                                        // on its way while this row is worked on
+        top = team_reduce<LaxMaxOp, kTeam>(top, scratch);
+        const float from = top == -INFINITY ? 0.f : top;                   // an empty row: exponentials of -infinity
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            if (v * kTeam * E < sees) {
+#pragma unroll
+                for (int q = 0; q < E; ++q) {
+                    t[v][q] = __builtin_amdgcn_exp2f((t[v][q] - from) * kLog2e);
+                    sum += t[v][q];
+                }
+            }
+        }
+        sum = team_reduce<SumOp, kTeam>(sum, scratch2);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        T *row = p0 + i * a.p_q;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            const int slab = v * kTeam * E, j = slab + me.lane * E;
+            v4u out = {0u, 0u, 0u, 0u};
+            if (slab < sees) {
+#pragma unroll
+                for (int q = 0; q < E; ++q) {
+                    t[v][q] *= inv;
+                    if (slab + kTeam * E > sees && j + q >= sees) t[v][q] = 0.f;       // also in a row of NaN
+                }
+                out = narrow<T>(t[v]);
+            }
+            store_slab<T, kTeam>(row, slab, me.lane, tk, out);
+        }
+        i = next;
+    }
+}
+
+// Backward: a workgroup takes `rows_block` queries of one head and sequence, each team `rows_team` (a multiple of kStep) consecutive ones.
+// Of kStep rows and E keys that a lane holds, the diagonals are its registers' sums of the bucket gradient; every kStep rows they are
+// added to the team's array over relative positions in LDS, in two phases because the diagonals left of a lane's first key are its
+// neighbour's.  At the end the teams' arrays are added up over each bucket's positions, in a fixed order.  kBatch rows are in flight.
+template <typename T, int kTeam, int kVecs, int kStep, int kBatch>
+__global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float *__restrict__ work, const T *dp, const T *__restrict__ p,
+                                                                 Bounds bounds, const int32_t *__restrict__ key_len, BiasArgs a,
+                                                                 int pieces, int rows_team, unsigned worker_batch)
+{
+    constexpr int E = kVec<T>, kThreads = kTeamBlock<kTeam>, kTeams = kThreads / kTeam, kSlots = kTeam * kVecs * E;
+    static_assert(E % kStep == 0 && kStep % kBatch == 0, "whole batches in a step");
+    extern __shared__ float along[];                   // [teams][kSlots + rows_team - 1]
+    __shared__ float scratch[kBatch][kThreads / kWave];
+    __shared__ int32_t at[COMP_AMS_MAX_BUCKETS];
+    const Team<kTeam> me;
+    const unsigned bh = blockIdx.x / (unsigned)pieces, piece = blockIdx.x % (unsigned)pieces;
+    const unsigned b = bh / (unsigned)a.heads, h = bh % (unsigned)a.heads;
+    const int tk = (int)a.tk, tq = (int)a.tq, span = kSlots + rows_team - 1;
+    const int i0 = (int)piece * rows_team * kTeams, mine = i0 + me.id * rows_team, end = mine + rows_team;
+    const int64_t by_length = key_len ? min((int64_t)max(key_len[b], 0), a.tk) : a.tk;
+    const T *dp0 = dp + b * a.s_b + h * a.s_h, *p0 = p + b * a.p_b + h * a.p_h;
+    T *ds0 = ds + b * a.o_b + h * a.o_h;
+    float *diag = along + me.id * span;
+    for (int q = threadIdx.x; q < bounds.n; q += kThreads) at[q] = bounds.at[q];
+    for (int x = threadIdx.x; x < kTeams * span; x += kThreads) along[x] = 0.f;
+    __syncthreads();
+#pragma unroll 1
+    for (int first = mine; first < end; first += kStep) {
+        if (kTeam >= kWave && first >= tq) break;      // uniform over the team
+        float acc[kVecs][E + kStep - 1];
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+            for (int q = 0; q < E + kStep - 1; ++q) acc[v][q] = 0.f;
+#pragma unroll
+        for (int batch = 0; batch < kStep; batch += kBatch) {
+            v4u praw[kBatch][kVecs], draw[kBatch][kVecs];
+            int seen[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int i = first + batch + u;
+                seen[u] = i < tq ? row_seen(i, by_length, a) : 0;
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v) {
+                    praw[u][v] = load_slab<T, kTeam>(p0 + i * a.p_q, v * kTeam * E, me.lane, seen[u]);
+                    draw[u][v] = load_slab<T, kTeam>(dp0 + i * a.s_q, v * kTeam * E, me.lane, seen[u]);
+                }
+            }
+            auto row_sum = [&](int u) {
+                float s = 0.f;
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v) {
+                    if (v * kTeam * E < seen[u]) {
+                        float pw[E], dw[E];
+                        widen<T>(praw[u][v], pw);
+                        widen<T>(draw[u][v], dw);
+#pragma unroll
+                        for (int q = 0; q < E; ++q) s = fmaf(pw[q], dw[q], s);
+                    }
+                }
+                return s;
+            };
+            float total[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) total[u] = row_sum(u);
+            // the rows' reductions are independent: their steps interleave
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) total[u] = team_reduce<SumOp, kTeam>(total[u], scratch[u]);
+            // A key of probability zero takes no gradient whatever dp holds there.  While a row's sum is finite no product was NaN, so
+            // dp is finite there and the formula gives zero by itself; else such keys are cleared.
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if (!(fabsf(total[u]) < INFINITY)) {
+#pragma unroll
+                    for (int v = 0; v < kVecs; ++v) {
+                        float pw[E], dw[E];
+                        widen<T>(praw[u][v], pw);
+                        widen<T>(draw[u][v], dw);
+#pragma unroll
+                        for (int q = 0; q < E; ++q) dw[q] = pw[q] == 0.f ? 0.f : dw[q];
+                        draw[u][v] = narrow<T>(dw);
+                    }
+                    total[u] = team_reduce<SumOp, kTeam>(row_sum(u), scratch[u]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int i = first + batch + u;
+                T *row = ds0 + i * a.o_q;
+#pragma unroll
+                for (int v = 0; v < kVecs; ++v) {
+                    const int slab = v * kTeam * E;
+                    v4u out = {0u, 0u, 0u, 0u};
+                    if (slab < seen[u]) {
+                        float pw[E], dw[E];
+                        rewiden(praw[u][v]);
+                        rewiden(draw[u][v]);
+                        widen<T>(praw[u][v], pw);
+                        widen<T>(draw[u][v], dw);
+#pragma unroll
+                        for (int q = 0; q < E; ++q) {
+                            const float dt = pw[q] * (dw[q] - total[u]);
+                            acc[v][q - (batch + u) + kStep - 1] += dt;
+                            dw[q] = dt * a.scale;
+                        }
+                        out = narrow<T>(dw);
+                    }
+                    if (i < tq) store_slab<T, kTeam>(row, slab, me.lane, tk, out);
+                }
+            }
+        }
+        // diagonal a of the lane: key j0 + a seen from row `first`
+        float *to = diag + (end - 1 - first) + me.lane * E;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+            for (int q = 0; q < E; ++q) to[v * kTeam * E + q] += acc[v][q + kStep - 1];
+        if constexpr (kTeam > kWave) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+            for (int q = 1; q < kStep; ++q) to[v * kTeam * E - q] += acc[v][kStep - 1 - q];
+        if constexpr (kTeam > kWave) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    __syncthreads();
+    // Over the whole workgroup: place x is key x seen from its last row; team t's array begins (kTeams - 1 - t) rows_team further on.
+    const int places = kSlots + kTeams * rows_team - 1;
+    const int64_t base = -(int64_t)(i0 + kTeams * rows_team - 1) - a.offset;      // relative position of place 0
+    const unsigned w = b / worker_batch;
+    const int64_t parts = (int64_t)worker_batch * pieces, part = (int64_t)(b - w * worker_batch) * pieces + piece;
+    float *out = work + ((int64_t)(w * (unsigned)a.heads + h) * (bounds.n + 1)) * parts + part;
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int q = threadIdx.x / kWave; q <= bounds.n; q += kThreads / kWave) {
+        const int64_t from = q == 0 ? 0 : at[q - 1] - base, to = q == bounds.n ? places : at[q] - base;
+        const int x0 = (int)min(max(from, (int64_t)0), (int64_t)places), x1 = (int)min(max(to, (int64_t)0), (int64_t)places);
+        float s = 0.f;
+        for (int x = x0 + lane; x < x1; x += kWave) {
+#pragma unroll
+            for (int t = 0; t < kTeams; ++t) {
+                const int y = x - (kTeams - 1 - t) * rows_team;
+                if (y >= 0 && y < span) s += along[t * span + y];
+            }
+        }
+        s = lanes_reduce<SumOp, kWave>(s);
+        if (lane == 0) out[q * parts] = s;
+    }
+}
+
+// work[worker][heads][buckets][parts] -> dtable[worker][buckets][heads]; one wavefront per (bucket, head, worker), lanes in a fixed
+// order.
 template <typename G>
 __global__ __launch_bounds__(kWave) void bias_table_join(G *__restrict__ dtable, const float *__restrict__ work, int64_t heads,
-                                                         int64_t worker_batch, int64_t pieces, int buckets, int64_t grad_stride)
+                                                         int64_t parts, int buckets, int64_t grad_stride)
 {
     const int64_t w = blockIdx.z, h = blockIdx.y, q = blockIdx.x;
+    const float *in = work + ((w * heads + h) * buckets + q) * parts;
     float s = 0.f;
-    for (int64_t t = threadIdx.x; t < worker_batch * pieces; t += kWave) {
-        const int64_t b = w * worker_batch + t / pieces, piece = t % pieces;
-        s += work[((b * heads + h) * pieces + piece) * buckets + q];
-    }
+#pragma unroll 4
+    for (int64_t t = threadIdx.x; t < parts; t += kWave) s += in[t];
     s = lanes_reduce<SumOp, kWave>(s);
     if (threadIdx.x == 0) dtable[w * grad_stride + q * heads + h] = narrow1<G>(s);
 }

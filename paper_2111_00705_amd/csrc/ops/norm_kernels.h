@@ -86,17 +86,191 @@ __global__ __launch_bounds__(kNormThreads) void norm_param_any(float *__restrict
     out[a.cols + c] = db;
 }
 
-// The chunks' sums, added in ascending order, into the workers' rows of gradients.
+// --- rows that a team of lanes holds in registers -----------------------------------------------------------------------
+//
+// A team (16 lanes, a wavefront, or a workgroup) reads a row once, kVecs vectors a lane, and takes mean and variance from the
+// registers; gain and shift stay in registers over the rows that a team takes in turn.
+
+template <typename T, int kTeam, int kVecs>
+__global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_forward(T *y, float *__restrict__ mean, float *__restrict__ rstd, const T *x,
+                                                                     const float *__restrict__ gain, const float *__restrict__ shift,
+                                                                     NormArgs a)
+{
+    constexpr int E = kVec<T>, kTeams = kTeamBlock<kTeam> / kTeam;
+    __shared__ float scratch[kTeamBlock<kTeam> / kWave], scratch2[kTeamBlock<kTeam> / kWave];
+    const Team<kTeam> me;
+    const int cols = (int)a.cols;
+    int64_t row = (int64_t)blockIdx.x * kTeams + me.id;
+    if (row >= a.rows) return;                       // a whole team; with one team per workgroup, the whole workgroup
+    v4u raw[kVecs];
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) raw[v] = load_slab<T, kTeam>(x + r * a.x_stride, v * kTeam * E, me.lane, cols);
+    };
+    fetch(row);
+    float g[kVecs][E], b[kVecs][E];
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+        load_params<T, kTeam>(g[v], gain, v * kTeam * E, me.lane, cols);
+        if (shift) {
+            load_params<T, kTeam>(b[v], shift, v * kTeam * E, me.lane, cols);
+        } else {
+#pragma unroll
+            for (int q = 0; q < E; ++q) b[v][q] = 0.f;
+        }
+    }
+    for (;;) {
+        float d[kVecs][E], s = 0.f;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            widen<T>(raw[v], d[v]);
+#pragma unroll
+            for (int q = 0; q < E; ++q) s += d[v][q];
+        }
+        const int64_t next = row + (int64_t)gridDim.x * kTeams;
+        if (next < a.rows) fetch(next);              // on its way while this row is worked on
+        const float mu = team_reduce<SumOp, kTeam>(s, scratch) * a.inv_cols;
+        float var = 0.f;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            const int at = v * kTeam * E + me.lane * E;
+#pragma unroll
+            for (int q = 0; q < E; ++q) {
+                d[v][q] -= mu;
+                if ((v + 1) * kTeam * E <= cols || at + q < cols) var = fmaf(d[v][q], d[v][q], var);
+            }
+        }
+        const float r = 1.f / sqrtf(fmaf(team_reduce<SumOp, kTeam>(var, scratch2), a.inv_cols, a.eps));
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+#pragma unroll
+            for (int q = 0; q < E; ++q) d[v][q] = fmaf(d[v][q] * r, g[v][q], b[v][q]);
+            store_slab<T, kTeam>(y + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(d[v]));
+        }
+        if (me.lane == 0) {
+            if (mean) mean[row] = mu;
+            if (rstd) rstd[row] = r;
+        }
+        if (next >= a.rows) return;
+        row = next;
+    }
+}
+
+// Backward: the rows of one chunk of one worker, the teams in turn; every lane adds up the parameter gradients of its columns over
+// its rows, the teams' sums are joined in order, and work[worker][chunk] receives 2 x cols of them.
+template <typename T, int kTeam, int kVecs>
+__global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_backward(T *dx, float *__restrict__ work, const T *dy, const T *x,
+                                                                      const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                      const float *__restrict__ gain, NormArgs a, int64_t worker_rows,
+                                                                      int64_t chunk_rows)
+{
+    constexpr int E = kVec<T>, kTeams = kTeamBlock<kTeam> / kTeam, kSlots = kTeam * kVecs * E;
+    __shared__ float scratch[kTeamBlock<kTeam> / kWave], scratch2[kTeamBlock<kTeam> / kWave];
+    __shared__ float joined[kTeams > 1 ? kTeams * kSlots : 1];
+    const Team<kTeam> me;
+    const int cols = (int)a.cols;
+    const int64_t base = (int64_t)blockIdx.y * worker_rows;
+    const int64_t lo = base + (int64_t)blockIdx.x * chunk_rows, hi = base + min(((int64_t)blockIdx.x + 1) * chunk_rows, worker_rows);
+    float g[kVecs][E], dg[kVecs][E], db[kVecs][E];
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+        load_params<T, kTeam>(g[v], gain, v * kTeam * E, me.lane, cols);
+#pragma unroll
+        for (int q = 0; q < E; ++q) dg[v][q] = db[v][q] = 0.f;
+    }
+    v4u xraw[kVecs], dyraw[kVecs];
+    float mu = 0.f, r = 0.f;
+    auto fetch = [&](int64_t at) {
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            xraw[v] = load_slab<T, kTeam>(x + at * a.x_stride, v * kTeam * E, me.lane, cols);
+            dyraw[v] = load_slab<T, kTeam>(dy + at * a.dy_stride, v * kTeam * E, me.lane, cols);
+        }
+        mu = mean[at];
+        r = rstd[at];
+    };
+    int64_t row = lo + me.id;
+    if (row < hi) fetch(row);
+    while (row < hi) {
+        float xh[kVecs][E], up[kVecs][E], s = 0.f, q2 = 0.f;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            widen<T>(xraw[v], xh[v]);
+            widen<T>(dyraw[v], up[v]);
+#pragma unroll
+            for (int q = 0; q < E; ++q) {
+                xh[v][q] = (xh[v][q] - mu) * r;        // past the row: finite, times a zero gradient
+                const float t = up[v][q] * g[v][q];
+                s += t;
+                q2 = fmaf(t, xh[v][q], q2);
+                dg[v][q] = fmaf(up[v][q], xh[v][q], dg[v][q]);
+                db[v][q] += up[v][q];
+            }
+        }
+        const float scale = r;
+        const int64_t next = row + kTeams;
+        if (next < hi) fetch(next);
+        s = team_reduce<SumOp, kTeam>(s, scratch) * a.inv_cols;
+        q2 = team_reduce<SumOp, kTeam>(q2, scratch2) * a.inv_cols;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+#pragma unroll
+            for (int q = 0; q < E; ++q) up[v][q] = scale * (fmaf(up[v][q], g[v][q], -s) - xh[v][q] * q2);
+            store_slab<T, kTeam>(dx + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(up[v]));
+        }
+        row = next;
+    }
+    float *out = work + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.cols;
+    auto emit = [&](float (&acc)[kVecs][E], float *to) {
+        if constexpr (kTeams == 1) {
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+                for (int q = 0; q < E; ++q) {
+                    const int c = v * kTeam * E + me.lane * E + q;
+                    if (c < cols) to[c] = acc[v][q];
+                }
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+                for (int q = 0; q < E; ++q) joined[me.id * kSlots + v * kTeam * E + me.lane * E + q] = acc[v][q];
+            __syncthreads();
+            for (int c = threadIdx.x; c < cols; c += kTeamBlock<kTeam>) {
+                float sum = joined[c];
+#pragma unroll
+                for (int t = 1; t < kTeams; ++t) sum += joined[t * kSlots + c];
+                to[c] = sum;
+            }
+        }
+    };
+    emit(dg, out);
+    emit(db, out + a.cols);
+}
+
+// The chunks' sums into the workers' rows of gradients: 32 columns a workgroup, eight lanes a column that take every eighth chunk
+// in ascending order and are then added in order.
+constexpr int kJoinCols = 32, kJoinParts = kNormThreads / kJoinCols;
 template <typename G>
 __global__ __launch_bounds__(kNormThreads) void norm_param_join(G *__restrict__ dgain, G *__restrict__ dshift,
                                                                 const float *__restrict__ work, int64_t cols, int chunks,
                                                                 int64_t grad_stride)
 {
-    const int64_t c = (int64_t)blockIdx.x * kNormThreads + threadIdx.x;
-    if (c >= 2 * cols) return;
-    const float *in = work + (int64_t)blockIdx.y * chunks * 2 * cols + c;
+    __shared__ float parts[kJoinParts][kJoinCols];
+    const int part = threadIdx.x / kJoinCols, lane = threadIdx.x % kJoinCols;
+    const int64_t c = (int64_t)blockIdx.x * kJoinCols + lane;
     float s = 0.f;
-    for (int q = 0; q < chunks; ++q) s += in[(int64_t)q * 2 * cols];
+    if (c < 2 * cols) {
+        const float *in = work + (int64_t)blockIdx.y * chunks * 2 * cols + c;
+#pragma unroll 8
+        for (int q = part; q < chunks; q += kJoinParts) s += in[(int64_t)q * 2 * cols];
+    }
+    parts[part][lane] = s;
+    __syncthreads();
+    if (part != 0 || c >= 2 * cols) return;
+#pragma unroll
+    for (int q = 1; q < kJoinParts; ++q) s += parts[q][lane];
     const int64_t at = (int64_t)blockIdx.y * grad_stride;
     if (c < cols) dgain[at + c] = narrow1<G>(s);
     else if (dshift) dshift[at + c - cols] = narrow1<G>(s);

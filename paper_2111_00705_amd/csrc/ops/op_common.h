@@ -80,6 +80,10 @@ template <> __device__ __forceinline__ v4u narrow<f16_t>(const float (&x)[8])
 template <typename T> __device__ __forceinline__ v4u load_vec(const T *p) { return *reinterpret_cast<const v4u_any *>(p); }
 template <typename T> __device__ __forceinline__ void store_vec(T *p, const v4u &v) { *reinterpret_cast<v4u_any *>(p) = v; }
 
+// Makes the compiler take what is widened from `v` before and after for different values: a row held in registers is widened anew
+// by each pass over it, instead of being kept in its wide form too.
+__device__ __forceinline__ void rewiden(v4u &v) { asm volatile("" : "+v"(v)); }
+
 template <typename T> __device__ __forceinline__ uint32_t bits1(T x);
 template <> __device__ __forceinline__ uint32_t bits1<float>(float x) { return __float_as_uint(x); }
 template <> __device__ __forceinline__ uint32_t bits1<bf16_t>(bf16_t x) { return x.v; }
@@ -93,8 +97,8 @@ template <typename T> __device__ __forceinline__ void put_bits(v4u &raw, int q, 
 }
 
 // Row elements [at, at + kVec) of a row of `len`, those outside [0, len) as `fill` bits.  Touches nothing outside the row.
-template <typename T>
-__device__ __forceinline__ v4u load_row(const T *row, int64_t at, int64_t len, uint32_t fill = 0u)
+template <typename T, typename I>      // I: int or int64_t
+__device__ __forceinline__ v4u load_row(const T *row, I at, I len, uint32_t fill = 0u)
 {
     constexpr int E = kVec<T>;
     if (at >= 0 && at + E <= len) return load_vec(row + at);
@@ -107,8 +111,8 @@ __device__ __forceinline__ v4u load_row(const T *row, int64_t at, int64_t len, u
     }
     return raw;
 }
-template <typename T>
-__device__ __forceinline__ void store_row(T *row, int64_t at, int64_t len, const v4u &raw)
+template <typename T, typename I>
+__device__ __forceinline__ void store_row(T *row, I at, I len, const v4u &raw)
 {
     constexpr int E = kVec<T>;
     if (at >= 0 && at + E <= len) {
@@ -124,18 +128,82 @@ __device__ __forceinline__ void store_row(T *row, int64_t at, int64_t len, const
         }
 }
 
+// A row that a team of kTeam lanes holds in registers lies in slabs of kTeam vectors, lane after lane.  `first` is a slab's first
+// element; a slab that lies inside [0, len) is loaded without a look at the lanes.  Offsets stay 32-bit beside the row's address.
+template <typename T, int kTeam>
+__device__ __forceinline__ v4u load_slab(const T *row, int first, int lane, int len, uint32_t fill = 0u)
+{
+    constexpr int E = kVec<T>;
+    const int at = first + lane * E;
+    if (first + kTeam * E <= len) return load_vec(reinterpret_cast<const T *>(reinterpret_cast<const char *>(row) + (uint32_t)at * (uint32_t)sizeof(T)));
+    return load_row(row, at, len, fill);
+}
+template <typename T, int kTeam>
+__device__ __forceinline__ void store_slab(T *row, int first, int lane, int len, const v4u &raw)
+{
+    constexpr int E = kVec<T>;
+    const int at = first + lane * E;
+    if (first + kTeam * E <= len) store_vec(reinterpret_cast<T *>(reinterpret_cast<char *>(row) + (uint32_t)at * (uint32_t)sizeof(T)), raw);
+    else store_row(row, at, len, raw);
+}
+// Parameters (fp32) of the same elements: kVec<T> floats.
+template <typename T, int kTeam>
+__device__ __forceinline__ void load_params(float (&x)[kVec<T>], const float *p, int first, int lane, int len)
+{
+    constexpr int E = kVec<T>;
+    const int at = first + lane * E;
+#pragma unroll
+    for (int u = 0; u < E; u += 4) {
+        float four[4];
+        widen<float>(load_row(p, at + u, len), four);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[u + q] = four[q];
+    }
+}
+
+// Which team of the workgroup a lane belongs to, and its place in the team.
+template <int kTeam> struct Team {
+    int id, lane;
+    __device__ __forceinline__ Team()
+    {
+        if constexpr (kTeam >= kWave) id = __builtin_amdgcn_readfirstlane(threadIdx.x / kTeam);   // uniform: rows get scalar addresses
+        else id = threadIdx.x / kTeam;
+        lane = threadIdx.x & (kTeam - 1);
+    }
+};
+// Threads of the workgroup that such teams share.
+template <int kTeam> constexpr int kTeamBlock = kTeam > 256 ? kTeam : 256;
+
 // --- reductions over a team of kTeam lanes (a power of two; a wavefront or less: lanes side by side; more: the whole
 // workgroup).  Fixed trees: the result depends on the lanes' values only, and every lane of the team receives it. ---------
 
+// fmaxf ignores NaN, and is one instruction: for maxima whose row shows a NaN elsewhere.
+struct LaxMaxOp { static __device__ __forceinline__ float apply(float a, float b) { return fmaxf(a, b); } };
 struct SumOp { static __device__ __forceinline__ float apply(float a, float b) { return a + b; } };
 // NaN wins: a row with a NaN must not look like one without.
 struct MaxOp { static __device__ __forceinline__ float apply(float a, float b) { return (a > b || a != a) ? a : b; } };
 
+// The permutes that ride in a vector instruction: a neighbour, the other pair, the other four, the other eight of a row of sixteen
+// lanes; then the four rows through scalar registers.  (Six __shfl_xor are six round trips through the LDS unit.)  Every lane of the
+// rows that take part must be active.
+template <int kCtrl> __device__ __forceinline__ float dpp(float v)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), kCtrl, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float lane_value(float v, int lane)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane));
+}
 template <typename Op, int kLanes>
 __device__ __forceinline__ float lanes_reduce(float v)
 {
-#pragma unroll
-    for (int off = kLanes / 2; off >= 1; off >>= 1) v = Op::apply(v, __shfl_xor(v, off, kWave));
+    static_assert(kLanes == 16 || kLanes == 64, "a row of lanes or a wavefront");
+    v = Op::apply(v, dpp<0xb1>(v));        // quad_perm [1,0,3,2]
+    v = Op::apply(v, dpp<0x4e>(v));        // quad_perm [2,3,0,1]
+    v = Op::apply(v, dpp<0x141>(v));       // row_half_mirror
+    v = Op::apply(v, dpp<0x140>(v));       // row_mirror
+    if constexpr (kLanes == 64)
+        v = Op::apply(Op::apply(lane_value(v, 0), lane_value(v, 16)), Op::apply(lane_value(v, 32), lane_value(v, 48)));
     return v;
 }
 

@@ -69,6 +69,37 @@ void with_type(int32_t type, F &&f)
         REQUIRE((stride) >= 0 && ((rows) <= 1 || (stride) < kMaxElements / (rows)), "%s: %s is out of range", what, name);        \
     } while (0)
 
+// --- constants chosen from sizes, as types ---------------------------------------------------------------------------
+
+// f(Shape) with `vecs`, in [kLeast, kVecs], as a compile-time constant.
+template <int kThreads, int kVecs> struct Shape {
+    static constexpr int threads = kThreads, vecs = kVecs;
+};
+template <int kThreads, int kLeast, int kVecs, typename F>
+void with_vecs(int vecs, F &&f)
+{
+    if constexpr (kVecs == kLeast) {
+        f(Shape<kThreads, kVecs>{});
+    } else {
+        if (vecs >= kVecs) f(Shape<kThreads, kVecs>{});
+        else with_vecs<kThreads, kLeast, kVecs - 1>(vecs, f);
+    }
+}
+
+// f(Shape) with the team of lanes and the vectors a lane that hold a row of `len` elements in registers: 16 lanes up to 32 vectors,
+// a wavefront up to 256, a workgroup of 256 up to 1024, of 1024 up to 2048.  false if the row is longer than that.
+template <typename T, typename F>
+bool with_team(int64_t len, F &&f)
+{
+    const int64_t vecs = ceil_div(len, kVec<T>);
+    if (vecs <= 32) with_vecs<16, 1, 2>((int)ceil_div(vecs, 16), f);
+    else if (vecs <= 256) with_vecs<64, 1, 4>((int)ceil_div(vecs, 64), f);
+    else if (vecs <= 1024) with_vecs<256, 2, 4>((int)ceil_div(vecs, 256), f);
+    else if (vecs <= 2048) f(Shape<1024, 2>{});
+    else return false;
+    return true;
+}
+
 // --- layer norm ---------------------------------------------------------------------------------------------------
 
 int norm_check(const char *what, int64_t rows, int64_t cols, int32_t type)
@@ -78,6 +109,8 @@ int norm_check(const char *what, int64_t rows, int64_t cols, int32_t type)
     REQUIRE(cols >= 1 && cols < (int64_t)1 << 31, "%s: cols=%lld must be in [1, 2^31)", what, (long long)cols);
     return COMP_AMS_OK;
 }
+
+constexpr int64_t kNormBlocks = 2048;
 
 // How a worker's rows are cut for the parameter gradients: chunks of rows with one set of column sums each.
 struct NormChunks {
@@ -131,7 +164,19 @@ int bias_strides(const char *what, const char *name, const void *p, int64_t batc
     return COMP_AMS_OK;
 }
 
-int64_t bias_pieces(int64_t tq) { return ceil_div(tq, kBiasAnyRows); }
+// How the queries of a head and sequence are cut for the backward pass: the registers' form takes rows_team consecutive queries a team.
+struct BiasShape {
+    bool held;               // false: bias_backward_any
+    int32_t rows_team, rows_block;
+    int64_t pieces;
+};
+BiasShape bias_backward_shape(int64_t tq, int64_t tk, int32_t type)
+{
+    const int64_t e = 16 / (int64_t)type_size(type), vecs = ceil_div(std::max<int64_t>(tk, 1), e);
+    if (vecs > 1024) return {false, kBiasAnyRows, kBiasAnyRows, ceil_div(tq, kBiasAnyRows)};
+    const int32_t teams = vecs <= 32 ? 16 : vecs <= 256 ? 4 : 1, rows = (int32_t)(vecs <= 256 ? e : 2 * e);
+    return {true, rows, rows * teams, ceil_div(tq, rows * teams)};
+}
 
 // --- vocabulary rows ----------------------------------------------------------------------------------------------------
 
@@ -186,21 +231,6 @@ PieceShape piece_shape(int64_t rows, int64_t vocab, int32_t type)
     return s;
 }
 
-// f(threads, vecs) with both as compile-time constants.
-template <int kThreads, int kVecs> struct Shape {
-    static constexpr int threads = kThreads, vecs = kVecs;
-};
-template <int kThreads, int kVecs, typename F>
-void with_vecs(int vecs, F &&f)
-{
-    if constexpr (kVecs == 1) {
-        f(Shape<kThreads, 1>{});
-    } else {
-        if (vecs >= kVecs) f(Shape<kThreads, kVecs>{});
-        else with_vecs<kThreads, kVecs - 1>(vecs, f);
-    }
-}
-
 }  // namespace
 
 extern "C" {
@@ -222,8 +252,15 @@ int comp_ams_layer_norm(void *y, float *mean, float *rstd, const void *x, const 
     const NormArgs a = {rows, cols, x_stride, y_stride, 0, eps, (float)(1.0 / (double)cols)};
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        norm_forward_any<T><<<(unsigned)std::min(rows, kMaxGrid), kNormThreads, 0, stream>>>(static_cast<T *>(y), mean, rstd,
-                                                                                          static_cast<const T *>(x), gain, shift, a);
+        const bool held = with_team<T>(cols, [&](auto shape) {
+            using S = decltype(shape);
+            const int64_t teams = kTeamBlock<S::threads> / S::threads;
+            norm_forward<T, S::threads, S::vecs><<<(unsigned)std::min<int64_t>(ceil_div(rows, teams), kNormBlocks), kTeamBlock<S::threads>, 0, stream>>>(
+                static_cast<T *>(y), mean, rstd, static_cast<const T *>(x), gain, shift, a);
+        });
+        if (!held)
+            norm_forward_any<T><<<(unsigned)std::min(rows, kMaxGrid), kNormThreads, 0, stream>>>(static_cast<T *>(y), mean, rstd,
+                                                                                              static_cast<const T *>(x), gain, shift, a);
     });
     return launched(what);
 }
@@ -266,6 +303,12 @@ int comp_ams_layer_norm_backward(void *dx, void *dgain, void *dshift, const void
     float *sums = static_cast<float *>(work);
     with_type(type, [&](auto t) {
         using T = decltype(t);
+        const bool held = with_team<T>(cols, [&](auto shape) {
+            using S = decltype(shape);
+            norm_backward<T, S::threads, S::vecs><<<dim3((unsigned)ch.count, (unsigned)n), kTeamBlock<S::threads>, 0, stream>>>(
+                static_cast<T *>(dx), sums, static_cast<const T *>(dy), static_cast<const T *>(x), mean, rstd, gain, a, rows / n, ch.rows);
+        });
+        if (held) return;
         // the parameter gradients first: dx may replace dy or x
         norm_param_any<T><<<dim3((unsigned)ceil_div(cols, kNormThreads), (unsigned)ch.count, (unsigned)n), kNormThreads, 0, stream>>>(
             sums, static_cast<const T *>(dy), static_cast<const T *>(x), mean, rstd, a, rows / n, ch.rows);
@@ -275,7 +318,7 @@ int comp_ams_layer_norm_backward(void *dx, void *dgain, void *dshift, const void
     });
     with_type(grad_type, [&](auto t) {
         using G = decltype(t);
-        norm_param_join<G><<<dim3((unsigned)ceil_div(2 * cols, kNormThreads), (unsigned)n), kNormThreads, 0, stream>>>(
+        norm_param_join<G><<<dim3((unsigned)ceil_div(2 * cols, kJoinCols), (unsigned)n), kNormThreads, 0, stream>>>(
             static_cast<G *>(dgain), static_cast<G *>(dshift), sums, cols, (int)ch.count, grad_stride);
     });
     return launched(what);
@@ -301,6 +344,19 @@ int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const 
     a.offset = offset, a.scale = scale, a.causal = causal != 0;
     with_type(type, [&](auto t) {
         using T = decltype(t);
+        const bool held = tk <= 1024 * kVec<T> && with_team<T>(tk, [&](auto shape) {
+            using S = decltype(shape);
+            if constexpr (S::threads <= 256) {
+                constexpr int kTeams = kTeamBlock<S::threads> / S::threads;
+                const int rows_block = (int)std::min<int64_t>(tq, kTeams * 8);
+                const int64_t pieces = ceil_div(tq, rows_block);
+                const size_t lds = (size_t)(tk + rows_block - 1) * sizeof(float);
+                bias_forward<T, S::threads, S::vecs><<<(unsigned)(batch * heads * pieces), kTeamBlock<S::threads>, lds,
+                                                      static_cast<hipStream_t>(hip_stream)>>>(
+                    static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a, (int)pieces, rows_block);
+            }
+        });
+        if (held) return;
         bias_forward_any<T><<<(unsigned)a.rows, kBiasThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
             static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a);
     });
@@ -314,7 +370,7 @@ int comp_ams_rel_bias_work_bytes(int64_t batch, int64_t heads, int64_t tq, int64
     if (const int rc = bias_check(what, nullptr, 1, nullptr, batch, heads, tq, tk, 0, 1.f, type, &none)) return rc;
     REQUIRE(n_buckets >= 1 && n_buckets <= COMP_AMS_MAX_BUCKETS, "%s: n_buckets=%d must be in [1, %d]", what, n_buckets, COMP_AMS_MAX_BUCKETS);
     REQUIRE(bytes, "%s: bytes is NULL", what);
-    *bytes = (uint64_t)(batch * heads * bias_pieces(tq)) * (uint64_t)n_buckets * sizeof(float);
+    *bytes = (uint64_t)(batch * heads * bias_backward_shape(tq, tk, type).pieces) * (uint64_t)n_buckets * sizeof(float);
     return COMP_AMS_OK;
 }
 
@@ -346,7 +402,7 @@ int comp_ams_rel_bias_softmax_backward(void *ds, void *dtable, const void *dp, c
     }
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     float *sums = static_cast<float *>(work);
-    const int64_t pieces = bias_pieces(tq);
+    const BiasShape cut = bias_backward_shape(tq, tk, type);
     if (!empty) {
         BiasArgs a = {};
         a.heads = heads, a.tq = tq, a.tk = tk, a.rows = batch * heads * tq;
@@ -356,14 +412,29 @@ int comp_ams_rel_bias_softmax_backward(void *ds, void *dtable, const void *dp, c
         a.offset = offset, a.scale = scale, a.causal = causal != 0;
         with_type(type, [&](auto t) {
             using T = decltype(t);
-            bias_backward_any<T><<<(unsigned)(batch * heads * pieces), kBiasAnyThreads, 0, stream>>>(
-                static_cast<T *>(ds), sums, static_cast<const T *>(dp), static_cast<const T *>(p), bounds, key_len, a, pieces);
+            const unsigned grid = (unsigned)(batch * heads * cut.pieces);
+            if (!cut.held) {
+                bias_backward_any<T><<<grid, kBiasAnyThreads, 0, stream>>>(static_cast<T *>(ds), sums, static_cast<const T *>(dp),
+                                                                          static_cast<const T *>(p), bounds, key_len, a, cut.pieces, batch / n);
+                return;
+            }
+            with_team<T>(tk, [&](auto shape) {
+                using S = decltype(shape);
+                if constexpr (S::threads <= 256) {
+                    constexpr int kTeams = kTeamBlock<S::threads> / S::threads, kStep = S::vecs > 2 ? 4 : kVec<T>,
+                                  kBatch = S::vecs == 1 ? 4 : S::vecs == 2 ? 2 : 1;
+                    const size_t lds = (size_t)kTeams * (S::threads * S::vecs * kVec<T> + cut.rows_team - 1) * sizeof(float);
+                    bias_backward<T, S::threads, S::vecs, kStep, kBatch><<<grid, kTeamBlock<S::threads>, lds, stream>>>(
+                        static_cast<T *>(ds), sums, static_cast<const T *>(dp), static_cast<const T *>(p), bounds, key_len, a,
+                        (int)cut.pieces, cut.rows_team, (unsigned)(batch / n));
+                }
+            });
         });
     }
     with_type(grad_type, [&](auto t) {
         using G = decltype(t);
         bias_table_join<G><<<dim3((unsigned)n_buckets, (unsigned)heads, (unsigned)n), kWave, 0, stream>>>(
-            static_cast<G *>(dtable), sums, heads, empty ? 0 : batch / n, pieces, n_buckets, grad_stride);
+            static_cast<G *>(dtable), sums, heads, empty ? 0 : batch / n * cut.pieces, n_buckets, grad_stride);
     });
     return launched(what);
 }
@@ -412,7 +483,7 @@ int comp_ams_token_logprobs(float *logp, float *entropy, int32_t *top_idx, float
             logprobs_regs<T, S::threads, S::vecs><<<(unsigned)(rows * s.count), S::threads, 0, stream>>>(
                 logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, groups, s.count, s.len, pieces, keys);
         };
-        if (s.threads == kPieceThreads) with_vecs<kPieceThreads, kPieceVecs>(s.vecs, launch);
+        if (s.threads == kPieceThreads) with_vecs<kPieceThreads, 1, kPieceVecs>(s.vecs, launch);
         else launch(Shape<kPieceThreads / 2, 1>{});
         if (s.count > 1)
             logprobs_join<T><<<(unsigned)rows, kVocabThreads, (size_t)s.count * k * sizeof(uint64_t), stream>>>(
@@ -485,8 +556,8 @@ int comp_ams_distill_grad(float *loss, void *dlogits, const float *dloss, const 
         };
         const int64_t vecs = ceil_div(vocab, kVec<T>);          // vectors of the row
         if (vecs <= 256) launch(Shape<256, 1>{});
-        else if (vecs <= 512 * 8) with_vecs<512, 8>((int)ceil_div(vecs, 512), launch);
-        else if (vecs <= 1024 * 8) with_vecs<1024, 8>((int)ceil_div(vecs, 1024), launch);
+        else if (vecs <= 512 * 8) with_vecs<512, 1, 8>((int)ceil_div(vecs, 512), launch);
+        else if (vecs <= 1024 * 8) with_vecs<1024, 5, 8>((int)ceil_div(vecs, 1024), launch);
         else if (vecs <= 1024 * 16) launch(Shape<1024, 16>{});
         else launch(Shape<1024, 0>{});
     });

@@ -210,6 +210,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_regs(float *__restrict__ lo
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
             float x[E];
+            rewiden(raw[v]);
             widen<T>(raw[v], x);
 #pragma unroll
             for (int q = 0; q < E; ++q) {
@@ -246,6 +247,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_regs(float *__restrict__ lo
             for (int v = 0; v < kVecs; ++v) {
                 if (vec_max[v] >= bound) {
                     float x[E];
+                    rewiden(raw[v]);
                     widen<T>(raw[v], x);
 #pragma unroll
                     for (int q = 0; q < E; ++q) {
@@ -427,7 +429,7 @@ __device__ __forceinline__ void merge_list(Listed &e, int k)
 
 // Maximum and sum of a row's elements [at, at + kVecs kThreads E) taken into this thread's (top, sum).
 template <typename T, int kThreads, int kVecs>
-__device__ __forceinline__ void take_chunk(Lse &v, const v4u (&raw)[kVecs], float unit)
+__device__ __forceinline__ void take_chunk(Lse &v, v4u (&raw)[kVecs], float unit)
 {
     constexpr int E = kVec<T>;
     float top = v.top;
@@ -443,6 +445,7 @@ __device__ __forceinline__ void take_chunk(Lse &v, const v4u (&raw)[kVecs], floa
 #pragma unroll
     for (int r = 0; r < kVecs; ++r) {
         float x[E];
+        rewiden(raw[r]);
         widen<T>(raw[r], x);
 #pragma unroll
         for (int q = 0; q < E; ++q) s += __builtin_amdgcn_exp2f((x[q] - from) * unit);
@@ -571,6 +574,7 @@ __global__ __launch_bounds__(kThreads) void distill_both(float *__restrict__ los
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) {
             float x[E];
+            rewiden(raw[r]);
             widen<T>(raw[r], x);
 #pragma unroll
             for (int q = 0; q < E; ++q) x[q] = gradient(x[q]);
