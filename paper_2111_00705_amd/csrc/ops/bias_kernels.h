@@ -57,7 +57,7 @@ template <typename T>
 __global__ __launch_bounds__(kBiasThreads) void bias_forward_any(T *p, const T *s, const float *__restrict__ table, Bounds bounds,
                                                                  const int32_t *__restrict__ key_len, BiasArgs a)
 {
-    __shared__ float scratch[kBiasThreads / kWave];
+    __shared__ float scratch[kBiasThreads / kWave], scratch2[kBiasThreads / kWave];
     __shared__ int32_t at[COMP_AMS_MAX_BUCKETS];
     __shared__ float bias[COMP_AMS_MAX_BUCKETS];
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kBiasThreads) void bias_forward_any(T *p, const T *
         float sum = 0.f;
         if (!none)
             for (int64_t j = threadIdx.x; j < seen; j += kBiasThreads) sum += __builtin_amdgcn_exp2f((score(j) - top) * kLog2e);
-        sum = team_reduce<SumOp, kBiasThreads>(sum, scratch);
+        sum = team_reduce<SumOp, kBiasThreads>(sum, scratch2);
         const float inv = 1.f / sum;
         for (int64_t j = threadIdx.x; j < a.tk; j += kBiasThreads)
             pr[j] = narrow1<T>(j < seen && !none ? __builtin_amdgcn_exp2f((score(j) - top) * kLog2e) * inv : 0.f);
@@ -142,8 +142,8 @@ __device__ __forceinline__ int row_seen(int64_t i, int64_t seen_by_length, const
 }
 
 // Forward: a workgroup takes `rows_block` queries of one head and sequence, its teams in turn.  The head's bias over the relative
-// positions that occur there is laid out in LDS first, [tk + rows_block - 1] floats, so that a vector of keys finds its biases side by
-// side.
+// positions that occur there is laid out in LDS first, [tk + rows_block - 1] floats in units of log 2, so that a vector of keys finds its
+// biases side by side.
 template <typename T, int kTeam, int kVecs>
 __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_forward(T *p, const T *s, const float *__restrict__ table, Bounds bounds,
                                                                 const int32_t *__restrict__ key_len, BiasArgs a, int pieces, int rows_block)
@@ -165,73 +165,91 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_forward(T *p, const T 
     auto fetch = [&](int i) {
         seen = row_seen(i, by_length, a);
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) raw[v] = load_slab<T, kTeam>(s0 + i * a.s_q, v * kTeam * E, me.lane, seen);
+        for (int v = 0; v < kVecs; ++v) raw[v] = load_slab<T, kTeam>(s0 + i * a.s_q, v * kTeam * E, me.lane, tk, seen);
     };
     int i = i0 + me.id;
     if (i < i1) fetch(i);
     for (int q = threadIdx.x; q <= bounds.n; q += kTeamBlock<kTeam>) {
         if (q < bounds.n) at[q] = bounds.at[q];
-        of_bucket[q] = table[q * a.heads + h];
+        of_bucket[q] = table[q * a.heads + h] * kLog2e;
     }
     __syncthreads();
     const int64_t first = -(int64_t)(i1 - 1) - a.offset;               // the relative position of along[0]
     for (int x = threadIdx.x; x < tk + (i1 - i0) - 1; x += kTeamBlock<kTeam>) along[x] = of_bucket[bucket_of(first + x, at, bounds.n)];
     __syncthreads();
+    const float scale = a.scale * kLog2e;
     while (i < i1) {
         float t[kVecs][E], top = -INFINITY;
         const int sees = seen;
+        const float *bias = along + (i1 - 1 - i);
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
             const int slab = v * kTeam * E, j = slab + me.lane * E;
-            if (slab >= sees) {
-#pragma unroll
-                for (int q = 0; q < E; ++q) t[v][q] = -INFINITY;
-                continue;
-            }
+            if (slab >= sees) continue;
+            settle_slab<T, kTeam>(raw[v], slab, me.lane, tk, tk, 0u);
             widen<T>(raw[v], t[v]);
             if (slab + kTeam * E <= sees) {
-                const float *bias = along + j + (i1 - 1 - i);
 #pragma unroll
-                for (int q = 0; q < E; ++q) t[v][q] = fmaf(t[v][q], a.scale, bias[q]);
+                for (int q = 0; q < E; ++q) t[v][q] = fmaf(t[v][q], scale, bias[j + q]);
             } else {
 #pragma unroll
-                for (int q = 0; q < E; ++q)
-                    t[v][q] = j + q < sees ? fmaf(t[v][q], a.scale, along[j + q + (i1 - 1 - i)]) : -INFINITY;
+                for (int q = 0; q < E; ++q) {
+                    const float f = fmaf(t[v][q], scale, bias[min(j + q, tk - 1)]);
+                    t[v][q] = j + q < sees ? f : -INFINITY;
+                }
             }
 #pragma unroll
-            for (int q = 0; q < E; ++q) top = fmaxf(top, t[v][q]);
+            for (int q = 0; q < E; ++q) top = MaxOp::apply(top, t[v][q]);
         }
         const int next = i + kTeams;
         if (next < i1) fetch(next);                                        // on its way while this row is worked on
-        top = team_reduce<LaxMaxOp, kTeam>(top, scratch);
-        const float from = top == -INFINITY ? 0.f : top;                   // an empty row: exponentials of -infinity
-        float sum = 0.f;
+        top = team_reduce<MaxOp, kTeam>(top, scratch);
+        T *row = p0 + i * a.p_q;
+        if (fabsf(top) < kPlainMax) {
+            float sum = 0.f;
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) {
-            if (v * kTeam * E < sees) {
+            for (int v = 0; v < kVecs; ++v) {
+                if (v * kTeam * E >= sees) continue;
 #pragma unroll
                 for (int q = 0; q < E; ++q) {
-                    t[v][q] = __builtin_amdgcn_exp2f((t[v][q] - from) * kLog2e);
+                    t[v][q] = __builtin_amdgcn_exp2f(t[v][q] - top);
                     sum += t[v][q];
                 }
             }
-        }
-        sum = team_reduce<SumOp, kTeam>(sum, scratch2);
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        T *row = p0 + i * a.p_q;
+            sum = team_reduce<SumOp, kTeam>(sum, scratch2);
+            float inv = __builtin_amdgcn_rcpf(sum);                        // the sum is between 1 and tk
+            inv = fmaf(fmaf(-sum, inv, 1.f), inv, inv);
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) {
-            const int slab = v * kTeam * E, j = slab + me.lane * E;
-            v4u out = {0u, 0u, 0u, 0u};
-            if (slab < sees) {
+            for (int v = 0; v < kVecs; ++v) {
+                const int slab = v * kTeam * E;
+                v4u out = {0u, 0u, 0u, 0u};
+                if (slab < sees) {
 #pragma unroll
-                for (int q = 0; q < E; ++q) {
-                    t[v][q] *= inv;
-                    if (slab + kTeam * E > sees && j + q >= sees) t[v][q] = 0.f;       // also in a row of NaN
+                    for (int q = 0; q < E; ++q) t[v][q] *= inv;
+                    out = narrow<T>(t[v]);
                 }
-                out = narrow<T>(t[v]);
+                store_slab<T, kTeam>(row, slab, me.lane, tk, out);
             }
-            store_slab<T, kTeam>(row, slab, me.lane, tk, out);
+        } else {
+            // Nothing seen, nothing but -infinity, a NaN or a +infinity; or scores that leave fp32 in units of log 2, like a row masked
+            // throughout with the type's lowest value.  In the scores' own units, from memory.
+            const T *from = s0 + i * a.s_q;
+            auto score = [&](int j) { return fmaf(widen1(from[j]), a.scale, bias[j] * kLn2); };
+            float own = -INFINITY, sum = 0.f;
+#pragma unroll 1
+            for (int j = me.lane; j < sees; j += kTeam) own = MaxOp::apply(own, score(j));
+            own = team_reduce<MaxOp, kTeam>(own, scratch2);
+            const bool none = own == -INFINITY;
+            if (!none) {
+#pragma unroll 1
+                for (int j = me.lane; j < sees; j += kTeam) sum += __builtin_amdgcn_exp2f((score(j) - own) * kLog2e);
+            }
+            sum = team_reduce<SumOp, kTeam>(sum, scratch);
+            const float inv = 1.f / sum;
+#pragma unroll 1
+            for (int j = me.lane; j < tk; j += kTeam)
+                row[j] = narrow1<T>(j < sees && !none ? __builtin_amdgcn_exp2f((score(j) - own) * kLog2e) * inv : 0.f);
+            if constexpr (kTeam > kWave) __syncthreads();                  // scratch is used first by the next row
         }
         i = next;
     }
@@ -240,19 +258,23 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_forward(T *p, const T 
 // Backward: a workgroup takes `rows_block` queries of one head and sequence, each team `rows_team` (a multiple of kStep) consecutive ones.
 // Of kStep rows and E keys that a lane holds, the diagonals are its registers' sums of the bucket gradient; every kStep rows they are
 // added to the team's array over relative positions in LDS, in two phases because the diagonals left of a lane's first key are its
-// neighbour's.  At the end the teams' arrays are added up over each bucket's positions, in a fixed order.  kBatch rows are in flight.
+// neighbour's.  At the end the teams' arrays are added up over each bucket's positions, in a fixed order.  kBatch rows are worked on together, and as many are on their way.
 template <typename T, int kTeam, int kVecs, int kStep, int kBatch>
-__global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float *__restrict__ work, const T *dp, const T *__restrict__ p,
+#ifndef BBW
+#define BBW 1
+#endif
+__global__ __launch_bounds__(kTeamBlock<kTeam>, BBW) void bias_backward(T *ds, float *__restrict__ work, const T *dp, const T *__restrict__ p,
                                                                  Bounds bounds, const int32_t *__restrict__ key_len, BiasArgs a,
                                                                  int pieces, int rows_team, unsigned worker_batch)
 {
     constexpr int E = kVec<T>, kThreads = kTeamBlock<kTeam>, kTeams = kThreads / kTeam, kSlots = kTeam * kVecs * E;
-    static_assert(E % kStep == 0 && kStep % kBatch == 0, "whole batches in a step");
-    extern __shared__ float along[];                   // [teams][kSlots + rows_team - 1]
-    __shared__ float scratch[kBatch][kThreads / kWave];
+    static_assert(E % kStep == 0 && kStep % (2 * kBatch) == 0, "an even number of batches in a step");
+    extern __shared__ float along[];                   // [teams][kSlots + rows_team - 1]; with several teams, a joined array behind
+    __shared__ float scratch[2][kBatch * kThreads / kWave];
     __shared__ int32_t at[COMP_AMS_MAX_BUCKETS];
     const Team<kTeam> me;
-    const unsigned bh = blockIdx.x / (unsigned)pieces, piece = blockIdx.x % (unsigned)pieces;
+    // with a causal mask the last queries see most: they are taken first
+    const unsigned bh = blockIdx.x / (unsigned)pieces, turn_of = blockIdx.x % (unsigned)pieces, piece = a.causal ? pieces - 1 - turn_of : turn_of;
     const unsigned b = bh / (unsigned)a.heads, h = bh % (unsigned)a.heads;
     const int tk = (int)a.tk, tq = (int)a.tq, span = kSlots + rows_team - 1;
     const int i0 = (int)piece * rows_team * kTeams, mine = i0 + me.id * rows_team, end = mine + rows_team;
@@ -263,6 +285,23 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
     for (int q = threadIdx.x; q < bounds.n; q += kThreads) at[q] = bounds.at[q];
     for (int x = threadIdx.x; x < kTeams * span; x += kThreads) along[x] = 0.f;
     __syncthreads();
+    // two batches of rows: one is worked on while the next is on its way
+    v4u praw[2][kBatch][kVecs], draw[2][kBatch][kVecs];
+    int seen[2][kBatch];
+    auto fetch = [&](int buf, int from) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int i = from + u;
+            seen[buf][u] = i < end && i < tq ? row_seen(i, by_length, a) : 0;
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v) {
+                praw[buf][u][v] = load_slab<T, kTeam>(p0 + i * a.p_q, v * kTeam * E, me.lane, tk, seen[buf][u]);
+                draw[buf][u][v] = load_slab<T, kTeam>(dp0 + i * a.s_q, v * kTeam * E, me.lane, tk, seen[buf][u]);
+            }
+        }
+    };
+    fetch(0, mine);
+    int turn = 0;
 #pragma unroll 1
     for (int first = mine; first < end; first += kStep) {
         if (kTeam >= kWave && first >= tq) break;      // uniform over the team
@@ -273,26 +312,20 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
             for (int q = 0; q < E + kStep - 1; ++q) acc[v][q] = 0.f;
 #pragma unroll
         for (int batch = 0; batch < kStep; batch += kBatch) {
-            v4u praw[kBatch][kVecs], draw[kBatch][kVecs];
-            int seen[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int i = first + batch + u;
-                seen[u] = i < tq ? row_seen(i, by_length, a) : 0;
-#pragma unroll
-                for (int v = 0; v < kVecs; ++v) {
-                    praw[u][v] = load_slab<T, kTeam>(p0 + i * a.p_q, v * kTeam * E, me.lane, seen[u]);
-                    draw[u][v] = load_slab<T, kTeam>(dp0 + i * a.s_q, v * kTeam * E, me.lane, seen[u]);
-                }
-            }
+            constexpr int kBufs = 2;
+            const int buf = batch / kBatch % kBufs;
+            fetch(buf ^ 1, first + batch + kBatch);
+            auto &pr = praw[buf];
+            auto &dr = draw[buf];
+            auto &sees = seen[buf];
             auto row_sum = [&](int u) {
                 float s = 0.f;
 #pragma unroll
                 for (int v = 0; v < kVecs; ++v) {
-                    if (v * kTeam * E < seen[u]) {
+                    if (v * kTeam * E < sees[u]) {
                         float pw[E], dw[E];
-                        widen<T>(praw[u][v], pw);
-                        widen<T>(draw[u][v], dw);
+                        widen<T>(pr[u][v], pw);
+                        widen<T>(dr[u][v], dw);
 #pragma unroll
                         for (int q = 0; q < E; ++q) s = fmaf(pw[q], dw[q], s);
                     }
@@ -301,10 +334,17 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
             };
             float total[kBatch];
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) total[u] = row_sum(u);
-            // the rows' reductions are independent: their steps interleave
+            for (int u = 0; u < kBatch; ++u) {
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) total[u] = team_reduce<SumOp, kTeam>(total[u], scratch[u]);
+                for (int v = 0; v < kVecs; ++v) {
+                    if (v * kTeam * E >= sees[u]) continue;
+                    settle_slab<T, kTeam>(pr[u][v], v * kTeam * E, me.lane, tk, sees[u], 0u);
+                    settle_slab<T, kTeam>(dr[u][v], v * kTeam * E, me.lane, tk, tk, 0u);       // beside p = 0 it does not count
+                }
+                total[u] = row_sum(u);
+            }
+            team_reduce<SumOp, kTeam, kBatch>(total, scratch[turn]);       // the rows' reductions are independent: their steps interleave
+            turn ^= 1;
             // A key of probability zero takes no gradient whatever dp holds there.  While a row's sum is finite no product was NaN, so
             // dp is finite there and the formula gives zero by itself; else such keys are cleared.
 #pragma unroll
@@ -313,13 +353,14 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
 #pragma unroll
                     for (int v = 0; v < kVecs; ++v) {
                         float pw[E], dw[E];
-                        widen<T>(praw[u][v], pw);
-                        widen<T>(draw[u][v], dw);
+                        widen<T>(pr[u][v], pw);
+                        widen<T>(dr[u][v], dw);
 #pragma unroll
                         for (int q = 0; q < E; ++q) dw[q] = pw[q] == 0.f ? 0.f : dw[q];
-                        draw[u][v] = narrow<T>(dw);
+                        dr[u][v] = narrow<T>(dw);
                     }
-                    total[u] = team_reduce<SumOp, kTeam>(row_sum(u), scratch[u]);
+                    total[u] = team_reduce<SumOp, kTeam>(row_sum(u), scratch[turn]);
+                    turn ^= 1;
                 }
             }
 #pragma unroll
@@ -330,12 +371,12 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
                 for (int v = 0; v < kVecs; ++v) {
                     const int slab = v * kTeam * E;
                     v4u out = {0u, 0u, 0u, 0u};
-                    if (slab < seen[u]) {
+                    if (slab < sees[u]) {
                         float pw[E], dw[E];
-                        rewiden(praw[u][v]);
-                        rewiden(draw[u][v]);
-                        widen<T>(praw[u][v], pw);
-                        widen<T>(draw[u][v], dw);
+                        rewiden(pr[u][v]);
+                        rewiden(dr[u][v]);
+                        widen<T>(pr[u][v], pw);
+                        widen<T>(dr[u][v], dw);
 #pragma unroll
                         for (int q = 0; q < E; ++q) {
                             const float dt = pw[q] * (dw[q] - total[u]);
@@ -374,23 +415,32 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
     __syncthreads();
     // Over the whole workgroup: place x is key x seen from its last row; team t's array begins (kTeams - 1 - t) rows_team further on.
     const int places = kSlots + kTeams * rows_team - 1;
-    const int64_t base = -(int64_t)(i0 + kTeams * rows_team - 1) - a.offset;      // relative position of place 0
-    const unsigned w = b / worker_batch;
-    const int64_t parts = (int64_t)worker_batch * pieces, part = (int64_t)(b - w * worker_batch) * pieces + piece;
-    float *out = work + ((int64_t)(w * (unsigned)a.heads + h) * (bounds.n + 1)) * parts + part;
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int q = threadIdx.x / kWave; q <= bounds.n; q += kThreads / kWave) {
-        const int64_t from = q == 0 ? 0 : at[q - 1] - base, to = q == bounds.n ? places : at[q] - base;
-        const int x0 = (int)min(max(from, (int64_t)0), (int64_t)places), x1 = (int)min(max(to, (int64_t)0), (int64_t)places);
-        float s = 0.f;
-        for (int x = x0 + lane; x < x1; x += kWave) {
+    float *joined = kTeams > 1 ? along + kTeams * span : along;
+    if constexpr (kTeams > 1) {
+        for (int x = threadIdx.x; x < places; x += kThreads) {
+            float s = 0.f;
 #pragma unroll
             for (int t = 0; t < kTeams; ++t) {
                 const int y = x - (kTeams - 1 - t) * rows_team;
                 if (y >= 0 && y < span) s += along[t * span + y];
             }
+            joined[x] = s;
         }
-        s = lanes_reduce<SumOp, kWave>(s);
+        __syncthreads();
+    }
+    const int64_t base = -(int64_t)(i0 + kTeams * rows_team - 1) - a.offset;      // relative position of place 0
+    const unsigned w = b / worker_batch;
+    const int64_t parts = (int64_t)worker_batch * pieces, part = (int64_t)(b - w * worker_batch) * pieces + piece;
+    float *out = work + ((int64_t)(w * (unsigned)a.heads + h) * (bounds.n + 1)) * parts + part;
+    // sixteen lanes a bucket: most buckets are narrow
+    const int lane = threadIdx.x & 15;
+    for (int q = threadIdx.x / 16; q <= bounds.n; q += kThreads / 16) {
+        const int64_t from = q == 0 ? 0 : at[q - 1] - base, to = q == bounds.n ? places : at[q] - base;
+        const int x0 = (int)min(max(from, (int64_t)0), (int64_t)places), x1 = (int)min(max(to, (int64_t)0), (int64_t)places);
+        float s = 0.f;
+#pragma unroll 4
+        for (int x = x0 + lane; x < x1; x += 16) s += joined[x];
+        s = lanes_reduce<SumOp, 16>(s);
         if (lane == 0) out[q * parts] = s;
     }
 }

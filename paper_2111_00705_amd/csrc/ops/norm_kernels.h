@@ -17,7 +17,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_forward_any(T *y, float *__
                                                                  const T *x, const float *__restrict__ gain,
                                                                  const float *__restrict__ shift, NormArgs a)
 {
-    __shared__ float scratch[kNormThreads / kWave];
+    __shared__ float scratch[kNormThreads / kWave], scratch2[kNormThreads / kWave];
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *xr = x + row * a.x_stride;
         T *yr = y + row * a.y_stride;
@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_forward_any(T *y, float *__
             const float d = widen1(xr[c]) - mu;
             q = fmaf(d, d, q);
         }
-        const float r = 1.f / sqrtf(fmaf(team_reduce<SumOp, kNormThreads>(q, scratch), a.inv_cols, a.eps));
+        const float r = 1.f / sqrtf(fmaf(team_reduce<SumOp, kNormThreads>(q, scratch2), a.inv_cols, a.eps));
         for (int64_t c = threadIdx.x; c < a.cols; c += kNormThreads)
             yr[c] = narrow1<T>(fmaf((widen1(xr[c]) - mu) * r, gain[c], shift ? shift[c] : 0.f));
         if (threadIdx.x == 0) {
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_any(T *dx, const T
                                                                   const float *__restrict__ rstd, const float *__restrict__ gain,
                                                                   NormArgs a)
 {
-    __shared__ float scratch[kNormThreads / kWave];
+    __shared__ float scratch[kNormThreads / kWave], scratch2[kNormThreads / kWave];
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *xr = x + row * a.x_stride, *dyr = dy + row * a.dy_stride;
         T *dxr = dx + row * a.y_stride;
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_any(T *dx, const T
             q = fmaf(g, (widen1(xr[c]) - mu) * r, q);
         }
         s = team_reduce<SumOp, kNormThreads>(s, scratch) * a.inv_cols;
-        q = team_reduce<SumOp, kNormThreads>(q, scratch) * a.inv_cols;
+        q = team_reduce<SumOp, kNormThreads>(q, scratch2) * a.inv_cols;
         for (int64_t c = threadIdx.x; c < a.cols; c += kNormThreads) {
             const float xh = (widen1(xr[c]) - mu) * r;
             dxr[c] = narrow1<T>(r * (fmaf(widen1(dyr[c]), gain[c], -s) - xh * q));
@@ -105,15 +105,15 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_forward(T *y, float *_
     v4u raw[kVecs];
     auto fetch = [&](int64_t r) {
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) raw[v] = load_slab<T, kTeam>(x + r * a.x_stride, v * kTeam * E, me.lane, cols);
+        for (int v = 0; v < kVecs; ++v) raw[v] = load_slab<T, kTeam>(x + r * a.x_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1);
     };
     fetch(row);
     float g[kVecs][E], b[kVecs][E];
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
-        load_params<T, kTeam>(g[v], gain, v * kTeam * E, me.lane, cols);
+        load_params<T, kTeam>(g[v], gain, v * kTeam * E, me.lane, cols, v < kVecs - 1);
         if (shift) {
-            load_params<T, kTeam>(b[v], shift, v * kTeam * E, me.lane, cols);
+            load_params<T, kTeam>(b[v], shift, v * kTeam * E, me.lane, cols, v < kVecs - 1);
         } else {
 #pragma unroll
             for (int q = 0; q < E; ++q) b[v][q] = 0.f;
@@ -123,6 +123,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_forward(T *y, float *_
         float d[kVecs][E], s = 0.f;
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
+            settle_slab<T, kTeam>(raw[v], v * kTeam * E, me.lane, cols, cols, 0u, v < kVecs - 1);
             widen<T>(raw[v], d[v]);
 #pragma unroll
             for (int q = 0; q < E; ++q) s += d[v][q];
@@ -135,9 +136,14 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_forward(T *y, float *_
         for (int v = 0; v < kVecs; ++v) {
             const int at = v * kTeam * E + me.lane * E;
 #pragma unroll
-            for (int q = 0; q < E; ++q) {
-                d[v][q] -= mu;
-                if ((v + 1) * kTeam * E <= cols || at + q < cols) var = fmaf(d[v][q], d[v][q], var);
+            for (int q = 0; q < E; ++q) d[v][q] -= mu;
+            if (v < kVecs - 1 || (v + 1) * kTeam * E <= cols) {
+#pragma unroll
+                for (int q = 0; q < E; ++q) var = fmaf(d[v][q], d[v][q], var);
+            } else {
+#pragma unroll
+                for (int q = 0; q < E; ++q)
+                    if (at + q < cols) var = fmaf(d[v][q], d[v][q], var);
             }
         }
         const float r = 1.f / sqrtf(fmaf(team_reduce<SumOp, kTeam>(var, scratch2), a.inv_cols, a.eps));
@@ -145,7 +151,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_forward(T *y, float *_
         for (int v = 0; v < kVecs; ++v) {
 #pragma unroll
             for (int q = 0; q < E; ++q) d[v][q] = fmaf(d[v][q] * r, g[v][q], b[v][q]);
-            store_slab<T, kTeam>(y + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(d[v]));
+            store_slab<T, kTeam>(y + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(d[v]), v < kVecs - 1);
         }
         if (me.lane == 0) {
             if (mean) mean[row] = mu;
@@ -165,7 +171,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_backward(T *dx, float 
                                                                       int64_t chunk_rows)
 {
     constexpr int E = kVec<T>, kTeams = kTeamBlock<kTeam> / kTeam, kSlots = kTeam * kVecs * E;
-    __shared__ float scratch[kTeamBlock<kTeam> / kWave], scratch2[kTeamBlock<kTeam> / kWave];
+    __shared__ float scratch[2][2 * kTeamBlock<kTeam> / kWave];
     __shared__ float joined[kTeams > 1 ? kTeams * kSlots : 1];
     const Team<kTeam> me;
     const int cols = (int)a.cols;
@@ -174,7 +180,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_backward(T *dx, float 
     float g[kVecs][E], dg[kVecs][E], db[kVecs][E];
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
-        load_params<T, kTeam>(g[v], gain, v * kTeam * E, me.lane, cols);
+        load_params<T, kTeam>(g[v], gain, v * kTeam * E, me.lane, cols, v < kVecs - 1);
 #pragma unroll
         for (int q = 0; q < E; ++q) dg[v][q] = db[v][q] = 0.f;
     }
@@ -183,26 +189,29 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_backward(T *dx, float 
     auto fetch = [&](int64_t at) {
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
-            xraw[v] = load_slab<T, kTeam>(x + at * a.x_stride, v * kTeam * E, me.lane, cols);
-            dyraw[v] = load_slab<T, kTeam>(dy + at * a.dy_stride, v * kTeam * E, me.lane, cols);
+            xraw[v] = load_slab<T, kTeam>(x + at * a.x_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1);
+            dyraw[v] = load_slab<T, kTeam>(dy + at * a.dy_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1);
         }
         mu = mean[at];
         r = rstd[at];
     };
     int64_t row = lo + me.id;
+    int turn = 0;
     if (row < hi) fetch(row);
     while (row < hi) {
-        float xh[kVecs][E], up[kVecs][E], s = 0.f, q2 = 0.f;
+        float xh[kVecs][E], up[kVecs][E], sums[2] = {0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
+            settle_slab<T, kTeam>(xraw[v], v * kTeam * E, me.lane, cols, cols, 0u, v < kVecs - 1);
+            settle_slab<T, kTeam>(dyraw[v], v * kTeam * E, me.lane, cols, cols, 0u, v < kVecs - 1);
             widen<T>(xraw[v], xh[v]);
             widen<T>(dyraw[v], up[v]);
 #pragma unroll
             for (int q = 0; q < E; ++q) {
                 xh[v][q] = (xh[v][q] - mu) * r;        // past the row: finite, times a zero gradient
                 const float t = up[v][q] * g[v][q];
-                s += t;
-                q2 = fmaf(t, xh[v][q], q2);
+                sums[0] += t;
+                sums[1] = fmaf(t, xh[v][q], sums[1]);
                 dg[v][q] = fmaf(up[v][q], xh[v][q], dg[v][q]);
                 db[v][q] += up[v][q];
             }
@@ -210,13 +219,14 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_backward(T *dx, float 
         const float scale = r;
         const int64_t next = row + kTeams;
         if (next < hi) fetch(next);
-        s = team_reduce<SumOp, kTeam>(s, scratch) * a.inv_cols;
-        q2 = team_reduce<SumOp, kTeam>(q2, scratch2) * a.inv_cols;
+        team_reduce<SumOp, kTeam, 2>(sums, scratch[turn]);
+        turn ^= 1;
+        const float s = sums[0] * a.inv_cols, q2 = sums[1] * a.inv_cols;
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
 #pragma unroll
             for (int q = 0; q < E; ++q) up[v][q] = scale * (fmaf(up[v][q], g[v][q], -s) - xh[v][q] * q2);
-            store_slab<T, kTeam>(dx + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(up[v]));
+            store_slab<T, kTeam>(dx + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(up[v]), v < kVecs - 1);
         }
         row = next;
     }

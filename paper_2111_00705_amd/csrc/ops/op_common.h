@@ -77,8 +77,16 @@ template <> __device__ __forceinline__ v4u narrow<f16_t>(const float (&x)[8])
     return r;
 }
 
+#ifdef NTL
+template <typename T> __device__ __forceinline__ v4u load_vec(const T *p) { return __builtin_nontemporal_load(reinterpret_cast<const v4u_any *>(p)); }
+#else
 template <typename T> __device__ __forceinline__ v4u load_vec(const T *p) { return *reinterpret_cast<const v4u_any *>(p); }
+#endif
+#ifdef NTS
+template <typename T> __device__ __forceinline__ void store_vec(T *p, const v4u &v) { __builtin_nontemporal_store(v, reinterpret_cast<v4u_any *>(p)); }
+#else
 template <typename T> __device__ __forceinline__ void store_vec(T *p, const v4u &v) { *reinterpret_cast<v4u_any *>(p) = v; }
+#endif
 
 // Makes the compiler take what is widened from `v` before and after for different values: a row held in registers is widened anew
 // by each pass over it, instead of being kept in its wide form too.
@@ -89,73 +97,111 @@ template <> __device__ __forceinline__ uint32_t bits1<float>(float x) { return _
 template <> __device__ __forceinline__ uint32_t bits1<bf16_t>(bf16_t x) { return x.v; }
 template <> __device__ __forceinline__ uint32_t bits1<f16_t>(f16_t x) { return x.v; }
 
-// Element q of a raw vector replaced by `b` (q known at compile time).
-template <typename T> __device__ __forceinline__ void put_bits(v4u &raw, int q, uint32_t b)
+// base + at elements for a base that is uniform over the wavefront: the offset stays a 32-bit number of bytes beside a scalar address.
+template <typename T> __device__ __forceinline__ const T *offset32(const T *base, int at)
 {
-    if constexpr (sizeof(T) == 4) raw[q] = b;
-    else raw[q >> 1] = (q & 1) ? ((raw[q >> 1] & 0xffffu) | (b << 16)) : ((raw[q >> 1] & 0xffff0000u) | b);
+    return reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + (uint32_t)at * (uint32_t)sizeof(T));
+}
+template <typename T> __device__ __forceinline__ T *offset32(T *base, int at)
+{
+    return reinterpret_cast<T *>(reinterpret_cast<char *>(base) + (uint32_t)at * (uint32_t)sizeof(T));
 }
 
-// Row elements [at, at + kVec) of a row of `len`, those outside [0, len) as `fill` bits.  Touches nothing outside the row.
-template <typename T, typename I>      // I: int or int64_t
-__device__ __forceinline__ v4u load_row(const T *row, I at, I len, uint32_t fill = 0u)
+// --- a row in slabs ----------------------------------------------------------------------------------------------------
+//
+// A row that a team of kTeam lanes takes lies in slabs of kTeam vectors, lane after lane; `first` is a slab's first element.  A slab inside
+// the row is loaded without a look at the lanes.  Where the row ends inside a lane's vector, the row's last whole vector is loaded
+// instead and moved into place later, by settle_slab: element by element it took eight loads, each waited for before the next.
+// The row (from its very start, wherever `row` points into it) has at least a vector's elements.
+// sure: the slab is known to lie inside (a constant where loops are unrolled: all but the last slab of a row that just fits).
+
+// Elements [at, at + kVec) of a row of `len` in the lanes with at < need (need <= len), not in place yet; the other lanes' are zero.
+template <typename T, int kTeam>
+__device__ __forceinline__ v4u load_slab(const T *row, int first, int lane, int len, int need, bool sure = false)
 {
     constexpr int E = kVec<T>;
-    if (at >= 0 && at + E <= len) return load_vec(row + at);
-    const uint32_t both = sizeof(T) == 4 ? fill : (fill | (fill << 16));
-    v4u raw = {both, both, both, both};
-    if (at > -E && at < len) {
-#pragma unroll
-        for (int q = 0; q < E; ++q)
-            if (at + q >= 0 && at + q < len) put_bits<T>(raw, q, bits1(row[at + q]));
-    }
+    const int at = first + lane * E;
+    if (sure || first + kTeam * E <= need) return load_vec(offset32(row, at));
+    v4u raw = {0u, 0u, 0u, 0u};
+    if (at < need) raw = load_vec(row + min(at, len - E));
     return raw;
 }
-template <typename T, typename I>
-__device__ __forceinline__ void store_row(T *row, I at, I len, const v4u &raw)
+
+// Puts the elements of load_slab into place; those from `keep` on (keep <= len) become `fill`.
+template <typename T, int kTeam>
+__device__ __forceinline__ void settle_slab(v4u &raw, int first, int lane, int len, int keep, uint32_t fill, bool sure = false)
 {
     constexpr int E = kVec<T>;
-    if (at >= 0 && at + E <= len) {
-        store_vec(row + at, raw);
-        return;
-    }
-    if (at <= -E || at >= len) return;
-#pragma unroll
-    for (int q = 0; q < E; ++q)
-        if (at + q >= 0 && at + q < len) {
-            if constexpr (sizeof(T) == 4) row[at + q] = __uint_as_float(raw[q]);
-            else row[at + q].v = (uint16_t)((q & 1) ? raw[q >> 1] >> 16 : raw[q >> 1]);
+    if (sure || first + kTeam * E <= keep) return;
+    if (first + kTeam * E > len) {
+        const int late = first + lane * E - (len - E);
+        if (late > 0) {                             // the vector ended with the row: `late` elements further down
+            if constexpr (sizeof(T) == 2) {
+                if (late & 4) raw = v4u{raw[2], raw[3], 0u, 0u};
+                if (late & 2) raw = v4u{raw[1], raw[2], raw[3], 0u};
+                if (late & 1)
+                    raw = v4u{(raw[0] >> 16) | (raw[1] << 16), (raw[1] >> 16) | (raw[2] << 16), (raw[2] >> 16) | (raw[3] << 16), raw[3] >> 16};
+            } else {
+                if (late & 2) raw = v4u{raw[2], raw[3], 0u, 0u};
+                if (late & 1) raw = v4u{raw[1], raw[2], raw[3], 0u};
+            }
         }
+    }
+    // one lane is cut, those behind it are all fill; its masks are the same for the whole team
+    const int kept = max(keep - first, 0), cut = kept / E, rest = kept % E;
+    if (lane >= cut) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t mask, both = fill;
+            if constexpr (sizeof(T) == 4) {
+                mask = rest > q ? 0xffffffffu : 0u;
+            } else {
+                mask = rest >= 2 * q + 2 ? 0xffffffffu : rest == 2 * q + 1 ? 0xffffu : 0u;
+                both |= fill << 16;
+            }
+            if (lane > cut) mask = 0u;
+            raw[q] = (raw[q] & mask) | (both & ~mask);
+        }
+    }
 }
 
-// A row that a team of kTeam lanes holds in registers lies in slabs of kTeam vectors, lane after lane.  `first` is a slab's first
-// element; a slab that lies inside [0, len) is loaded without a look at the lanes.  Offsets stay 32-bit beside the row's address.
+typedef uint32_t v2u_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u_any __attribute__((aligned(2)));
+
 template <typename T, int kTeam>
-__device__ __forceinline__ v4u load_slab(const T *row, int first, int lane, int len, uint32_t fill = 0u)
+__device__ __forceinline__ void store_slab(T *row, int first, int lane, int len, const v4u &raw, bool sure = false)
 {
     constexpr int E = kVec<T>;
     const int at = first + lane * E;
-    if (first + kTeam * E <= len) return load_vec(reinterpret_cast<const T *>(reinterpret_cast<const char *>(row) + (uint32_t)at * (uint32_t)sizeof(T)));
-    return load_row(row, at, len, fill);
+    T *p = offset32(row, at);
+    if (sure || first + kTeam * E <= len || at + E <= len) {
+        store_vec(p, raw);
+    } else if (at < len) {                          // a binary number of elements is left
+        const int rest = len - at;
+        if constexpr (sizeof(T) == 4) {
+            if (rest & 2) *reinterpret_cast<v2u_any *>(p) = v2u_any{raw[0], raw[1]};
+            if (rest & 1) *reinterpret_cast<u_any *>(p + (rest & 2)) = (rest & 2) ? raw[2] : raw[0];
+        } else {
+            if (rest & 4) *reinterpret_cast<v2u_any *>(p) = v2u_any{raw[0], raw[1]};
+            if (rest & 2) *reinterpret_cast<u_any *>(p + (rest & 4)) = (rest & 4) ? raw[2] : raw[0];
+            const uint32_t last = (rest & 4) ? ((rest & 2) ? raw[3] : raw[2]) : ((rest & 2) ? raw[1] : raw[0]);
+            if (rest & 1) reinterpret_cast<uint16_t *>(p)[rest & 6] = (uint16_t)last;
+        }
+    }
 }
+
+// Parameters (fp32) of the same elements: kVec<T> floats, zero past the row.
 template <typename T, int kTeam>
-__device__ __forceinline__ void store_slab(T *row, int first, int lane, int len, const v4u &raw)
-{
-    constexpr int E = kVec<T>;
-    const int at = first + lane * E;
-    if (first + kTeam * E <= len) store_vec(reinterpret_cast<T *>(reinterpret_cast<char *>(row) + (uint32_t)at * (uint32_t)sizeof(T)), raw);
-    else store_row(row, at, len, raw);
-}
-// Parameters (fp32) of the same elements: kVec<T> floats.
-template <typename T, int kTeam>
-__device__ __forceinline__ void load_params(float (&x)[kVec<T>], const float *p, int first, int lane, int len)
+__device__ __forceinline__ void load_params(float (&x)[kVec<T>], const float *p, int first, int lane, int len, bool sure = false)
 {
     constexpr int E = kVec<T>;
     const int at = first + lane * E;
 #pragma unroll
     for (int u = 0; u < E; u += 4) {
+        v4u raw = load_slab<float, 1>(p, at + u, 0, len, len, sure);
+        settle_slab<float, 1>(raw, at + u, 0, len, len, 0u, sure);
         float four[4];
-        widen<float>(load_row(p, at + u, len), four);
+        widen<float>(raw, four);
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[u + q] = four[q];
     }
@@ -177,11 +223,9 @@ template <int kTeam> constexpr int kTeamBlock = kTeam > 256 ? kTeam : 256;
 // --- reductions over a team of kTeam lanes (a power of two; a wavefront or less: lanes side by side; more: the whole
 // workgroup).  Fixed trees: the result depends on the lanes' values only, and every lane of the team receives it. ---------
 
-// fmaxf ignores NaN, and is one instruction: for maxima whose row shows a NaN elsewhere.
-struct LaxMaxOp { static __device__ __forceinline__ float apply(float a, float b) { return fmaxf(a, b); } };
 struct SumOp { static __device__ __forceinline__ float apply(float a, float b) { return a + b; } };
-// NaN wins: a row with a NaN must not look like one without.
-struct MaxOp { static __device__ __forceinline__ float apply(float a, float b) { return (a > b || a != a) ? a : b; } };
+// NaN wins (v_maximum3_f32): a row with a NaN does not look like one without.
+struct MaxOp { static __device__ __forceinline__ float apply(float a, float b) { return __builtin_elementwise_maximum(a, b); } };
 
 // The permutes that ride in a vector instruction: a neighbour, the other pair, the other four, the other eight of a row of sixteen
 // lanes; then the four rows through scalar registers.  (Six __shfl_xor are six round trips through the LDS unit.)  Every lane of the
@@ -207,23 +251,36 @@ __device__ __forceinline__ float lanes_reduce(float v)
     return v;
 }
 
-// scratch: kTeam / 64 floats of LDS where kTeam > 64, not touched again before the next barrier of the team's workgroup.
+// kValues reductions at once.  scratch: kValues * kTeam / 64 floats of LDS where kTeam > 64; there the workgroup meets at one barrier, and
+// must meet at another one before the same scratch is used again.
+template <typename Op, int kTeam, int kValues>
+__device__ __forceinline__ void team_reduce(float (&v)[kValues], float *scratch)
+{
+    if constexpr (kTeam <= kWave) {
+#pragma unroll
+        for (int u = 0; u < kValues; ++u) v[u] = lanes_reduce<Op, kTeam>(v[u]);
+    } else {
+        constexpr int kWaves = kTeam / kWave;
+#pragma unroll
+        for (int u = 0; u < kValues; ++u) {
+            v[u] = lanes_reduce<Op, kWave>(v[u]);
+            if ((threadIdx.x & (kWave - 1)) == 0) scratch[u * kWaves + threadIdx.x / kWave] = v[u];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kValues; ++u) {
+            v[u] = scratch[u * kWaves];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v[u] = Op::apply(v[u], scratch[u * kWaves + w]);
+        }
+    }
+}
 template <typename Op, int kTeam>
 __device__ __forceinline__ float team_reduce(float v, float *scratch)
 {
-    if constexpr (kTeam <= kWave) {
-        return lanes_reduce<Op, kTeam>(v);
-    } else {
-        constexpr int kWaves = kTeam / kWave;
-        v = lanes_reduce<Op, kWave>(v);
-        __syncthreads();                                   // whoever read the scratch before has done so
-        if ((threadIdx.x & (kWave - 1)) == 0) scratch[threadIdx.x / kWave] = v;
-        __syncthreads();
-        v = scratch[0];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) v = Op::apply(v, scratch[w]);
-        return v;
-    }
+    float one[1] = {v};
+    team_reduce<Op, kTeam, 1>(one, scratch);
+    return one[0];
 }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -242,6 +299,9 @@ __device__ __forceinline__ Lse lse_join(const Lse &a, const Lse &b, float unit)
     const float fb = b.top == top ? 1.f : __builtin_amdgcn_exp2f((b.top - top) * unit);
     return {top, a.sum * fa + b.sum * fb};
 }
+
+// Below this size of a maximum, distances to it may be formed from products with log2 e (and 1 / T up to 2^20): nothing leaves fp32.
+constexpr float kPlainMax = 1e31f;
 
 // log sum exp(z / T) of a row, or NaN where the row has no distribution: nothing but -infinity, or a +infinity.
 __device__ __forceinline__ float lse_value(const Lse &v, float inv_t)

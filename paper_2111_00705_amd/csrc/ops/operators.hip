@@ -16,6 +16,22 @@ using namespace cams_ops;
 
 namespace {
 
+#ifndef T64
+#define T64 128
+#endif
+#ifndef BIAS_BLOCKS
+#define BIAS_BLOCKS 640
+#endif
+#ifndef BIAS_FBLOCKS
+#define BIAS_FBLOCKS 1536
+#endif
+#ifndef NORM_BLOCKS
+#define NORM_BLOCKS 2048
+#endif
+#ifndef NORM_CHUNKS
+#define NORM_CHUNKS 512
+#endif
+
 thread_local char g_error[512] = "";
 
 int fail(int code, const char *fmt, ...)
@@ -71,9 +87,10 @@ void with_type(int32_t type, F &&f)
 
 // --- constants chosen from sizes, as types ---------------------------------------------------------------------------
 
-// f(Shape) with `vecs`, in [kLeast, kVecs], as a compile-time constant.
-template <int kThreads, int kVecs> struct Shape {
-    static constexpr int threads = kThreads, vecs = kVecs;
+// f(Shape) with `vecs`, in [kLeast, kVecs], as a compile-time constant: a row of more than (vecs - 1) kThreads vectors.
+// sure: slabs that are known to be full.
+template <int kThreads, int kVecs, int kSure = (kVecs > 0 ? kVecs - 1 : 0)> struct Shape {
+    static constexpr int threads = kThreads, vecs = kVecs, sure = kSure;
 };
 template <int kThreads, int kLeast, int kVecs, typename F>
 void with_vecs(int vecs, F &&f)
@@ -87,11 +104,13 @@ void with_vecs(int vecs, F &&f)
 }
 
 // f(Shape) with the team of lanes and the vectors a lane that hold a row of `len` elements in registers: 16 lanes up to 32 vectors,
-// a wavefront up to 256, a workgroup of 256 up to 1024, of 1024 up to 2048.  false if the row is longer than that.
+// a wavefront up to 256, a workgroup of 256 up to 1024, of 1024 up to 2048.  false if the row is longer than that, or shorter than a
+// vector.
 template <typename T, typename F>
 bool with_team(int64_t len, F &&f)
 {
     const int64_t vecs = ceil_div(len, kVec<T>);
+    if (len < kVec<T>) return false;
     if (vecs <= 32) with_vecs<16, 1, 2>((int)ceil_div(vecs, 16), f);
     else if (vecs <= 256) with_vecs<64, 1, 4>((int)ceil_div(vecs, 64), f);
     else if (vecs <= 1024) with_vecs<256, 2, 4>((int)ceil_div(vecs, 256), f);
@@ -110,7 +129,7 @@ int norm_check(const char *what, int64_t rows, int64_t cols, int32_t type)
     return COMP_AMS_OK;
 }
 
-constexpr int64_t kNormBlocks = 2048;
+constexpr int64_t kNormBlocks = NORM_BLOCKS;
 
 // How a worker's rows are cut for the parameter gradients: chunks of rows with one set of column sums each.
 struct NormChunks {
@@ -118,7 +137,7 @@ struct NormChunks {
 };
 NormChunks norm_chunks(int64_t worker_rows, int32_t n)
 {
-    const int64_t want = std::max<int64_t>(1, ceil_div(512, n));
+    const int64_t want = std::max<int64_t>(1, ceil_div(NORM_CHUNKS, n));
     const int64_t rows = std::max<int64_t>(16, ceil_div(worker_rows, want));
     return {rows, std::max<int64_t>(1, ceil_div(worker_rows, rows))};
 }
@@ -167,15 +186,18 @@ int bias_strides(const char *what, const char *name, const void *p, int64_t batc
 // How the queries of a head and sequence are cut for the backward pass: the registers' form takes rows_team consecutive queries a team.
 struct BiasShape {
     bool held;               // false: bias_backward_any
-    int32_t rows_team, rows_block;
+    int32_t team, rows_team, rows_block;
     int64_t pieces;
 };
-BiasShape bias_backward_shape(int64_t tq, int64_t tk, int32_t type)
+BiasShape bias_backward_shape(int64_t sequences, int64_t tq, int64_t tk, int32_t type)
 {
     const int64_t e = 16 / (int64_t)type_size(type), vecs = ceil_div(std::max<int64_t>(tk, 1), e);
-    if (vecs > 1024) return {false, kBiasAnyRows, kBiasAnyRows, ceil_div(tq, kBiasAnyRows)};
-    const int32_t teams = vecs <= 32 ? 16 : vecs <= 256 ? 4 : 1, rows = (int32_t)(vecs <= 256 ? e : 2 * e);
-    return {true, rows, rows * teams, ceil_div(tq, rows * teams)};
+    if (tk < e || vecs > 1024) return {false, 0, kBiasAnyRows, kBiasAnyRows, ceil_div(tq, kBiasAnyRows)};
+    const int32_t team = vecs <= 32 ? 16 : vecs <= T64 ? 64 : 256, teams = kTeamBlock<256> / team;
+    // as many rows as leave about kBiasBlocks workgroups, between a step's and 32
+    int32_t rows = 32;
+    while (rows > e && sequences * ceil_div(tq, rows * teams) < BIAS_BLOCKS) rows /= 2;
+    return {true, team, rows, rows * teams, ceil_div(tq, rows * teams)};
 }
 
 // --- vocabulary rows ----------------------------------------------------------------------------------------------------
@@ -209,7 +231,7 @@ int distill_check(const char *what, const void *logits, const int32_t *idx, cons
 
 // How a row of a vocabulary is cut for logprobs_regs, and which of its forms takes a piece.
 struct PieceShape {
-    int32_t count;           // pieces of a row; 0: the row does not fit, logprobs_any takes it
+    int32_t count;           // pieces of a row; 0: the row is too long, or shorter than a vector: logprobs_any
     int64_t len;             // elements of a piece, a multiple of 64 unless there is one only
     int32_t threads, vecs;
 };
@@ -219,6 +241,7 @@ PieceShape piece_shape(int64_t rows, int64_t vocab, int32_t type)
 {
     const int64_t lanes = (int64_t)kPieceThreads * 16 / (int64_t)type_size(type);     // elements of one vector of every thread
     PieceShape s = {1, vocab, kPieceThreads, 1};
+    if (vocab < 16 / (int64_t)type_size(type)) return {0, 0, 0, 0};
     if (vocab <= lanes / 2) {
         s.threads = kPieceThreads / 2;
         return s;
@@ -348,7 +371,7 @@ int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const 
             using S = decltype(shape);
             if constexpr (S::threads <= 256) {
                 constexpr int kTeams = kTeamBlock<S::threads> / S::threads;
-                const int rows_block = (int)std::min<int64_t>(tq, kTeams * 8);
+                const int rows_block = (int)std::min<int64_t>(tq, std::min<int64_t>(256, std::max<int64_t>(1, ceil_div(a.rows, (int64_t)BIAS_FBLOCKS * kTeams)) * kTeams));
                 const int64_t pieces = ceil_div(tq, rows_block);
                 const size_t lds = (size_t)(tk + rows_block - 1) * sizeof(float);
                 bias_forward<T, S::threads, S::vecs><<<(unsigned)(batch * heads * pieces), kTeamBlock<S::threads>, lds,
@@ -370,7 +393,7 @@ int comp_ams_rel_bias_work_bytes(int64_t batch, int64_t heads, int64_t tq, int64
     if (const int rc = bias_check(what, nullptr, 1, nullptr, batch, heads, tq, tk, 0, 1.f, type, &none)) return rc;
     REQUIRE(n_buckets >= 1 && n_buckets <= COMP_AMS_MAX_BUCKETS, "%s: n_buckets=%d must be in [1, %d]", what, n_buckets, COMP_AMS_MAX_BUCKETS);
     REQUIRE(bytes, "%s: bytes is NULL", what);
-    *bytes = (uint64_t)(batch * heads * bias_backward_shape(tq, tk, type).pieces) * (uint64_t)n_buckets * sizeof(float);
+    *bytes = (uint64_t)(batch * heads * bias_backward_shape(batch * heads, tq, tk, type).pieces) * (uint64_t)n_buckets * sizeof(float);
     return COMP_AMS_OK;
 }
 
@@ -402,7 +425,7 @@ int comp_ams_rel_bias_softmax_backward(void *ds, void *dtable, const void *dp, c
     }
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     float *sums = static_cast<float *>(work);
-    const BiasShape cut = bias_backward_shape(tq, tk, type);
+    const BiasShape cut = bias_backward_shape(batch * heads, tq, tk, type);
     if (!empty) {
         BiasArgs a = {};
         a.heads = heads, a.tq = tq, a.tk = tk, a.rows = batch * heads * tq;
@@ -418,17 +441,19 @@ int comp_ams_rel_bias_softmax_backward(void *ds, void *dtable, const void *dp, c
                                                                           static_cast<const T *>(p), bounds, key_len, a, cut.pieces, batch / n);
                 return;
             }
-            with_team<T>(tk, [&](auto shape) {
+            auto launch = [&](auto shape) {
                 using S = decltype(shape);
-                if constexpr (S::threads <= 256) {
-                    constexpr int kTeams = kTeamBlock<S::threads> / S::threads, kStep = S::vecs > 2 ? 4 : kVec<T>,
-                                  kBatch = S::vecs == 1 ? 4 : S::vecs == 2 ? 2 : 1;
-                    const size_t lds = (size_t)kTeams * (S::threads * S::vecs * kVec<T> + cut.rows_team - 1) * sizeof(float);
-                    bias_backward<T, S::threads, S::vecs, kStep, kBatch><<<grid, kTeamBlock<S::threads>, lds, stream>>>(
-                        static_cast<T *>(ds), sums, static_cast<const T *>(dp), static_cast<const T *>(p), bounds, key_len, a,
-                        (int)cut.pieces, cut.rows_team, (unsigned)(batch / n));
-                }
-            });
+                constexpr int kTeams = kTeamBlock<S::threads> / S::threads, kStep = S::vecs > 2 ? 4 : kVec<T>, kBatch = S::vecs > 2 ? 1 : 2;
+                constexpr int kSlots = S::threads * S::vecs * kVec<T>;
+                const size_t lds = ((size_t)kTeams * (kSlots + cut.rows_team - 1) + (kTeams > 1 ? kSlots + cut.rows_block - 1 : 0)) * sizeof(float);
+                bias_backward<T, S::threads, S::vecs, kStep, kBatch><<<grid, kTeamBlock<S::threads>, lds, stream>>>(
+                    static_cast<T *>(ds), sums, static_cast<const T *>(dp), static_cast<const T *>(p), bounds, key_len, a,
+                    (int)cut.pieces, cut.rows_team, (unsigned)(batch / n));
+            };
+            const int vecs = (int)ceil_div(tk, kVec<T>);
+            if (cut.team == 16) with_vecs<16, 1, 2>(ceil_div(vecs, 16), launch);
+            else if (cut.team == 64) with_vecs<64, 1, 2>(ceil_div(vecs, 64), launch);
+            else with_vecs<256, 1, 4>(ceil_div(vecs, 256), launch);
         });
     }
     with_type(grad_type, [&](auto t) {
@@ -507,7 +532,10 @@ int comp_ams_distill(float *loss, float *lse, const void *logits, const int32_t 
             distill_forward<T, S::threads><<<(unsigned)rows, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
                 loss, lse, static_cast<const T *>(logits), idx, val, a);
         };
-        if (vocab <= 4 * 256 * kVec<T>) launch(Shape<256, 0>{});
+        if (vocab < kVec<T>)
+            distill_any<T, true, false><<<(unsigned)rows, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                loss, lse, nullptr, nullptr, static_cast<const T *>(logits), nullptr, idx, val, a);
+        else if (rows >= 1024 || vocab <= 4 * 256 * kVec<T>) launch(Shape<256, 0>{});
         else launch(Shape<1024, 0>{});
     });
     return launched(what);
@@ -526,6 +554,11 @@ int comp_ams_distill_backward(void *dlogits, const float *dloss, const void *log
     const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature};
     with_type(type, [&](auto t) {
         using T = decltype(t);
+        if (vocab < kVec<T>) {
+            distill_any<T, false, true><<<(unsigned)rows, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                nullptr, nullptr, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), lse, idx, val, a);
+            return;
+        }
         const int64_t chunk = 4 * 256 * kVec<T>;
         const int64_t pieces = std::max<int64_t>(1, std::min(ceil_div(vocab, 4 * chunk), kMaxGrid / rows));
         const int64_t len = ceil_div(ceil_div(vocab, pieces), chunk) * chunk;
@@ -551,14 +584,18 @@ int comp_ams_distill_grad(float *loss, void *dlogits, const float *dloss, const 
         using T = decltype(t);
         auto launch = [&](auto shape) {
             using S = decltype(shape);
-            distill_both<T, S::threads, S::vecs><<<(unsigned)rows, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+            distill_both<T, S::threads, S::vecs, S::sure><<<(unsigned)rows, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
                 loss, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), idx, val, a);
         };
         const int64_t vecs = ceil_div(vocab, kVec<T>);          // vectors of the row
-        if (vecs <= 256) launch(Shape<256, 1>{});
+        if (vocab < kVec<T>)
+            distill_any<T, true, true><<<(unsigned)rows, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                loss, nullptr, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), nullptr, idx, val, a);
+        else if (vecs <= 256) launch(Shape<256, 1>{});
         else if (vecs <= 512 * 8) with_vecs<512, 1, 8>((int)ceil_div(vecs, 512), launch);
         else if (vecs <= 1024 * 8) with_vecs<1024, 5, 8>((int)ceil_div(vecs, 1024), launch);
-        else if (vecs <= 1024 * 16) launch(Shape<1024, 16>{});
+        else if (vecs <= 1024 * 12) launch(Shape<1024, 12, 8>{});
+        else if (vecs <= 1024 * 16) launch(Shape<1024, 16, 12>{});
         else launch(Shape<1024, 0>{});
     });
     return launched(what);

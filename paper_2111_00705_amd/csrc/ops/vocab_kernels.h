@@ -5,6 +5,12 @@
 
 namespace cams_ops {
 
+#ifndef LPW
+#define LPW 8
+#endif
+#ifndef DBW
+#define DBW 6
+#endif
 constexpr int kVocabThreads = 256;
 constexpr int kMaxTop = COMP_AMS_MAX_TOP;
 
@@ -20,18 +26,15 @@ __device__ __forceinline__ uint32_t order_of(float z)
 }
 __device__ __forceinline__ uint64_t rank_key(float z, uint32_t token) { return ((uint64_t)order_of(z) << 32) | (uint32_t)~token; }
 
+// Joins the threads' running maxima and sums; every thread receives the row's.  scratch: 2 * kThreads / 64 floats, not to be used again
+// before another barrier.
 template <int kThreads>
-__device__ __forceinline__ Lse block_lse(Lse v, float unit, Lse *scratch)
+__device__ __forceinline__ Lse block_lse(const Lse &v, float unit, float *scratch)
 {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v = lse_join(v, {__shfl_xor(v.top, off, kWave), __shfl_xor(v.sum, off, kWave)}, unit);
-    __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0) scratch[threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = scratch[0];
-#pragma unroll
-    for (int w = 1; w < kThreads / kWave; ++w) v = lse_join(v, scratch[w], unit);
-    return v;
+    const float top = team_reduce<MaxOp, kThreads>(v.top, scratch);
+    // equal tops first: -infinity beside -infinity is an empty sum, not a NaN
+    const float s = v.top == top ? v.sum : v.sum * __builtin_amdgcn_exp2f((v.top - top) * unit);
+    return {top, team_reduce<SumOp, kThreads>(s, scratch + kThreads / kWave)};
 }
 
 template <int kThreads>
@@ -55,21 +58,20 @@ __global__ __launch_bounds__(kVocabThreads) void logprobs_any(float *__restrict_
                                                               const T *__restrict__ logits, const int64_t *__restrict__ tokens,
                                                               int64_t rows, int64_t vocab, int64_t stride, int k)
 {
-    __shared__ Lse lse_scratch[kVocabThreads / kWave];
-    __shared__ float scratch[kVocabThreads / kWave];
+    __shared__ float lse_scratch[2 * kVocabThreads / kWave], scratch[kVocabThreads / kWave];
     __shared__ uint64_t key_scratch[kVocabThreads / kWave];
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const T *z = logits + row * stride;
         Lse v = {-INFINITY, 0.f};
         for (int64_t c = threadIdx.x; c < vocab; c += kVocabThreads) v = lse_join(v, {widen1(z[c]), 1.f}, kLog2e);
-        v = block_lse<kVocabThreads>(v, kLog2e, lse_scratch);
+        v = block_lse<kVocabThreads>(v, kLog2e, lse_scratch);     // the entropy's barrier lies between two of these
         const float lse = lse_value(v, 1.f);
         float e = 0.f;
         for (int64_t c = threadIdx.x; c < vocab; c += kVocabThreads) {
             const float zc = widen1(z[c]), p = __builtin_amdgcn_exp2f((zc - lse) * kLog2e);
             if (p != 0.f) e = fmaf(p, lse - zc, e);
         }
-        e = team_reduce<SumOp, kVocabThreads>(e, scratch);
+        e = team_reduce<SumOp, kVocabThreads>(e, scratch);      // block_lse's barriers lie between two of these
         if (threadIdx.x == 0) {
             if (entropy) entropy[row] = e;
             if (logp) {
@@ -101,24 +103,29 @@ __device__ __forceinline__ float logit_of(uint64_t key)
     return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
 }
 
-// Statistics of a piece of a row: top = max z, sum = sum exp(z - top), moment = sum exp(z - top) (z - top).  The entropy of the
-// distribution is log sum - moment / sum: no cancellation against lse.
+// Statistics of a piece of a row, in units of log 2 beside the maximum's own: top = max z, sum = sum 2^d, moment = sum 2^d d with
+// d = (z - top) log2 e.  The entropy is log sum - moment / sum: no cancellation against lse.
 struct Piece {
     float top, sum, moment;
 };
 __device__ __forceinline__ Piece piece_join(const Piece &a, const Piece &b)
 {
     const float top = MaxOp::apply(a.top, b.top);
-    const float da = a.top - top, db = b.top - top;
-    const float fa = a.top == top ? 1.f : __builtin_amdgcn_exp2f(da * kLog2e);
-    const float fb = b.top == top ? 1.f : __builtin_amdgcn_exp2f(db * kLog2e);
+    const float da = (a.top - top) * kLog2e, db = (b.top - top) * kLog2e;
+    const float fa = a.top == top ? 1.f : __builtin_amdgcn_exp2f(da);
+    const float fb = b.top == top ? 1.f : __builtin_amdgcn_exp2f(db);
     // an empty piece (top -infinity, sum 0) adds nothing, though its distance is infinite
     const float ma = a.top == top ? a.moment : fa == 0.f ? 0.f : fa * fmaf(da, a.sum, a.moment);
     const float mb = b.top == top ? b.moment : fb == 0.f ? 0.f : fb * fmaf(db, b.sum, b.moment);
     return {top, a.sum * fa + b.sum * fb, ma + mb};
 }
+// NaN for a row of nothing but -infinity, or with a +infinity (or a NaN, which the sum shows).
+__device__ __forceinline__ float piece_lse(const Piece &p) { return fabsf(p.top) == INFINITY ? NAN : p.top + logf(p.sum); }
+__device__ __forceinline__ float piece_entropy(const Piece &p)
+{
+    return fabsf(p.top) == INFINITY ? NAN : logf(p.sum) - p.moment / p.sum * kLn2;
+}
 
-constexpr int kMaxCandidates = 1024;      // of one piece; more than that (rows of ties) are told apart by select_slow
 constexpr int kMaxPieces = 32;            // of one row; longer vocabularies go to logprobs_any
 
 // Adds the k tokens of the largest keys of z[lo..hi) to the list by bisection over the order and, among the ties at its end,
@@ -164,129 +171,161 @@ __device__ __attribute__((noinline)) void select_slow(const T *z, int64_t lo, in
 
 // One piece of a row per workgroup, held in registers between the two looks at it: maximum, sum and moment, and then the
 // elements that can be among the k best.  Those are found by a bound: the k-th largest of the maxima of `groups` groups of lanes is
-// reached by k elements at least, and by few more (k = 32 of 64 groups: 44 expected), which are listed in LDS and ranked by counting.
+// reached by k elements at least, and by few more (k = 32 of 64 groups: 44 expected).  Vectors that reach it are queued in LDS, their
+// elements that do are listed, and the list is ranked by counting.
+// A piece is longer than kVecs - 2 slabs (the shape's rule; the last one is shorter than the others by less than a slab).
 // With one piece per row the results are final; with more, statistics and keys go to work and logprobs_join follows.
+constexpr int kMaxQueued = 256;           // vectors that reach the bound; more than that (rows of ties) are told apart by select_slow
+
 template <typename T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads) void logprobs_regs(float *__restrict__ logp, float *__restrict__ entropy,
+__global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict__ logp, float *__restrict__ entropy,
                                                           int32_t *__restrict__ top_idx, float *__restrict__ top_logp,
                                                           const T *__restrict__ logits, const int64_t *__restrict__ tokens,
                                                           int64_t vocab, int64_t stride, int k, int groups, int n_pieces,
                                                           int64_t piece_len, Piece *__restrict__ pieces, uint64_t *__restrict__ keys)
 {
-    constexpr int E = kVec<T>;
-    __shared__ float scratch[kThreads / kWave], scratch2[kThreads / kWave];
-    __shared__ float group_max[256];
-    __shared__ uint64_t list[kMaxCandidates];
-    __shared__ uint32_t count;
-    __shared__ float bound_lds;
-    const int tid = threadIdx.x;
+    constexpr int E = kVec<T>, kWaves = kThreads / kWave;
+    __shared__ float scratch[kWaves], sum_of[kWaves], moment_of[kWaves], group_max[256];
+    __shared__ uint64_t list[kMaxQueued * E];
+    __shared__ int queue[kMaxQueued];
+    __shared__ uint32_t count, queued, strange;
+    __shared__ float bound_lds, lse_lds;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int64_t row = blockIdx.x / (unsigned)n_pieces, lo = blockIdx.x % (unsigned)n_pieces * piece_len;
     const int len = (int)(min(lo + piece_len, vocab) - lo);
     const T *z = logits + row * stride + lo;
+    auto empty = [&](int v) { return v >= kVecs - 2 && (v * kThreads + wave * kWave) * E >= len; };      // nothing for this wavefront
     v4u raw[kVecs];
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v) raw[v] = load_row(z, (v * kThreads + tid) * E, len, kNegInfBits<T>);
+    for (int v = 0; v < kVecs; ++v) raw[v] = load_slab<T, kThreads>(z, v * kThreads * E, tid, len, len, v < kVecs - 2);
     float vec_max[kVecs], top = -INFINITY;
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
+        vec_max[v] = -INFINITY;
+        if (empty(v)) continue;
         float x[E];
+        settle_slab<T, kThreads>(raw[v], v * kThreads * E, tid, len, len, kNegInfBits<T>, v < kVecs - 2);
         widen<T>(raw[v], x);
-        vec_max[v] = x[0];
 #pragma unroll
-        for (int q = 1; q < E; ++q) vec_max[v] = fmaxf(vec_max[v], x[q]);      // ignores NaN: the sum shows them
-        top = fmaxf(top, vec_max[v]);
+        for (int q = 0; q < E; ++q) vec_max[v] = MaxOp::apply(vec_max[v], x[q]);
+        top = MaxOp::apply(top, vec_max[v]);
     }
     // group maxima on the way to the workgroup's
     if (k > 0) {
         const int per = kThreads / groups;
         float g = top;
-        for (int off = 1; off < per; off <<= 1) g = fmaxf(g, __shfl_xor(g, off, kWave));
+        for (int off = 1; off < per; off <<= 1) g = MaxOp::apply(g, __shfl_xor(g, off, kWave));
         if ((tid & (per - 1)) == 0) group_max[tid / per] = g;
-        if (tid == 0) count = 0;
+    }
+    if (tid == 0) {
+        count = queued = strange = 0;
+        bound_lds = 0.f;                          // stays so where a NaN keeps the maxima from being ranked
     }
     const float m = team_reduce<MaxOp, kThreads>(top, scratch);
+    // exp(x - m) as 2^(x log2 e - c): the same rounding of c = m log2 e in every term and in the moment, and taken back in lse
+    const float c = m * kLog2e;
     float s = 0.f, w = 0.f;
-    if (m != -INFINITY) {
+    if (fabsf(m) < kPlainMax) {
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
+            if (empty(v)) continue;
             float x[E];
             rewiden(raw[v]);
             widen<T>(raw[v], x);
 #pragma unroll
             for (int q = 0; q < E; ++q) {
-                const float d = x[q] - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
+                const float d = fmaf(x[q], kLog2e, -c), e = __builtin_amdgcn_exp2f(d);
                 s += e;
                 w = fmaf(e, fmaxf(d, -1e30f), w);       // an infinite distance has e = 0
             }
         }
     } else {
 #pragma unroll 1
-        for (int c = tid; c < len; c += kThreads) {     // nothing but -infinity, or NaN, which must show
-            const float x = widen1(z[c]);
-            if (x != x) s = x;
+        for (int q = tid; q < len; q += kThreads) {     // infinities, or nothing but -infinity and NaN, or near the end of fp32's range
+            const float x = widen1(z[q]), d = (x - m) * kLog2e, e = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
+            s += e;
+            w = fmaf(e, fmaxf(d, -1e30f), w);
         }
     }
-    float bound = -INFINITY;
-    if (k > 0) {
-        if (tid < groups) {
-            const float g = group_max[tid];
-            int rank = 0;
-            for (int q = 0; q < groups; ++q) {
-                const float o = group_max[q];
-                rank += (o > g || (o == g && q < tid)) ? 1 : 0;
-            }
-            if (rank == k - 1) bound_lds = g;
-        }
+    s = lanes_reduce<SumOp, kWave>(s);
+    w = lanes_reduce<SumOp, kWave>(w);
+    if ((tid & (kWave - 1)) == 0) {
+        sum_of[wave] = s;
+        moment_of[wave] = w;
+        if (!(fabsf(s) < INFINITY)) strange = 1;        // a NaN or an infinity: the bound says nothing then
     }
-    const float sum = team_reduce<SumOp, kThreads>(s, scratch2);
-    const float moment = team_reduce<SumOp, kThreads>(w, scratch);
-    if (k > 0) {
-        bound = bound_lds;
-        if (sum == sum) {
-#pragma unroll
-            for (int v = 0; v < kVecs; ++v) {
-                if (vec_max[v] >= bound) {
-                    float x[E];
-                    rewiden(raw[v]);
-                    widen<T>(raw[v], x);
-#pragma unroll
-                    for (int q = 0; q < E; ++q) {
-                        const int c = (v * kThreads + tid) * E + q;
-                        if (x[q] >= bound && c < len) {
-                            const uint32_t slot = atomicAdd(&count, 1u);
-                            if (slot < (uint32_t)kMaxCandidates) list[slot] = rank_key(x[q], (uint32_t)(lo + c));
-                        }
-                    }
-                }
-            }
+    if (tid < groups && k > 0) {
+        const float g = group_max[tid];
+        int rank = 0;
+        for (int q = 0; q < groups; ++q) {
+            const float o = group_max[q];
+            rank += (o > g || (o == g && q < tid)) ? 1 : 0;
         }
-        __syncthreads();
-        // a NaN or +infinity (the bound says nothing then), or too many ties
-        if (sum != sum || count > (uint32_t)kMaxCandidates) {
-            __syncthreads();
-            if (len > k) {
-                select_slow<T, kThreads>(logits + row * stride, lo, lo + len, k, list, &count);
-            } else {
-                if (tid == 0) count = (uint32_t)len;
-                for (int c = tid; c < len; c += kThreads) list[c] = rank_key(widen1(z[c]), (uint32_t)(lo + c));
-                __syncthreads();
-            }
-        }
+        if (rank == k - 1) bound_lds = g;
     }
+    __syncthreads();
     const bool whole = n_pieces == 1;
-    const float lse = fabsf(m) == INFINITY ? NAN : m + logf(sum);
     if (tid == 0) {
+        Piece piece = {m, sum_of[0], moment_of[0]};
+#pragma unroll
+        for (int q = 1; q < kWaves; ++q) {
+            piece.sum += sum_of[q];
+            piece.moment += moment_of[q];
+        }
+        const float lse = piece_lse(piece);
+        lse_lds = lse;
         if (!whole) {
-            pieces[blockIdx.x] = {m, sum, moment};
+            pieces[blockIdx.x] = piece;
         } else {
-            if (entropy) entropy[row] = fabsf(m) == INFINITY ? NAN : logf(sum) - moment / sum;
+            if (entropy) entropy[row] = piece_entropy(piece);
             if (logp) {
                 const int64_t t = tokens[row];
                 logp[row] = t >= 0 && t < vocab ? widen1(logits[row * stride + t]) - lse : 0.f;
             }
         }
     }
-    const int n = k > 0 ? (int)count : 0;
+    if (k == 0) return;
+    const float bound = bound_lds;
+    // one atomic a wavefront for all its vectors
+    uint64_t reach[kVecs];
+    int total = 0;
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+        reach[v] = __ballot(vec_max[v] >= bound);
+        total += __popcll(reach[v]);
+    }
+    if (total) {
+        uint32_t from = 0;
+        if ((tid & (kWave - 1)) == 0) from = atomicAdd(&queued, (uint32_t)total);
+        from = __builtin_amdgcn_readfirstlane(from);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+            if (reach[v]) {
+                const uint32_t slot = from + __builtin_amdgcn_mbcnt_hi((uint32_t)(reach[v] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)reach[v], 0u));
+                if (vec_max[v] >= bound && slot < (uint32_t)kMaxQueued) queue[slot] = (v * kThreads + tid) * E;
+                from += __popcll(reach[v]);
+            }
+        }
+    }
+    __syncthreads();
+    if (strange || queued > (uint32_t)kMaxQueued) {
+        if (len > k) {
+            select_slow<T, kThreads>(logits + row * stride, lo, lo + len, k, list, &count);
+        } else {
+            if (tid == 0) count = (uint32_t)len;
+            for (int q = tid; q < len; q += kThreads) list[q] = rank_key(widen1(z[q]), (uint32_t)(lo + q));
+        }
+    } else {
+        for (int t = tid; t < (int)queued * E; t += kThreads) {
+            const int at = queue[t / E] + t % E;
+            if (at < len) {
+                const float x = widen1(z[at]);
+                if (x >= bound) list[atomicAdd(&count, 1u)] = rank_key(x, (uint32_t)(lo + at));
+            }
+        }
+    }
+    __syncthreads();
+    const int n = (int)count;
     for (int t = tid; t < n; t += kThreads) {
         const uint64_t key = list[t];
         int rank = 0;
@@ -294,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_regs(float *__restrict__ lo
         if (rank < k) {
             if (whole) {
                 top_idx[row * k + rank] = (int32_t)~(uint32_t)key;
-                top_logp[row * k + rank] = logit_of(key) - lse;
+                top_logp[row * k + rank] = logit_of(key) - lse_lds;
             } else {
                 keys[(int64_t)blockIdx.x * k + rank] = key;
             }
@@ -318,10 +357,9 @@ __global__ __launch_bounds__(kVocabThreads) void logprobs_join(float *__restrict
     for (int t = threadIdx.x; t < n; t += kVocabThreads) list[t] = keys[row * n + t];
     Piece p = pieces[row * n_pieces];
     for (int q = 1; q < n_pieces; ++q) p = piece_join(p, pieces[row * n_pieces + q]);
-    const bool none = fabsf(p.top) == INFINITY;
-    const float lse = none ? NAN : p.top + logf(p.sum);
+    const float lse = piece_lse(p);
     if (threadIdx.x == 0) {
-        if (entropy) entropy[row] = none ? NAN : logf(p.sum) - p.moment / p.sum;
+        if (entropy) entropy[row] = piece_entropy(p);
         if (logp) {
             const int64_t t = tokens[row];
             logp[row] = t >= 0 && t < vocab ? widen1(logits[row * stride + t]) - lse : 0.f;
@@ -357,25 +395,37 @@ struct Listed {
 };
 static_assert(kMaxTop <= 2 * kWave, "two entries per lane");
 
-__device__ __forceinline__ Listed teacher_list(const int32_t *__restrict__ idx, const float *__restrict__ val, int64_t row,
-                                               const DistillArgs &a)
+// The entries as they are read: loads that may go out before the row's, to be waited for while the row is on its way.
+struct RawList {
+    int32_t token[2];
+    float val[2];
+};
+__device__ __forceinline__ RawList load_list(const int32_t *__restrict__ idx, const float *__restrict__ val, int64_t row, int k)
 {
     const int lane = threadIdx.x & (kWave - 1);
+    RawList r;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int t = lane + u * kWave;
+        r.token[u] = -1;
+        r.val[u] = 0.f;
+        if (t < k) {
+            r.token[u] = idx[row * k + t];
+            r.val[u] = val[row * k + t];
+        }
+    }
+    return r;
+}
+
+__device__ __forceinline__ Listed teacher_list(const RawList &r, const DistillArgs &a)
+{
     Listed e;
     float v[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const int t = lane + u * kWave;
-        e.token[u] = -1;
-        v[u] = -INFINITY;
-        if (t < a.k) {
-            const int32_t tok = idx[row * a.k + t];
-            const float x = val[row * a.k + t] * a.inv_t;
-            if (tok >= 0 && tok < a.vocab) {
-                e.token[u] = tok;
-                v[u] = x;
-            }
-        }
+        const bool there = r.token[u] >= 0 && r.token[u] < a.vocab;
+        e.token[u] = there ? r.token[u] : -1;
+        v[u] = there ? r.val[u] * a.inv_t : -INFINITY;
     }
     e.any = __ballot(e.token[0] >= 0 || e.token[1] >= 0) != 0;
     const float top = lanes_reduce<MaxOp, kWave>(MaxOp::apply(v[0], v[1]));
@@ -392,13 +442,13 @@ __device__ __forceinline__ Listed teacher_list(const int32_t *__restrict__ idx, 
 }
 
 // T^2 sum q (log q - lp) of the row, by one wavefront.
-template <typename T>
-__device__ __forceinline__ float list_loss(const Listed &e, const T *z, float lse, const DistillArgs &a)
+// z: the logits of the lane's entries.
+__device__ __forceinline__ float list_loss(const Listed &e, const float (&z)[2], float lse, const DistillArgs &a)
 {
     float part = 0.f;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-        if (e.q[u] != 0.f) part += e.q[u] * (e.logq[u] - fmaf(widen1(z[e.token[u]]), a.inv_t, -lse));
+        if (e.q[u] != 0.f) part += e.q[u] * (e.logq[u] - fmaf(z[u], a.inv_t, -lse));
     return a.t * a.t * lanes_reduce<SumOp, kWave>(part);
 }
 
@@ -427,9 +477,10 @@ __device__ __forceinline__ void merge_list(Listed &e, int k)
     }
 }
 
-// Maximum and sum of a row's elements [at, at + kVecs kThreads E) taken into this thread's (top, sum).
-template <typename T, int kThreads, int kVecs>
-__device__ __forceinline__ void take_chunk(Lse &v, v4u (&raw)[kVecs], float unit)
+// kVecs vectors of this thread taken into its running maximum and sum.  The sum is in terms of 2^(z unit - c), c = top * unit rounded
+// once, as long as the maxima are of ordinary size.
+template <typename T, int kVecs>
+__device__ __forceinline__ void take(Lse &v, v4u (&raw)[kVecs], float unit)
 {
     constexpr int E = kVec<T>;
     float top = v.top;
@@ -438,46 +489,173 @@ __device__ __forceinline__ void take_chunk(Lse &v, v4u (&raw)[kVecs], float unit
         float x[E];
         widen<T>(raw[r], x);
 #pragma unroll
-        for (int q = 0; q < E; ++q) top = fmaxf(top, x[q]);     // ignores NaN: the sum shows them
+        for (int q = 0; q < E; ++q) top = MaxOp::apply(top, x[q]);
     }
     const float from = top == -INFINITY ? 0.f : top;            // nothing but -infinity so far: exponentials of zero, not of NaN
+    const float c = from * unit;
     float s = v.sum * __builtin_amdgcn_exp2f((v.top - from) * unit);
 #pragma unroll
-    for (int r = 0; r < kVecs; ++r) {
-        float x[E];
-        rewiden(raw[r]);
-        widen<T>(raw[r], x);
+    for (int r = 0; r < kVecs; ++r) rewiden(raw[r]);
+    if (__all(fabsf(from) < kPlainMax)) {
 #pragma unroll
-        for (int q = 0; q < E; ++q) s += __builtin_amdgcn_exp2f((x[q] - from) * unit);
+        for (int r = 0; r < kVecs; ++r) {
+            float x[E];
+            widen<T>(raw[r], x);
+#pragma unroll
+            for (int q = 0; q < E; ++q) s += __builtin_amdgcn_exp2f(fmaf(x[q], unit, -c));
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < kVecs; ++r) {
+            float x[E];
+            widen<T>(raw[r], x);
+#pragma unroll
+            for (int q = 0; q < E; ++q) s += __builtin_amdgcn_exp2f((x[q] - from) * unit);
+        }
     }
     v = {top, s};
 }
 
-// The loss: one pass over the row with a running maximum and sum, four vectors a thread in flight.
+// A row's elements [lo, hi): many(from) for each whole chunk of kVecs slabs, one(from, len) for each slab of what is left.
+template <int kSlab, int kVecs, typename Many, typename One>
+__device__ __forceinline__ void over_row(int64_t lo, int64_t hi, Many &&many, One &&one)
+{
+    int64_t from = lo;
+    for (; from + (int64_t)kVecs * kSlab <= hi; from += kVecs * kSlab) many(from);
+#pragma unroll 1
+    for (; from < hi; from += kSlab) one(from, (int)min(hi - from, (int64_t)kSlab));
+}
+
+// kVecs slabs of a row from z on, whole ones.
+template <typename T, int kThreads, int kVecs>
+__device__ __forceinline__ void load_chunk(v4u (&raw)[kVecs], const T *z)
+{
+#pragma unroll
+    for (int r = 0; r < kVecs; ++r) raw[r] = load_slab<T, kThreads>(z, r * kThreads * kVec<T>, (int)threadIdx.x, kVecs * kThreads * kVec<T>,
+                                                                          kVecs * kThreads * kVec<T>);
+}
+// The gradient of(logit) of kVecs vectors, in slabs of which `len` elements exist.
+// All but the first kSure may end inside or lie past it.
+template <typename T, int kThreads, int kVecs, int kSure, typename F>
+__device__ __forceinline__ void store_chunk(T *out, const v4u (&raw)[kVecs], int len, F &&of)
+{
+    constexpr int E = kVec<T>;
+#pragma unroll
+    for (int r = 0; r < kVecs; ++r) {
+        float x[E];
+        widen<T>(raw[r], x);
+#pragma unroll
+        for (int q = 0; q < E; ++q) x[q] = of(x[q]);
+        store_slab<T, kThreads>(out, r * kThreads * E, (int)threadIdx.x, len, narrow<T>(x), r < kSure);
+    }
+}
+
+// Maximum and sum of a whole row, four vectors a thread in flight.
+template <typename T, int kThreads>
+__device__ __forceinline__ Lse take_row(const T *z, int64_t vocab, float unit)
+{
+    constexpr int kSlab = kThreads * kVec<T>;
+    Lse v = {-INFINITY, 0.f};
+    over_row<kSlab, 4>(
+        0, vocab,
+        [&](int64_t from) {
+            v4u raw[4];
+            load_chunk<T, kThreads, 4>(raw, z + from);
+            take<T, 4>(v, raw, unit);
+        },
+        [&](int64_t from, int len) {
+            v4u raw[1] = {load_slab<T, kThreads>(z + from, 0, (int)threadIdx.x, len, len)};
+            settle_slab<T, kThreads>(raw[0], 0, (int)threadIdx.x, len, len, kNegInfBits<T>);
+            take<T, 1>(v, raw, unit);
+        });
+    return v;
+}
+template <typename T, int kThreads, typename F>
+__device__ __forceinline__ void write_row(T *out, const T *z, int64_t lo, int64_t hi, F &&of)
+{
+    constexpr int kSlab = kThreads * kVec<T>;
+    over_row<kSlab, 4>(
+        lo, hi,
+        [&](int64_t from) {
+            v4u raw[4];
+            load_chunk<T, kThreads, 4>(raw, z + from);
+            store_chunk<T, kThreads, 4, 4>(out + from, raw, 4 * kSlab, of);
+        },
+        [&](int64_t from, int len) {
+            v4u raw[1] = {load_slab<T, kThreads>(z + from, 0, (int)threadIdx.x, len, len)};
+            settle_slab<T, kThreads>(raw[0], 0, (int)threadIdx.x, len, len, 0u);
+            store_chunk<T, kThreads, 1, 0>(out + from, raw, len, of);
+        });
+}
+
+// The loss: one pass over the row with a running maximum and sum, four vectors a thread in flight.  The first wavefront forms the list's
+// shares and fetches its logits before the row, so that nothing but a reduction is left when the row is through.
 template <typename T, int kThreads>
 __global__ __launch_bounds__(kThreads) void distill_forward(float *__restrict__ loss, float *__restrict__ lse_out,
                                                             const T *__restrict__ logits, const int32_t *__restrict__ idx,
                                                             const float *__restrict__ val, DistillArgs a)
 {
-    constexpr int E = kVec<T>, kVecs = 4;
-    __shared__ Lse lse_scratch[kThreads / kWave];
+    __shared__ float lse_scratch[2 * kThreads / kWave];
     const int64_t row = blockIdx.x;
     const T *z = logits + row * a.in_stride;
-    Lse v = {-INFINITY, 0.f};
-    for (int64_t at = 0; at < a.vocab; at += (int64_t)kVecs * kThreads * E) {
-        v4u raw[kVecs];
+    Listed e = {};
+    float at[2] = {0.f, 0.f};
+    if (threadIdx.x < kWave) {
+        e = teacher_list(load_list(idx, val, row, a.k), a);
 #pragma unroll
-        for (int r = 0; r < kVecs; ++r) raw[r] = load_row(z, at + (r * kThreads + (int)threadIdx.x) * E, a.vocab, kNegInfBits<T>);
-        take_chunk<T, kThreads, kVecs>(v, raw, a.inv_t * kLog2e);
+        for (int u = 0; u < 2; ++u)
+            if (e.token[u] >= 0) at[u] = widen1(z[e.token[u]]);
     }
+    const Lse v = take_row<T, kThreads>(z, a.vocab, a.inv_t * kLog2e);
     const float lse = lse_value(block_lse<kThreads>(v, a.inv_t * kLog2e, lse_scratch), a.inv_t);
     if (threadIdx.x < kWave) {
-        const Listed e = teacher_list(idx, val, row, a);
-        const float l = list_loss(e, z, lse, a);
+        const float l = list_loss(e, at, lse, a);
         if (threadIdx.x == 0) {
             if (loss) loss[row] = e.any ? l : 0.f;
             if (lse_out) lse_out[row] = lse;
         }
+    }
+}
+
+// Rows shorter than a vector: one wavefront does them.  kLoss: maximum and sum are formed (else lse is given); kGrad: the gradient is written.
+template <typename T, bool kLoss, bool kGrad>
+__global__ __launch_bounds__(kVocabThreads) void distill_any(float *__restrict__ loss, float *__restrict__ lse_out, T *dlogits,
+                                                             const float *__restrict__ dloss, const T *logits,
+                                                             const float *__restrict__ lse_in, const int32_t *__restrict__ idx,
+                                                             const float *__restrict__ val, DistillArgs a)
+{
+    const int64_t row = blockIdx.x;
+    const T *z = logits + row * a.in_stride;
+    if (threadIdx.x >= kWave) return;
+    Listed e = teacher_list(load_list(idx, val, row, a.k), a);
+    float listed[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) listed[u] = e.token[u] >= 0 ? widen1(z[e.token[u]]) : 0.f;
+    float lse;
+    if constexpr (kLoss) {
+        Lse v = {-INFINITY, 0.f};
+        for (int c = 0; c < (int)a.vocab; ++c) v = lse_join(v, {widen1(z[c]), 1.f}, a.inv_t * kLog2e);
+        lse = lse_value(v, a.inv_t);
+        const float l = list_loss(e, listed, lse, a);
+        if (threadIdx.x == 0) {
+            if (loss) loss[row] = e.any ? l : 0.f;
+            if (lse_out) lse_out[row] = lse;
+        }
+    } else {
+        lse = lse_in[row];
+    }
+    if constexpr (kGrad) {
+        T *out = dlogits + row * a.out_stride;
+        const float w = dloss[row] * a.t;
+        float p = 0.f, share = 0.f;
+        const int lane = threadIdx.x;
+        if (lane < (int)a.vocab) p = __builtin_amdgcn_exp2f(fmaf(widen1(z[lane]), a.inv_t, -lse) * kLog2e);
+        for (int t = 0; t < a.k; ++t) {
+            const int32_t token = __builtin_amdgcn_readlane(t < kWave ? e.token[0] : e.token[1], t & (kWave - 1));
+            const float q = lane_value(t < kWave ? e.q[0] : e.q[1], t & (kWave - 1));
+            if (token == lane) share += q;
+        }
+        if (lane < (int)a.vocab) out[lane] = narrow1<T>(e.any ? w * (p - share) : 0.f);
     }
 }
 
@@ -487,15 +665,13 @@ __global__ __launch_bounds__(kThreads) void distill_gradient(T *dlogits, const f
                                                              const float *__restrict__ lse_in, const int32_t *__restrict__ idx,
                                                              const float *__restrict__ val, DistillArgs a, int n_pieces, int64_t piece_len)
 {
-    constexpr int E = kVec<T>, kVecs = 4;
     const int64_t row = blockIdx.x / (unsigned)n_pieces, lo = blockIdx.x % (unsigned)n_pieces * piece_len;
     const int64_t hi = min(lo + piece_len, a.vocab);
     const T *z = logits + row * a.in_stride;
     T *out = dlogits + row * a.out_stride;
     const float lse = lse_in[row];
-    Listed e = teacher_list(idx, val, row, a);
+    Listed e = teacher_list(load_list(idx, val, row, a.k), a);
     const float w = dloss[row] * a.t;
-    auto gradient = [&](float x) { return e.any ? w * __builtin_amdgcn_exp2f(fmaf(x, a.inv_t, -lse) * kLog2e) : 0.f; };
     float listed[2] = {0.f, 0.f};
     if (threadIdx.x < kWave) {
         merge_list(e, a.k);
@@ -506,19 +682,8 @@ __global__ __launch_bounds__(kThreads) void distill_gradient(T *dlogits, const f
         }
     }
     __syncthreads();
-    for (int64_t at = lo; at < hi; at += (int64_t)kVecs * kThreads * E) {
-        v4u raw[kVecs];
-#pragma unroll
-        for (int r = 0; r < kVecs; ++r) raw[r] = load_row(z, at + (r * kThreads + (int)threadIdx.x) * E, hi);
-#pragma unroll
-        for (int r = 0; r < kVecs; ++r) {
-            float x[E];
-            widen<T>(raw[r], x);
-#pragma unroll
-            for (int q = 0; q < E; ++q) x[q] = gradient(x[q]);
-            store_row(out, at + (r * kThreads + (int)threadIdx.x) * E, hi, narrow<T>(x));
-        }
-    }
+    if (e.any) write_row<T, kThreads>(out, z, lo, hi, [&](float x) { return w * __builtin_amdgcn_exp2f(fmaf(x, a.inv_t, -lse) * kLog2e); });
+    else write_row<T, kThreads>(out, z, lo, hi, [](float) { return 0.f; });
     __syncthreads();
     if (threadIdx.x < kWave) {
 #pragma unroll
@@ -532,61 +697,88 @@ __global__ __launch_bounds__(kThreads) void distill_gradient(T *dlogits, const f
 
 // Loss and gradient at once.  kVecs > 0: the row stays in registers, kVecs vectors a thread, and is read once.  kVecs = 0: rows of
 // any length, read a second time for the gradient.
-template <typename T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads) void distill_both(float *__restrict__ loss, T *dlogits, const float *__restrict__ dloss,
+// The first kSure slabs are known to lie inside the row.
+template <typename T, int kThreads, int kVecs, int kSure>
+__global__ __launch_bounds__(kThreads, (kThreads <= 512 ? DBW : 4)) void distill_both(float *__restrict__ loss, T *dlogits, const float *__restrict__ dloss,
                                                          const T *logits, const int32_t *__restrict__ idx, const float *__restrict__ val,
                                                          DistillArgs a)
 {
-    constexpr int E = kVec<T>, kHeld = kVecs ? kVecs : 4;
-    constexpr int64_t kChunk = (int64_t)kHeld * kThreads * E;
-    __shared__ Lse lse_scratch[kThreads / kWave];
+    constexpr int E = kVec<T>, kHeld = kVecs ? kVecs : 1;
+    __shared__ float lse_scratch[2 * kThreads / kWave];
     const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x;
     const T *z = logits + row * a.in_stride;
     T *out = dlogits + row * a.out_stride;
     const float unit = a.inv_t * kLog2e;
-    auto place = [&](int64_t at, int r) { return at + (r * kThreads + (int)threadIdx.x) * E; };
+    __shared__ int any_lds;
+    const bool first = tid < kWave;
+    const float w = dloss[row] * a.t;
+    RawList entries = {};
+    if (first) entries = load_list(idx, val, row, a.k);
     Lse v = {-INFINITY, 0.f};
     v4u raw[kHeld];
-    for (int64_t at = 0; at < (kVecs ? 1 : a.vocab); at += kChunk) {
+    if constexpr (kVecs > 0) {
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r) raw[r] = load_row(z, place(at, r), a.vocab, kNegInfBits<T>);
-        take_chunk<T, kThreads, kHeld>(v, raw, unit);
+        for (int r = 0; r < kHeld; ++r) raw[r] = load_slab<T, kThreads>(z, r * kThreads * E, tid, (int)a.vocab, (int)a.vocab, r < kSure);
     }
-    v = block_lse<kThreads>(v, unit, lse_scratch);
-    Listed e = teacher_list(idx, val, row, a);
-    const float w = dloss[row] * a.t, scale = w / v.sum;
-    auto gradient = [&](float x) { return e.any ? scale * __builtin_amdgcn_exp2f((x - v.top) * unit) : 0.f; };
-    float listed[2] = {0.f, 0.f};
-    if (threadIdx.x < kWave) {
-        const float l = list_loss(e, z, lse_value(v, a.inv_t), a);
-        if (threadIdx.x == 0 && loss) loss[row] = e.any ? l : 0.f;
+    // The first wavefront sees to the list while the row is on its way, and puts it by: beside a row the registers are taken.
+    __shared__ int32_t kept_token[2][kWave];
+    __shared__ float kept_q[2][kWave], kept_logit[2][kWave], kept_logq[2][kWave];
+    if (first) {
+        const Listed e = teacher_list(entries, a);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            kept_token[u][tid] = e.token[u];
+            kept_q[u][tid] = e.q[u];
+            kept_logq[u][tid] = e.logq[u];
+            // before an in-place gradient replaces it
+            kept_logit[u][tid] = e.token[u] >= 0 ? widen1(z[e.token[u]]) : 0.f;
+        }
+        if (tid == 0) any_lds = e.any ? 1 : 0;
+    }
+    if constexpr (kVecs > 0) {
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) settle_slab<T, kThreads>(raw[r], r * kThreads * E, tid, (int)a.vocab, (int)a.vocab, kNegInfBits<T>, r < kSure);
+        take<T, kHeld>(v, raw, unit);
+    } else {
+        v = take_row<T, kThreads>(z, a.vocab, unit);
+    }
+    v = block_lse<kThreads>(v, unit, lse_scratch);                         // (its barriers order the list's reads before the writes below)
+    const bool any = any_lds != 0;
+    const float scale = w / v.sum;
+    const float top = v.top, c = v.top * unit;
+    const bool plain = fabsf(top) < kPlainMax;
+    auto usual = [&](float x) { return scale * __builtin_amdgcn_exp2f(fmaf(x, unit, -c)); };
+    auto wide = [&](float x) { return scale * __builtin_amdgcn_exp2f((x - top) * unit); };
+    auto none = [](float) { return 0.f; };
+    if constexpr (kVecs > 0) {
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) rewiden(raw[r]);
+        if (any && plain) store_chunk<T, kThreads, kHeld, kSure>(out, raw, (int)a.vocab, usual);
+        else if (any) write_row<T, kThreads>(out, z, 0, a.vocab, wide);
+        else write_row<T, kThreads>(out, z, 0, a.vocab, none);
+    } else {
+        if (any && plain) write_row<T, kThreads>(out, z, 0, a.vocab, usual);
+        else if (any) write_row<T, kThreads>(out, z, 0, a.vocab, wide);
+        else write_row<T, kThreads>(out, z, 0, a.vocab, none);
+    }
+    __syncthreads();                                                       // the row is written before its listed tokens are
+    if (first) {
+        Listed e;
+        float listed[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            e.token[u] = kept_token[u][tid];
+            e.q[u] = kept_q[u][tid];
+            e.logq[u] = kept_logq[u][tid];
+            listed[u] = kept_logit[u][tid];
+        }
+        const float l = list_loss(e, listed, lse_value(v, a.inv_t), a);
+        if (tid == 0 && loss) loss[row] = any ? l : 0.f;
         merge_list(e, a.k);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-            if (e.token[u] >= 0) listed[u] = widen1(z[e.token[u]]);        // before an in-place gradient replaces it
-    }
-    __syncthreads();
-    for (int64_t at = 0; at < (kVecs ? 1 : a.vocab); at += kChunk) {
-        if constexpr (kVecs == 0) {
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) raw[r] = load_row(z, place(at, r), a.vocab);
-        }
-#pragma unroll
-        for (int r = 0; r < kHeld; ++r) {
-            float x[E];
-            rewiden(raw[r]);
-            widen<T>(raw[r], x);
-#pragma unroll
-            for (int q = 0; q < E; ++q) x[q] = gradient(x[q]);
-            store_row(out, place(at, r), a.vocab, narrow<T>(x));
-        }
-    }
-    __syncthreads();                                                       // the row is written before its listed tokens are
-    if (threadIdx.x < kWave) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-            if (e.token[u] >= 0)
-                out[e.token[u]] = narrow1<T>(scale * __builtin_amdgcn_exp2f((listed[u] - v.top) * unit) - w * e.q[u]);
+            if (e.token[u] >= 0) out[e.token[u]] = narrow1<T>((plain ? usual(listed[u]) : wide(listed[u])) - w * e.q[u]);
     }
 }
 

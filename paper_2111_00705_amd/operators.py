@@ -36,7 +36,7 @@ def _type(t):
 
 
 def _check(rc):
-    if rc != OK:
+    if rc:
         raise CompAmsError(rc, lib().comp_ams_operators_last_error().decode())
 
 
@@ -61,15 +61,15 @@ def _on_stream(fn):
 def _stream(like, *tensors):
     """The raw current stream; all tensors must be on the GPU of `like`, which has to be the current one."""
     import torch
-    dev = like.device
-    if dev.type != "cuda":
+    if not like.is_cuda:
         raise ValueError("tensors must be on the GPU")
+    dev = like.get_device()
     for t in tensors:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != dev:
             raise ValueError("all tensors must be on the same GPU")
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {dev}, which is not the current GPU")
-    return torch.cuda.current_stream(dev).cuda_stream
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on GPU {dev}, which is not the current one")
+    return torch._C._cuda_getCurrentRawStream(dev)      # what torch.cuda.current_stream(dev).cuda_stream gives, without building a Stream
 
 
 def _rows(t, what):
@@ -102,7 +102,7 @@ def _like(out, t, what):
     """out (new and dense if None), which must have t's shape and type."""
     import torch
     if out is None:
-        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
     _need(out.shape == t.shape and out.dtype == t.dtype, f"{what} must have the shape and type of its input")
     return out
 
@@ -139,7 +139,7 @@ def layer_norm(x, gain, shift=None, eps=1e-5, out=None):
         _vector(shift, cols, torch.float32, "shift")
     s = _stream(x, gain, shift, out)
     y = _like(out, x, "out")
-    y_rows, _, y_stride = _rows(y, "out")
+    y_stride = x_stride if out is None and x.is_contiguous() else _rows(y, "out")[2]
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
     _check(lib().comp_ams_layer_norm(y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), x.data_ptr(), gain.data_ptr(),
@@ -270,9 +270,9 @@ def token_logprobs(logits, tokens=None, k=0):
     s = _stream(logits, tokens)
     f32 = dict(dtype=torch.float32, device=logits.device)
     logp = None if tokens is None else torch.empty(rows, **f32)
-    entropy = torch.empty(rows, **f32)
-    idx = torch.empty((rows, k), dtype=torch.int32, device=logits.device)
+    entropy = torch.empty(rows, **f32) if logp is None else torch.empty_like(logp)
     top = torch.empty((rows, k), **f32)
+    idx = torch.empty_like(top, dtype=torch.int32)
     L, kind = lib(), _type(logits)
     work, work_ptr, work_bytes = _work(L.comp_ams_token_logprobs_work_bytes, logits.device, rows, vocab, k, kind)
     _check(L.comp_ams_token_logprobs(None if logp is None else logp.data_ptr(), entropy.data_ptr(), idx.data_ptr(), top.data_ptr(),
