@@ -19,6 +19,7 @@ struct BiasArgs {
     int64_t offset;
     float scale;
     int32_t causal;
+    bool stream_out;                      // p, ds are stored as a stream
 };
 
 constexpr int kBiasThreads = 256;
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_forward(T *p, const T 
                     for (int q = 0; q < E; ++q) t[v][q] *= inv;
                     out = narrow<T>(t[v]);
                 }
-                store_slab<T, kTeam>(row, slab, me.lane, tk, out);
+                store_slab<T, kTeam>(row, slab, me.lane, tk, out, false, a.stream_out);
             }
         } else {
             // Nothing seen, nothing but -infinity, a NaN or a +infinity; or scores that leave fp32 in units of log 2, like a row masked
@@ -260,10 +261,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_forward(T *p, const T 
 // added to the team's array over relative positions in LDS, in two phases because the diagonals left of a lane's first key are its
 // neighbour's.  At the end the teams' arrays are added up over each bucket's positions, in a fixed order.  kBatch rows are worked on together, and as many are on their way.
 template <typename T, int kTeam, int kVecs, int kStep, int kBatch>
-#ifndef BBW
-#define BBW 1
-#endif
-__global__ __launch_bounds__(kTeamBlock<kTeam>, BBW) void bias_backward(T *ds, float *__restrict__ work, const T *dp, const T *__restrict__ p,
+__global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float *__restrict__ work, const T *dp, const T *__restrict__ p,
                                                                  Bounds bounds, const int32_t *__restrict__ key_len, BiasArgs a,
                                                                  int pieces, int rows_team, unsigned worker_batch)
 {
@@ -385,7 +383,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>, BBW) void bias_backward(T *ds, f
                         }
                         out = narrow<T>(dw);
                     }
-                    if (i < tq) store_slab<T, kTeam>(row, slab, me.lane, tk, out);
+                    if (i < tq) store_slab<T, kTeam>(row, slab, me.lane, tk, out, false, a.stream_out);
                 }
             }
         }

@@ -7,6 +7,7 @@ namespace cams_ops {
 struct NormArgs {
     int64_t rows, cols, x_stride, y_stride, dy_stride;   // y_stride: that of dx in the backward pass
     float eps, inv_cols;
+    bool stream_out;                                     // y, dx are stored as a stream
 };
 
 constexpr int kNormThreads = 256;
@@ -151,7 +152,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_forward(T *y, float *_
         for (int v = 0; v < kVecs; ++v) {
 #pragma unroll
             for (int q = 0; q < E; ++q) d[v][q] = fmaf(d[v][q] * r, g[v][q], b[v][q]);
-            store_slab<T, kTeam>(y + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(d[v]), v < kVecs - 1);
+            store_slab<T, kTeam>(y + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(d[v]), v < kVecs - 1, a.stream_out);
         }
         if (me.lane == 0) {
             if (mean) mean[row] = mu;
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void norm_backward(T *dx, float 
         for (int v = 0; v < kVecs; ++v) {
 #pragma unroll
             for (int q = 0; q < E; ++q) up[v][q] = scale * (fmaf(up[v][q], g[v][q], -s) - xh[v][q] * q2);
-            store_slab<T, kTeam>(dx + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(up[v]), v < kVecs - 1);
+            store_slab<T, kTeam>(dx + row * a.y_stride, v * kTeam * E, me.lane, cols, narrow<T>(up[v]), v < kVecs - 1, a.stream_out);
         }
         row = next;
     }

@@ -77,16 +77,30 @@ template <> __device__ __forceinline__ v4u narrow<f16_t>(const float (&x)[8])
     return r;
 }
 
-#ifdef NTL
-template <typename T> __device__ __forceinline__ v4u load_vec(const T *p) { return __builtin_nontemporal_load(reinterpret_cast<const v4u_any *>(p)); }
-#else
-template <typename T> __device__ __forceinline__ v4u load_vec(const T *p) { return *reinterpret_cast<const v4u_any *>(p); }
-#endif
-#ifdef NTS
-template <typename T> __device__ __forceinline__ void store_vec(T *p, const v4u &v) { __builtin_nontemporal_store(v, reinterpret_cast<v4u_any *>(p)); }
-#else
-template <typename T> __device__ __forceinline__ void store_vec(T *p, const v4u &v) { *reinterpret_cast<v4u_any *>(p) = v; }
-#endif
+// `stream`, uniform: the access is not to be kept in the caches (see streamed() on the host side).  The empty statements keep the two
+// forms apart, which the compiler would merge into one without the hint.
+template <typename T> __device__ __forceinline__ v4u load_vec(const T *p, bool stream = false)
+{
+    v4u v;
+    if (stream) {
+        asm volatile("");
+        v = __builtin_nontemporal_load(reinterpret_cast<const v4u_any *>(p));
+        asm volatile("");
+    } else {
+        v = *reinterpret_cast<const v4u_any *>(p);
+    }
+    return v;
+}
+template <typename T> __device__ __forceinline__ void store_vec(T *p, const v4u &v, bool stream = false)
+{
+    if (stream) {
+        asm volatile("");
+        __builtin_nontemporal_store(v, reinterpret_cast<v4u_any *>(p));
+        asm volatile("");
+    } else {
+        *reinterpret_cast<v4u_any *>(p) = v;
+    }
+}
 
 // Makes the compiler take what is widened from `v` before and after for different values: a row held in registers is widened anew
 // by each pass over it, instead of being kept in its wide form too.
@@ -117,11 +131,11 @@ template <typename T> __device__ __forceinline__ T *offset32(T *base, int at)
 
 // Elements [at, at + kVec) of a row of `len` in the lanes with at < need (need <= len), not in place yet; the other lanes' are zero.
 template <typename T, int kTeam>
-__device__ __forceinline__ v4u load_slab(const T *row, int first, int lane, int len, int need, bool sure = false)
+__device__ __forceinline__ v4u load_slab(const T *row, int first, int lane, int len, int need, bool sure = false, bool stream = false)
 {
     constexpr int E = kVec<T>;
     const int at = first + lane * E;
-    if (sure || first + kTeam * E <= need) return load_vec(offset32(row, at));
+    if (sure || first + kTeam * E <= need) return load_vec(offset32(row, at), stream);
     v4u raw = {0u, 0u, 0u, 0u};
     if (at < need) raw = load_vec(row + min(at, len - E));
     return raw;
@@ -169,13 +183,13 @@ typedef uint32_t v2u_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u_any __attribute__((aligned(2)));
 
 template <typename T, int kTeam>
-__device__ __forceinline__ void store_slab(T *row, int first, int lane, int len, const v4u &raw, bool sure = false)
+__device__ __forceinline__ void store_slab(T *row, int first, int lane, int len, const v4u &raw, bool sure = false, bool stream = false)
 {
     constexpr int E = kVec<T>;
     const int at = first + lane * E;
     T *p = offset32(row, at);
     if (sure || first + kTeam * E <= len || at + E <= len) {
-        store_vec(p, raw);
+        store_vec(p, raw, stream);
     } else if (at < len) {                          // a binary number of elements is left
         const int rest = len - at;
         if constexpr (sizeof(T) == 4) {

@@ -16,22 +16,21 @@ using namespace cams_ops;
 
 namespace {
 
-#ifndef T64
-#define T64 128
-#endif
-#ifndef BIAS_BLOCKS
-#define BIAS_BLOCKS 640
-#endif
-#ifndef BIAS_FBLOCKS
-#define BIAS_FBLOCKS 1536
-#endif
 #ifndef NORM_BLOCKS
 #define NORM_BLOCKS 2048
 #endif
 #ifndef NORM_CHUNKS
-#define NORM_CHUNKS 512
+#define NORM_CHUNKS 1024
 #endif
-
+#ifndef BIAS_BLOCKS
+#define BIAS_BLOCKS 6400
+#endif
+#ifndef BIAS_FBLOCKS
+#define BIAS_FBLOCKS 1536
+#endif
+#ifndef T64
+#define T64 128
+#endif
 thread_local char g_error[512] = "";
 
 int fail(int code, const char *fmt, ...)
@@ -84,6 +83,11 @@ void with_type(int32_t type, F &&f)
                 (long long)(stride), (long long)(cols));                                                                       \
         REQUIRE((stride) >= 0 && ((rows) <= 1 || (stride) < kMaxElements / (rows)), "%s: %s is out of range", what, name);        \
     } while (0)
+
+// Whether an array that a call reads or writes once is streamed past the caches.  What is written is read by the model's next
+// operation, if anything of it is left in the 256 MB memory-side cache by then; what is read was written by the one before.
+bool streamed_out(int64_t elements, int32_t type) { return elements * (int64_t)type_size(type) > (int64_t)80 << 20; }
+bool streamed_in(int64_t elements, int32_t type) { return elements * (int64_t)type_size(type) > (int64_t)256 << 20; }
 
 // --- constants chosen from sizes, as types ---------------------------------------------------------------------------
 
@@ -272,7 +276,7 @@ int comp_ams_layer_norm(void *y, float *mean, float *rstd, const void *x, const 
     REQUIRE(std::isfinite(eps) && eps >= 0.f, "%s: eps must be finite and not negative", what);
     if (rows == 0) return COMP_AMS_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const NormArgs a = {rows, cols, x_stride, y_stride, 0, eps, (float)(1.0 / (double)cols)};
+    const NormArgs a = {rows, cols, x_stride, y_stride, 0, eps, (float)(1.0 / (double)cols), streamed_out(rows * cols, type)};
     with_type(type, [&](auto t) {
         using T = decltype(t);
         const bool held = with_team<T>(cols, [&](auto shape) {
@@ -321,7 +325,7 @@ int comp_ams_layer_norm_backward(void *dx, void *dgain, void *dshift, const void
     REQUIRE(work && work_bytes >= need, "%s: needs %llu bytes of work memory", what, (unsigned long long)need);
     REQUIRE(aligned(work, 16), "%s: work must be 16-byte aligned", what);
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const NormArgs a = {rows, cols, x_stride, dx_stride, dy_stride, 0.f, (float)(1.0 / (double)cols)};
+    const NormArgs a = {rows, cols, x_stride, dx_stride, dy_stride, 0.f, (float)(1.0 / (double)cols), streamed_out(rows * cols, type)};
     const NormChunks ch = norm_chunks(rows / n, n);
     float *sums = static_cast<float *>(work);
     with_type(type, [&](auto t) {
@@ -364,7 +368,7 @@ int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const 
     a.heads = heads, a.tq = tq, a.tk = tk, a.rows = batch * heads * tq;
     a.s_b = s_strides_host[0], a.s_h = s_strides_host[1], a.s_q = s_strides_host[2];
     a.p_b = p_strides_host[0], a.p_h = p_strides_host[1], a.p_q = p_strides_host[2];
-    a.offset = offset, a.scale = scale, a.causal = causal != 0;
+    a.offset = offset, a.scale = scale, a.causal = causal != 0, a.stream_out = streamed_out(a.rows * tk, type);
     with_type(type, [&](auto t) {
         using T = decltype(t);
         const bool held = tk <= 1024 * kVec<T> && with_team<T>(tk, [&](auto shape) {
@@ -432,7 +436,7 @@ int comp_ams_rel_bias_softmax_backward(void *ds, void *dtable, const void *dp, c
         a.o_b = strides_host[0], a.o_h = strides_host[1], a.o_q = strides_host[2];
         a.s_b = strides_host[3], a.s_h = strides_host[4], a.s_q = strides_host[5];
         a.p_b = strides_host[6], a.p_h = strides_host[7], a.p_q = strides_host[8];
-        a.offset = offset, a.scale = scale, a.causal = causal != 0;
+        a.offset = offset, a.scale = scale, a.causal = causal != 0, a.stream_out = streamed_out(a.rows * tk, type);
         with_type(type, [&](auto t) {
             using T = decltype(t);
             const unsigned grid = (unsigned)(batch * heads * cut.pieces);
@@ -506,7 +510,8 @@ int comp_ams_token_logprobs(float *logp, float *entropy, int32_t *top_idx, float
         auto launch = [&](auto shape) {
             using S = decltype(shape);
             logprobs_regs<T, S::threads, S::vecs><<<(unsigned)(rows * s.count), S::threads, 0, stream>>>(
-                logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, groups, s.count, s.len, pieces, keys);
+                logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, groups, s.count, s.len,
+                s.len < (int64_t)S::threads * S::vecs * kVec<T> ? 1 : 0, pieces, keys);
         };
         if (s.threads == kPieceThreads) with_vecs<kPieceThreads, 1, kPieceVecs>(s.vecs, launch);
         else launch(Shape<kPieceThreads / 2, 1>{});
@@ -524,7 +529,7 @@ int comp_ams_distill(float *loss, float *lse, const void *logits, const int32_t 
     if (const int rc = distill_check(what, logits, idx, val, rows, vocab, stride, k, temperature, type)) return rc;
     REQUIRE(aligned(loss, 4) && aligned(lse, 4), "%s: loss and lse must be 4-byte aligned", what);
     if (rows == 0) return COMP_AMS_OK;
-    const DistillArgs a = {rows, vocab, stride, 0, k, temperature, 1.f / temperature};
+    const DistillArgs a = {rows, vocab, stride, 0, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type)};
     with_type(type, [&](auto t) {
         using T = decltype(t);
         auto launch = [&](auto shape) {
@@ -551,7 +556,7 @@ int comp_ams_distill_backward(void *dlogits, const float *dloss, const void *log
     REQUIRE((dloss && lse) || rows == 0, "%s: dloss or lse is NULL", what);
     REQUIRE(aligned(dloss, 4) && aligned(lse, 4), "%s: dloss and lse must be 4-byte aligned", what);
     if (rows == 0) return COMP_AMS_OK;
-    const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature};
+    const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type)};
     with_type(type, [&](auto t) {
         using T = decltype(t);
         if (vocab < kVec<T>) {
@@ -579,7 +584,7 @@ int comp_ams_distill_grad(float *loss, void *dlogits, const float *dloss, const 
     REQUIRE(dloss || rows == 0, "%s: dloss is NULL", what);
     REQUIRE(aligned(dloss, 4) && aligned(loss, 4), "%s: dloss and loss must be 4-byte aligned", what);
     if (rows == 0) return COMP_AMS_OK;
-    const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature};
+    const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type)};
     with_type(type, [&](auto t) {
         using T = decltype(t);
         auto launch = [&](auto shape) {

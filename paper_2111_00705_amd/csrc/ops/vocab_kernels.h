@@ -5,12 +5,6 @@
 
 namespace cams_ops {
 
-#ifndef LPW
-#define LPW 8
-#endif
-#ifndef DBW
-#define DBW 6
-#endif
 constexpr int kVocabThreads = 256;
 constexpr int kMaxTop = COMP_AMS_MAX_TOP;
 
@@ -169,6 +163,53 @@ __device__ __attribute__((noinline)) void select_slow(const T *z, int64_t lo, in
     __syncthreads();
 }
 
+// The odd rows of a 16-bit array with an odd stride start between two dwords, where 16-byte loads lose a sixth of their rate (6.2 against
+// 5.2 TB/s on 1 GB read).  Such a row is read from the element before it, which belongs to the row before or to the space between, and
+// which is then ignored.  Returns how many elements that is; the first row of an array is taken as it stands.
+template <typename T>
+__device__ __forceinline__ int step_back(const T *z, int64_t row)
+{
+    return sizeof(T) == 2 && row > 0 && (reinterpret_cast<uintptr_t>(z) & 2) ? 1 : 0;
+}
+
+// Calls place(key, rank) for each of n keys in LDS with the number of larger ones, where that is below k.  Several lanes share a key
+// while there are lanes enough.
+template <int kThreads, typename F>
+__device__ __forceinline__ void rank_keys(const uint64_t *list, int n, int k, F &&place)
+{
+    const int lanes = n <= kThreads / 8 ? 8 : n <= kThreads / 4 ? 4 : n <= kThreads / 2 ? 2 : 1;
+    const int sub = threadIdx.x & (lanes - 1);
+    for (int t = threadIdx.x / lanes; t < n; t += kThreads / lanes) {
+        const uint64_t key = list[t];
+        int rank = 0;
+#pragma unroll 4
+        for (int q = sub; q < n; q += lanes) rank += list[q] > key ? 1 : 0;
+        for (int off = 1; off < lanes; off <<= 1) rank += __shfl_xor(rank, off, kWave);
+        if (sub == 0 && rank < k) place(key, rank);
+    }
+}
+
+// The k-th largest of `groups` (64, 128 or 256) values in LDS as its place in the order, by one wavefront: bisection over the bits of the
+// order, counting by ballots.  kBits: how many of them, from the top, tell values of the type apart.
+template <int kBits>
+__device__ __forceinline__ uint32_t kth_largest(const float *values, int groups, int k)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    uint32_t o[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) o[u] = u * kWave < groups ? order_of(values[u * kWave + lane]) : 0u;
+    uint32_t at = 0;
+    for (int bit = 31; bit > 31 - kBits; --bit) {
+        const uint32_t more = at | (1u << bit);
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) n += __popcll(__ballot(o[u] >= more));
+        if (n >= k) at = more;
+        if (n == k) break;                       // exactly k reach it: a bound as good as the k-th value itself
+    }
+    return at;
+}
+
 // One piece of a row per workgroup, held in registers between the two looks at it: maximum, sum and moment, and then the
 // elements that can be among the k best.  Those are found by a bound: the k-th largest of the maxima of `groups` groups of lanes is
 // reached by k elements at least, and by few more (k = 32 of 64 groups: 44 expected).  Vectors that reach it are queued in LDS, their
@@ -178,21 +219,25 @@ __device__ __attribute__((noinline)) void select_slow(const T *z, int64_t lo, in
 constexpr int kMaxQueued = 256;           // vectors that reach the bound; more than that (rows of ties) are told apart by select_slow
 
 template <typename T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict__ logp, float *__restrict__ entropy,
+__global__ __launch_bounds__(kThreads, 8) void logprobs_regs(float *__restrict__ logp, float *__restrict__ entropy,
                                                           int32_t *__restrict__ top_idx, float *__restrict__ top_logp,
                                                           const T *__restrict__ logits, const int64_t *__restrict__ tokens,
                                                           int64_t vocab, int64_t stride, int k, int groups, int n_pieces,
-                                                          int64_t piece_len, Piece *__restrict__ pieces, uint64_t *__restrict__ keys)
+                                                          int64_t piece_len, int room, Piece *__restrict__ pieces, uint64_t *__restrict__ keys)
 {
     constexpr int E = kVec<T>, kWaves = kThreads / kWave;
     __shared__ float scratch[kWaves], sum_of[kWaves], moment_of[kWaves], group_max[256];
     __shared__ uint64_t list[kMaxQueued * E];
-    __shared__ int queue[kMaxQueued];
-    __shared__ uint32_t count, queued, strange;
-    __shared__ float bound_lds, lse_lds;
+    __shared__ v4u queue[kMaxQueued];
+    __shared__ int queue_at[kMaxQueued];
+    __shared__ uint32_t count, queued, strange, bound_order;
+    __shared__ float lse_lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int64_t row = blockIdx.x / (unsigned)n_pieces, lo = blockIdx.x % (unsigned)n_pieces * piece_len;
-    const int len = (int)(min(lo + piece_len, vocab) - lo);
+    const int64_t row = blockIdx.x / (unsigned)n_pieces, begin = blockIdx.x % (unsigned)n_pieces * piece_len;
+    // `back` elements before the row's first one take part in the loads and in nothing else; room: there is a place for one
+    const int back = begin == 0 && room ? step_back(logits + row * stride, row) : 0;
+    const int64_t lo = begin - back;
+    const int len = (int)(min(begin + piece_len, vocab) - lo);
     const T *z = logits + row * stride + lo;
     auto empty = [&](int v) { return v >= kVecs - 2 && (v * kThreads + wave * kWave) * E >= len; };      // nothing for this wavefront
     v4u raw[kVecs];
@@ -205,6 +250,7 @@ __global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict
         if (empty(v)) continue;
         float x[E];
         settle_slab<T, kThreads>(raw[v], v * kThreads * E, tid, len, len, kNegInfBits<T>, v < kVecs - 2);
+        if (v == 0 && back && tid == 0) raw[v][0] = (raw[v][0] & 0xffff0000u) | kNegInfBits<T>;
         widen<T>(raw[v], x);
 #pragma unroll
         for (int q = 0; q < E; ++q) vec_max[v] = MaxOp::apply(vec_max[v], x[q]);
@@ -217,10 +263,7 @@ __global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict
         for (int off = 1; off < per; off <<= 1) g = MaxOp::apply(g, __shfl_xor(g, off, kWave));
         if ((tid & (per - 1)) == 0) group_max[tid / per] = g;
     }
-    if (tid == 0) {
-        count = queued = strange = 0;
-        bound_lds = 0.f;                          // stays so where a NaN keeps the maxima from being ranked
-    }
+    if (tid == 0) count = queued = strange = 0;
     const float m = team_reduce<MaxOp, kThreads>(top, scratch);
     // exp(x - m) as 2^(x log2 e - c): the same rounding of c = m log2 e in every term and in the moment, and taken back in lse
     const float c = m * kLog2e;
@@ -228,9 +271,9 @@ __global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict
     if (fabsf(m) < kPlainMax) {
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
+            rewiden(raw[v]);
             if (empty(v)) continue;
             float x[E];
-            rewiden(raw[v]);
             widen<T>(raw[v], x);
 #pragma unroll
             for (int q = 0; q < E; ++q) {
@@ -238,10 +281,11 @@ __global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict
                 s += e;
                 w = fmaf(e, fmaxf(d, -1e30f), w);       // an infinite distance has e = 0
             }
+            __builtin_amdgcn_sched_barrier(0);          // one vector after the other: few registers, and four workgroups a compute unit
         }
     } else {
 #pragma unroll 1
-        for (int q = tid; q < len; q += kThreads) {     // infinities, or nothing but -infinity and NaN, or near the end of fp32's range
+        for (int q = tid + back; q < len; q += kThreads) {     // infinities, or nothing but -infinity and NaN, or near the end of fp32's range
             const float x = widen1(z[q]), d = (x - m) * kLog2e, e = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
             s += e;
             w = fmaf(e, fmaxf(d, -1e30f), w);
@@ -254,29 +298,20 @@ __global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict
         moment_of[wave] = w;
         if (!(fabsf(s) < INFINITY)) strange = 1;        // a NaN or an infinity: the bound says nothing then
     }
-    if (tid < groups && k > 0) {
-        const float g = group_max[tid];
-        int rank = 0;
-        for (int q = 0; q < groups; ++q) {
-            const float o = group_max[q];
-            rank += (o > g || (o == g && q < tid)) ? 1 : 0;
-        }
-        if (rank == k - 1) bound_lds = g;
+    if (k > 0 && wave == kWaves - 1) {
+        const uint32_t o = kth_largest<8 * (int)sizeof(T)>(group_max, groups, k);
+        if ((tid & (kWave - 1)) == 0) bound_order = o;
     }
     __syncthreads();
     const bool whole = n_pieces == 1;
-    if (tid == 0) {
-        Piece piece = {m, sum_of[0], moment_of[0]};
-#pragma unroll
-        for (int q = 1; q < kWaves; ++q) {
-            piece.sum += sum_of[q];
-            piece.moment += moment_of[q];
-        }
-        const float lse = piece_lse(piece);
-        lse_lds = lse;
-        if (!whole) {
-            pieces[blockIdx.x] = piece;
-        } else {
+    if (wave == 0) {
+        const int q = tid & 15;
+        const Piece piece = {m, lanes_reduce<SumOp, 16>(q < kWaves ? sum_of[q] : 0.f),
+                             lanes_reduce<SumOp, 16>(q < kWaves ? moment_of[q] : 0.f)};
+        if (tid == 0 && !whole) pieces[blockIdx.x] = piece;
+        if (tid == 0 && whole) {
+            const float lse = piece_lse(piece);
+            lse_lds = lse;
             if (entropy) entropy[row] = piece_entropy(piece);
             if (logp) {
                 const int64_t t = tokens[row];
@@ -285,7 +320,8 @@ __global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict
         }
     }
     if (k == 0) return;
-    const float bound = bound_lds;
+    float bound = logit_of((uint64_t)bound_order << 32);
+    if (bound != bound) bound = -INFINITY;        // places below -infinity's are no number's
     // one atomic a wavefront for all its vectors
     uint64_t reach[kVecs];
     int total = 0;
@@ -302,43 +338,42 @@ __global__ __launch_bounds__(kThreads, LPW) void logprobs_regs(float *__restrict
         for (int v = 0; v < kVecs; ++v) {
             if (reach[v]) {
                 const uint32_t slot = from + __builtin_amdgcn_mbcnt_hi((uint32_t)(reach[v] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)reach[v], 0u));
-                if (vec_max[v] >= bound && slot < (uint32_t)kMaxQueued) queue[slot] = (v * kThreads + tid) * E;
+                if (vec_max[v] >= bound && slot < (uint32_t)kMaxQueued) {
+                    queue[slot] = raw[v];
+                    queue_at[slot] = (v * kThreads + tid) * E;
+                }
                 from += __popcll(reach[v]);
             }
         }
     }
     __syncthreads();
     if (strange || queued > (uint32_t)kMaxQueued) {
-        if (len > k) {
-            select_slow<T, kThreads>(logits + row * stride, lo, lo + len, k, list, &count);
+        if (len - back > k) {
+            select_slow<T, kThreads>(logits + row * stride, begin, lo + len, k, list, &count);
         } else {
-            if (tid == 0) count = (uint32_t)len;
-            for (int q = tid; q < len; q += kThreads) list[q] = rank_key(widen1(z[q]), (uint32_t)(lo + q));
+            if (tid == 0) count = (uint32_t)(len - back);
+            for (int q = tid + back; q < len; q += kThreads) list[q - back] = rank_key(widen1(z[q]), (uint32_t)(lo + q));
         }
     } else {
         for (int t = tid; t < (int)queued * E; t += kThreads) {
-            const int at = queue[t / E] + t % E;
-            if (at < len) {
-                const float x = widen1(z[at]);
-                if (x >= bound) list[atomicAdd(&count, 1u)] = rank_key(x, (uint32_t)(lo + at));
-            }
+            const int at = queue_at[t / E] + t % E;
+            const uint32_t word = queue[t / E][t % E * (int)sizeof(T) / 4];
+            float x;
+            if constexpr (sizeof(T) == 4) x = __uint_as_float(word);
+            else x = widen1(T{(uint16_t)((t & 1) ? word >> 16 : word)});
+            if (x >= bound && at >= back && at < len) list[atomicAdd(&count, 1u)] = rank_key(x, (uint32_t)(lo + at));
         }
     }
     __syncthreads();
     const int n = (int)count;
-    for (int t = tid; t < n; t += kThreads) {
-        const uint64_t key = list[t];
-        int rank = 0;
-        for (int q = 0; q < n; ++q) rank += list[q] > key ? 1 : 0;
-        if (rank < k) {
-            if (whole) {
-                top_idx[row * k + rank] = (int32_t)~(uint32_t)key;
-                top_logp[row * k + rank] = logit_of(key) - lse_lds;
-            } else {
-                keys[(int64_t)blockIdx.x * k + rank] = key;
-            }
+    rank_keys<kThreads>(list, n, k, [&](uint64_t key, int rank) {
+        if (whole) {
+            top_idx[row * k + rank] = (int32_t)~(uint32_t)key;
+            top_logp[row * k + rank] = logit_of(key) - lse_lds;
+        } else {
+            keys[(int64_t)blockIdx.x * k + rank] = key;
         }
-    }
+    });
     if (!whole)
         for (int t = n + tid; t < k; t += kThreads) keys[(int64_t)blockIdx.x * k + t] = 0;   // a short last piece
 }
@@ -366,11 +401,23 @@ __global__ __launch_bounds__(kVocabThreads) void logprobs_join(float *__restrict
         }
     }
     __syncthreads();
+    // every piece's keys are in descending order: a key's rank is its place among its own plus, by bisection, how many of each other
+    // piece's are larger
     for (int t = threadIdx.x; t < n; t += kVocabThreads) {
         const uint64_t key = list[t];
-        int rank = 0;
-        for (int q = 0; q < n; ++q) rank += list[q] > key ? 1 : 0;
-        if (rank < k && key) {
+        const int own = t / k;
+        int rank = t - own * k;
+        if (!key) continue;
+        for (int q = 0; q < n_pieces; ++q) {
+            if (q == own) continue;
+            int lo = 0, hi = k;                  // keys [0, lo) are larger, those from hi on are not
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (list[q * k + mid] > key) lo = mid + 1; else hi = mid;
+            }
+            rank += lo;
+        }
+        if (rank < k) {
             top_idx[row * k + rank] = (int32_t)~(uint32_t)key;
             top_logp[row * k + rank] = logit_of(key) - lse;
         }
@@ -383,6 +430,7 @@ struct DistillArgs {
     int64_t rows, vocab, in_stride, out_stride;
     int32_t k;
     float t, inv_t;          // the temperature and its reciprocal
+    bool stream_in, stream_out;
 };
 
 // The teacher's list of one row, two entries in each lane of a wavefront: every wavefront that needs the list forms its shares for
@@ -528,16 +576,16 @@ __device__ __forceinline__ void over_row(int64_t lo, int64_t hi, Many &&many, On
 
 // kVecs slabs of a row from z on, whole ones.
 template <typename T, int kThreads, int kVecs>
-__device__ __forceinline__ void load_chunk(v4u (&raw)[kVecs], const T *z)
+__device__ __forceinline__ void load_chunk(v4u (&raw)[kVecs], const T *z, bool stream)
 {
 #pragma unroll
     for (int r = 0; r < kVecs; ++r) raw[r] = load_slab<T, kThreads>(z, r * kThreads * kVec<T>, (int)threadIdx.x, kVecs * kThreads * kVec<T>,
-                                                                          kVecs * kThreads * kVec<T>);
+                                                                          kVecs * kThreads * kVec<T>, true, stream);
 }
 // The gradient of(logit) of kVecs vectors, in slabs of which `len` elements exist.
 // All but the first kSure may end inside or lie past it.
 template <typename T, int kThreads, int kVecs, int kSure, typename F>
-__device__ __forceinline__ void store_chunk(T *out, const v4u (&raw)[kVecs], int len, F &&of)
+__device__ __forceinline__ void store_chunk(T *out, const v4u (&raw)[kVecs], int len, bool stream, F &&of)
 {
     constexpr int E = kVec<T>;
 #pragma unroll
@@ -546,45 +594,64 @@ __device__ __forceinline__ void store_chunk(T *out, const v4u (&raw)[kVecs], int
         widen<T>(raw[r], x);
 #pragma unroll
         for (int q = 0; q < E; ++q) x[q] = of(x[q]);
-        store_slab<T, kThreads>(out, r * kThreads * E, (int)threadIdx.x, len, narrow<T>(x), r < kSure);
+        store_slab<T, kThreads>(out, r * kThreads * E, (int)threadIdx.x, len, narrow<T>(x), r < kSure, stream);
     }
 }
 
-// Maximum and sum of a whole row, four vectors a thread in flight.
+// Maximum and sum of a whole row: two sets of vectors, one of them on its way while the other is taken.
 template <typename T, int kThreads>
-__device__ __forceinline__ Lse take_row(const T *z, int64_t vocab, float unit)
+__device__ __forceinline__ Lse take_row(const T *z, int64_t vocab, float unit, bool stream, int back)
 {
-    constexpr int kSlab = kThreads * kVec<T>;
+    constexpr int kVecs = 4, kSlab = kThreads * kVec<T>, kChunk = kVecs * kSlab;
+    z -= back;
+    vocab += back;
+    auto ignore = [&](v4u &raw) {
+        if (back && threadIdx.x == 0) raw[0] = (raw[0] & 0xffff0000u) | kNegInfBits<T>;
+    };
     Lse v = {-INFINITY, 0.f};
-    over_row<kSlab, 4>(
-        0, vocab,
-        [&](int64_t from) {
-            v4u raw[4];
-            load_chunk<T, kThreads, 4>(raw, z + from);
-            take<T, 4>(v, raw, unit);
-        },
-        [&](int64_t from, int len) {
-            v4u raw[1] = {load_slab<T, kThreads>(z + from, 0, (int)threadIdx.x, len, len)};
-            settle_slab<T, kThreads>(raw[0], 0, (int)threadIdx.x, len, len, kNegInfBits<T>);
-            take<T, 1>(v, raw, unit);
-        });
+    int64_t from = 0;
+    if (vocab >= kChunk) {
+        v4u raw[2][kVecs];
+        load_chunk<T, kThreads, kVecs>(raw[0], z, stream);
+        ignore(raw[0][0]);
+        for (;;) {
+            from += kChunk;
+            bool more = from + kChunk <= vocab;
+            if (more) load_chunk<T, kThreads, kVecs>(raw[1], z + from, stream);
+            take<T, kVecs>(v, raw[0], unit);
+            if (!more) break;
+            from += kChunk;
+            more = from + kChunk <= vocab;
+            if (more) load_chunk<T, kThreads, kVecs>(raw[0], z + from, stream);
+            take<T, kVecs>(v, raw[1], unit);
+            if (!more) break;
+        }
+    }
+#pragma unroll 1
+    for (; from < vocab; from += kSlab) {
+        const int len = (int)min(vocab - from, (int64_t)kSlab);
+        v4u raw[1] = {load_slab<T, kThreads>(z + from, 0, (int)threadIdx.x, len, len)};
+        settle_slab<T, kThreads>(raw[0], 0, (int)threadIdx.x, len, len, kNegInfBits<T>);
+        if (from == 0) ignore(raw[0]);
+        take<T, 1>(v, raw, unit);
+    }
     return v;
 }
 template <typename T, int kThreads, typename F>
-__device__ __forceinline__ void write_row(T *out, const T *z, int64_t lo, int64_t hi, F &&of)
+__device__ __forceinline__ void write_row(T *out, const T *z, int64_t lo, int64_t hi, const DistillArgs &a, F &&of)
 {
     constexpr int kSlab = kThreads * kVec<T>;
     over_row<kSlab, 4>(
         lo, hi,
         [&](int64_t from) {
             v4u raw[4];
-            load_chunk<T, kThreads, 4>(raw, z + from);
-            store_chunk<T, kThreads, 4, 4>(out + from, raw, 4 * kSlab, of);
+            load_chunk<T, kThreads, 4>(raw, z + from, a.stream_in);
+            store_chunk<T, kThreads, 4, 4>(out + from, raw, 4 * kSlab, a.stream_out, of);
         },
         [&](int64_t from, int len) {
             v4u raw[1] = {load_slab<T, kThreads>(z + from, 0, (int)threadIdx.x, len, len)};
             settle_slab<T, kThreads>(raw[0], 0, (int)threadIdx.x, len, len, 0u);
-            store_chunk<T, kThreads, 1, 0>(out + from, raw, len, of);
+            store_chunk<T, kThreads, 1, 0>(out + from, raw, len, a.stream_out, of);
         });
 }
 
@@ -606,7 +673,7 @@ __global__ __launch_bounds__(kThreads) void distill_forward(float *__restrict__ 
         for (int u = 0; u < 2; ++u)
             if (e.token[u] >= 0) at[u] = widen1(z[e.token[u]]);
     }
-    const Lse v = take_row<T, kThreads>(z, a.vocab, a.inv_t * kLog2e);
+    const Lse v = take_row<T, kThreads>(z, a.vocab, a.inv_t * kLog2e, a.stream_in, step_back(z, row));
     const float lse = lse_value(block_lse<kThreads>(v, a.inv_t * kLog2e, lse_scratch), a.inv_t);
     if (threadIdx.x < kWave) {
         const float l = list_loss(e, at, lse, a);
@@ -682,8 +749,8 @@ __global__ __launch_bounds__(kThreads) void distill_gradient(T *dlogits, const f
         }
     }
     __syncthreads();
-    if (e.any) write_row<T, kThreads>(out, z, lo, hi, [&](float x) { return w * __builtin_amdgcn_exp2f(fmaf(x, a.inv_t, -lse) * kLog2e); });
-    else write_row<T, kThreads>(out, z, lo, hi, [](float) { return 0.f; });
+    if (e.any) write_row<T, kThreads>(out, z, lo, hi, a, [&](float x) { return w * __builtin_amdgcn_exp2f(fmaf(x, a.inv_t, -lse) * kLog2e); });
+    else write_row<T, kThreads>(out, z, lo, hi, a, [](float) { return 0.f; });
     __syncthreads();
     if (threadIdx.x < kWave) {
 #pragma unroll
@@ -699,7 +766,7 @@ __global__ __launch_bounds__(kThreads) void distill_gradient(T *dlogits, const f
 // any length, read a second time for the gradient.
 // The first kSure slabs are known to lie inside the row.
 template <typename T, int kThreads, int kVecs, int kSure>
-__global__ __launch_bounds__(kThreads, (kThreads <= 512 ? DBW : 4)) void distill_both(float *__restrict__ loss, T *dlogits, const float *__restrict__ dloss,
+__global__ __launch_bounds__(kThreads, (kThreads <= 512 ? 6 : 4)) void distill_both(float *__restrict__ loss, T *dlogits, const float *__restrict__ dloss,
                                                          const T *logits, const int32_t *__restrict__ idx, const float *__restrict__ val,
                                                          DistillArgs a)
 {
@@ -719,7 +786,7 @@ __global__ __launch_bounds__(kThreads, (kThreads <= 512 ? DBW : 4)) void distill
     v4u raw[kHeld];
     if constexpr (kVecs > 0) {
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r) raw[r] = load_slab<T, kThreads>(z, r * kThreads * E, tid, (int)a.vocab, (int)a.vocab, r < kSure);
+        for (int r = 0; r < kHeld; ++r) raw[r] = load_slab<T, kThreads>(z, r * kThreads * E, tid, (int)a.vocab, (int)a.vocab, r < kSure, a.stream_in);
     }
     // The first wavefront sees to the list while the row is on its way, and puts it by: beside a row the registers are taken.
     __shared__ int32_t kept_token[2][kWave];
@@ -741,7 +808,7 @@ __global__ __launch_bounds__(kThreads, (kThreads <= 512 ? DBW : 4)) void distill
         for (int r = 0; r < kHeld; ++r) settle_slab<T, kThreads>(raw[r], r * kThreads * E, tid, (int)a.vocab, (int)a.vocab, kNegInfBits<T>, r < kSure);
         take<T, kHeld>(v, raw, unit);
     } else {
-        v = take_row<T, kThreads>(z, a.vocab, unit);
+        v = take_row<T, kThreads>(z, a.vocab, unit, false, 0);
     }
     v = block_lse<kThreads>(v, unit, lse_scratch);                         // (its barriers order the list's reads before the writes below)
     const bool any = any_lds != 0;
@@ -754,13 +821,13 @@ __global__ __launch_bounds__(kThreads, (kThreads <= 512 ? DBW : 4)) void distill
     if constexpr (kVecs > 0) {
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) rewiden(raw[r]);
-        if (any && plain) store_chunk<T, kThreads, kHeld, kSure>(out, raw, (int)a.vocab, usual);
-        else if (any) write_row<T, kThreads>(out, z, 0, a.vocab, wide);
-        else write_row<T, kThreads>(out, z, 0, a.vocab, none);
+        if (any && plain) store_chunk<T, kThreads, kHeld, kSure>(out, raw, (int)a.vocab, a.stream_out, usual);
+        else if (any) write_row<T, kThreads>(out, z, 0, a.vocab, a, wide);
+        else write_row<T, kThreads>(out, z, 0, a.vocab, a, none);
     } else {
-        if (any && plain) write_row<T, kThreads>(out, z, 0, a.vocab, usual);
-        else if (any) write_row<T, kThreads>(out, z, 0, a.vocab, wide);
-        else write_row<T, kThreads>(out, z, 0, a.vocab, none);
+        if (any && plain) write_row<T, kThreads>(out, z, 0, a.vocab, a, usual);
+        else if (any) write_row<T, kThreads>(out, z, 0, a.vocab, a, wide);
+        else write_row<T, kThreads>(out, z, 0, a.vocab, a, none);
     }
     __syncthreads();                                                       // the row is written before its listed tokens are
     if (first) {
