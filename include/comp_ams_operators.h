@@ -74,7 +74,7 @@ int comp_ams_layer_norm_work_bytes(int64_t rows, int64_t cols, int32_t n, uint64
  *   1 <= n_buckets <= COMP_AMS_MAX_BUCKETS.  table: fp32 [n_buckets][heads].  key_len: int32 [batch], values outside
  *   [0, tk] count as the nearer end.
  * s_strides, p_strides: host arrays of three strides, {batch, head, query}.  batch, heads, tq, tk >= 0 with
- * tk < 2^31, batch heads tq < 2^31; |offset| < 2^31.  p may be s itself with the same strides.
+ * tk < 2^31, tq < 2^30, batch heads tq < 2^31; |offset| < 2^31.  p may be s itself with the same strides.
  */
 int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const int32_t *bounds_host, int32_t n_buckets,
                               const int32_t *key_len, int64_t batch, int64_t heads, int64_t tq, int64_t tk,

@@ -16,21 +16,6 @@ using namespace cams_ops;
 
 namespace {
 
-#ifndef NORM_BLOCKS
-#define NORM_BLOCKS 2048
-#endif
-#ifndef NORM_CHUNKS
-#define NORM_CHUNKS 1024
-#endif
-#ifndef BIAS_BLOCKS
-#define BIAS_BLOCKS 6400
-#endif
-#ifndef BIAS_FBLOCKS
-#define BIAS_FBLOCKS 1536
-#endif
-#ifndef T64
-#define T64 128
-#endif
 thread_local char g_error[512] = "";
 
 int fail(int code, const char *fmt, ...)
@@ -86,8 +71,8 @@ void with_type(int32_t type, F &&f)
 
 // Whether an array that a call reads or writes once is streamed past the caches.  What is written is read by the model's next
 // operation, if anything of it is left in the 256 MB memory-side cache by then; what is read was written by the one before.
-bool streamed_out(int64_t elements, int32_t type) { return elements * (int64_t)type_size(type) > (int64_t)80 << 20; }
-bool streamed_in(int64_t elements, int32_t type) { return elements * (int64_t)type_size(type) > (int64_t)256 << 20; }
+bool streamed_out(int64_t elements, int32_t type) { return elements > ((int64_t)80 << 20) / (int64_t)type_size(type); }
+bool streamed_in(int64_t elements, int32_t type) { return elements > ((int64_t)256 << 20) / (int64_t)type_size(type); }
 
 // --- constants chosen from sizes, as types ---------------------------------------------------------------------------
 
@@ -133,7 +118,12 @@ int norm_check(const char *what, int64_t rows, int64_t cols, int32_t type)
     return COMP_AMS_OK;
 }
 
-constexpr int64_t kNormBlocks = NORM_BLOCKS;
+// Workgroups of the forward pass: enough to fill the chip, few enough that a team keeps gain and shift in registers over several rows.
+// 16384 x 768 bf16, us: 1024 13.4, 2048 13.5, 4096 and 8192 (a row a team) 18.
+constexpr int64_t kNormBlocks = 2048;
+// Workgroups that the rows of all workers are cut into in the backward pass.  More keep more rows in flight, and write more partial
+// sums.  us at 512 / 768 / 1024 / 1280: 16384 x 768 bf16, n = 8 20.7 / 21.3 / 19.6 / 19.7; 20000 x 2047 fp32, n = 20 125 / 118 / 115 / 121.
+constexpr int64_t kNormChunkBlocks = 1024;
 
 // How a worker's rows are cut for the parameter gradients: chunks of rows with one set of column sums each.
 struct NormChunks {
@@ -141,7 +131,7 @@ struct NormChunks {
 };
 NormChunks norm_chunks(int64_t worker_rows, int32_t n)
 {
-    const int64_t want = std::max<int64_t>(1, ceil_div(NORM_CHUNKS, n));
+    const int64_t want = std::max<int64_t>(1, ceil_div(kNormChunkBlocks, n));
     const int64_t rows = std::max<int64_t>(16, ceil_div(worker_rows, want));
     return {rows, std::max<int64_t>(1, ceil_div(worker_rows, rows))};
 }
@@ -158,7 +148,7 @@ int bias_check(const char *what, const int32_t *bounds, int32_t n_buckets, const
     REQUIRE(batch >= 0 && heads >= 0 && tq >= 0 && tk >= 0, "%s: a size is negative", what);
     REQUIRE(tk < (int64_t)1 << 31, "%s: tk=%lld must be below 2^31", what, (long long)tk);
     const int64_t most = (int64_t)1 << 31;
-    REQUIRE(batch < most && heads < most && tq < most, "%s: a size is out of range", what);
+    REQUIRE(batch < most && heads < most && tq < most / 2, "%s: a size is out of range", what);
     if (batch && heads && tq)
         REQUIRE(batch * heads < most && batch * heads * tq < most, "%s: batch*heads*tq must be below 2^31", what);
     REQUIRE(offset > -most && offset < most, "%s: offset out of range", what);
@@ -187,20 +177,28 @@ int bias_strides(const char *what, const char *name, const void *p, int64_t batc
     return COMP_AMS_OK;
 }
 
+// Workgroups of the forward pass, each with its own layout of a head's bias in LDS.  16 x 12 x 512 x 512 bf16, us: 768 59, 1024 51,
+// 1536 41, 3072 45 (without streamed stores).
+constexpr int64_t kBiasForwardBlocks = 1536;
+
 // How the queries of a head and sequence are cut for the backward pass: the registers' form takes rows_team consecutive queries a team.
 struct BiasShape {
     bool held;               // false: bias_backward_any
     int32_t team, rows_team, rows_block;
     int64_t pieces;
 };
+// A wavefront takes a row of up to 128 vectors, a workgroup longer ones: by the wavefront, four teams' arrays over the positions leave room
+// for three workgroups a compute unit (2 x 16 x 1999 x 1999 f16 causal: 194 us against 136).
+// The rows a team takes: as many as leave kBiasBackwardBlocks workgroups, between a step's and 32.  us at 16 x 12 x 512 x 512 bf16 / the
+// causal case: at least 640 workgroups 59 / 136, 1600 53 / 136, 3200 49 / 121, 6400 47 / 113.
+constexpr int64_t kBiasBackwardBlocks = 6400;
 BiasShape bias_backward_shape(int64_t sequences, int64_t tq, int64_t tk, int32_t type)
 {
     const int64_t e = 16 / (int64_t)type_size(type), vecs = ceil_div(std::max<int64_t>(tk, 1), e);
     if (tk < e || vecs > 1024) return {false, 0, kBiasAnyRows, kBiasAnyRows, ceil_div(tq, kBiasAnyRows)};
-    const int32_t team = vecs <= 32 ? 16 : vecs <= T64 ? 64 : 256, teams = kTeamBlock<256> / team;
-    // as many rows as leave about kBiasBlocks workgroups, between a step's and 32
+    const int32_t team = vecs <= 32 ? 16 : vecs <= 128 ? 64 : 256, teams = kTeamBlock<256> / team;
     int32_t rows = 32;
-    while (rows > e && sequences * ceil_div(tq, rows * teams) < BIAS_BLOCKS) rows /= 2;
+    while (rows > e && sequences * ceil_div(tq, rows * teams) < kBiasBackwardBlocks) rows /= 2;
     return {true, team, rows, rows * teams, ceil_div(tq, rows * teams)};
 }
 
@@ -375,7 +373,8 @@ int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const 
             using S = decltype(shape);
             if constexpr (S::threads <= 256) {
                 constexpr int kTeams = kTeamBlock<S::threads> / S::threads;
-                const int rows_block = (int)std::min<int64_t>(tq, std::min<int64_t>(256, std::max<int64_t>(1, ceil_div(a.rows, (int64_t)BIAS_FBLOCKS * kTeams)) * kTeams));
+                const int64_t share = std::max<int64_t>(1, ceil_div(a.rows, kBiasForwardBlocks * kTeams)) * kTeams;
+                const int rows_block = (int)std::min<int64_t>(tq, std::min<int64_t>(256, share));
                 const int64_t pieces = ceil_div(tq, rows_block);
                 const size_t lds = (size_t)(tk + rows_block - 1) * sizeof(float);
                 bias_forward<T, S::threads, S::vecs><<<(unsigned)(batch * heads * pieces), kTeamBlock<S::threads>, lds,
