@@ -51,7 +51,7 @@ int comp_ams_layer_norm(void *y, float *mean, float *rstd, const void *x, const 
  * Its backward pass.  With xh = (x - mean) rstd and a = dy gain:
  *   dx = rstd (a - (1/cols) sum a - xh (1/cols) sum a xh)           per row
  *   dgain[w] = sum dy xh,  dshift[w] = sum dy                        over the rows of worker w
- * Worker w of n holds the rows [w rows/n, (w + 1) rows/n); rows must be a multiple of n.  dgain and dshift point at
+ * Worker w of n (1 <= n <= 65535) holds the rows [w rows/n, (w + 1) rows/n); rows must be a multiple of n.  dgain and dshift point at
  * the parameter's place in worker 0's row; the next worker's is grad_stride elements further.  dshift may be NULL.
  * dx may be dy or x itself with the same stride.  With rows = 0 the parameter gradients are zero.
  * work: comp_ams_layer_norm_work_bytes() bytes of device memory, 16-byte aligned, not kept from one call to the next.

@@ -1,4 +1,13 @@
 // Layer norm, forward and backward, with the gradients of gain and shift reduced per worker.
+//
+//   mean = (1/c) sum x,  rstd = 1/sqrt((1/c) sum (x - mean)^2 + eps),  y = (x - mean) rstd gain + shift
+//   xh = (x - mean) rstd,  a = dy gain:  dx = rstd (a - mean(a) - xh mean(a xh)),  dgain = sum dy xh,  dshift = sum dy
+//
+// HBM-bound: a row is read once and kept in registers, the variance is taken from the differences (no cancellation), and a lane keeps
+// its columns' gradient sums in registers over all rows of its chunk, so that x and dy are read once for dx and both parameter
+// gradients.  Measured (us, and TB/s of what a pass cannot do without): forward 16384 x 768 bf16 13.5 (3.7; 50 MB, half of it in the
+// memory-side cache), backward 19.3 with the join of the chunks (3.9); backward 20000 x 2047 fp32, n = 20 112 (4.4), of which the join 8.
+// A copy reaches 6.1 TB/s.  One kernel per chunk of rows and a join in fixed order instead of atomics: results never vary.
 #pragma once
 #include "op_common.h"
 

@@ -1,4 +1,14 @@
 // Rows over a vocabulary: log probabilities of tokens with entropy and alternatives, and distillation from top lists.
+//
+//   lse = log sum exp(z / T);  logp = z_t - lse;  entropy = lse - sum p z
+//   q = softmax(val / T) over the list;  loss = T^2 sum q (log q - (z / T - lse));  dz = dloss T (exp(z / T - lse) - q)
+//
+// HBM-bound, with vector instructions close behind where logits have 16 bits: an element costs 8.5 issue slots (widening, maximum,
+// fused multiply-add, exponential (two), sum, moment) where HBM leaves about 13.  So rows are read once and held in registers between
+// the passes over them, and exponentials are taken as 2^(z log2(e) / T - c) with one fused multiply-add.
+// Measured (us, TB/s of what a pass cannot do without; a copy reaches 6.1, reading alone 6.2): log probabilities with 32
+// alternatives 4096 x 100000 bf16 179 (4.6), of which their selection 17 and the join of four pieces 14; loss and gradient 4096 x 32768
+// bf16 107 (5.0); loss 2048 x 50001 f16 41 (5.0); gradient 1024 x 131072 fp32 190 (5.6).
 #pragma once
 #include "op_common.h"
 #include "../../../include/comp_ams_operators.h"

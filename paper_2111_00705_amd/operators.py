@@ -74,8 +74,11 @@ def _stream(like, *tensors):
 
 def _rows(t, what):
     """(rows, columns, row stride) of a tensor [..., columns] whose rows are evenly spaced and dense."""
-    _need(t.dim() >= 1, f"{what} needs at least one dimension")
-    cols = t.shape[-1]
+    shape = t.shape
+    _need(len(shape) >= 1, f"{what} needs at least one dimension")
+    cols = shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // cols if cols else 0), cols, max(cols, 1)
     _need(t.stride(-1) == 1 or cols <= 1, f"the last dimension of {what} must be dense")
     if t.dim() == 1:
         return 1, cols, cols
@@ -107,15 +110,21 @@ def _like(out, t, what):
     return out
 
 
-def _work(fn, device, *args):
-    """(work tensor or None, pointer, bytes) for the size that the library asks for."""
-    import torch
+@functools.lru_cache(maxsize=4096)
+def _work_bytes(name, *args):
     need = C.c_uint64(0)
-    _check(fn(*args, C.byref(need)))
-    if need.value == 0:
+    _check(getattr(lib(), name)(*args, C.byref(need)))
+    return need.value
+
+
+def _work(name, device, *args):
+    """(work tensor or None, pointer, bytes) for the size that the library asks for."""
+    need = _work_bytes(name, *args)
+    if need == 0:
         return None, None, 0
-    w = torch.empty(need.value, dtype=torch.uint8, device=device)
-    return w, w.data_ptr(), need.value
+    import torch
+    w = torch.empty(need, dtype=torch.uint8, device=device)
+    return w, w.data_ptr(), need
 
 
 def _param_grad(t, shape, what):
@@ -168,7 +177,7 @@ def layer_norm_backward(dy, x, mean, rstd, gain, dgain, dshift=None, out=None):
     dx = _like(out, x, "out")
     _, _, dx_stride = _rows(dx, "out")
     L = lib()
-    work, work_ptr, work_bytes = _work(L.comp_ams_layer_norm_work_bytes, x.device, rows, cols, n)
+    work, work_ptr, work_bytes = _work("comp_ams_layer_norm_work_bytes", x.device, rows, cols, n)
     _check(L.comp_ams_layer_norm_backward(dx.data_ptr(), dgain.data_ptr(), None if dshift is None else dshift.data_ptr(), dy.data_ptr(),
                                           x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), gain.data_ptr(), rows, cols, dx_stride,
                                           dy_stride, x_stride, n, stride, _type(x), _type(dgain), work_ptr, work_bytes, s))
@@ -194,7 +203,10 @@ def rel_bias_bounds(buckets, distance, causal=False):
 
 
 def _bounds(bounds):
-    b = np.ascontiguousarray(bounds, dtype=np.int32)
+    if type(bounds) is np.ndarray and bounds.dtype == np.int32 and bounds.flags.c_contiguous:
+        b = bounds
+    else:
+        b = np.ascontiguousarray(bounds, dtype=np.int32)
     _need(b.ndim == 1, "bounds must be one-dimensional")
     return b
 
@@ -240,7 +252,6 @@ def rel_bias_softmax_backward(dprobs, probs, bounds, dtable, scale=1.0, causal=F
     """Backward pass of rel_bias_softmax from the probabilities it returned: returns the gradient of the scores and writes
     dtable [n, buckets, heads] (a view of the optimiser's gradient buffer, of its type), worker w's from the w-th of n equal parts
     of the batch.  Keys of probability zero take no gradient.  out may be dprobs."""
-    import torch
     dp_strides, p_strides = _scores(dprobs, "dprobs"), _scores(probs, "probs")
     _need(dprobs.shape == probs.shape and dprobs.dtype == probs.dtype, "dprobs must have the shape and type of probs")
     batch, heads, tq, tk = probs.shape
@@ -250,7 +261,7 @@ def rel_bias_softmax_backward(dprobs, probs, bounds, dtable, scale=1.0, causal=F
     ds = _like(out, dprobs, "out")
     ds_strides = _scores(ds, "out")
     L, kind = lib(), _type(probs)
-    work, work_ptr, work_bytes = _work(L.comp_ams_rel_bias_work_bytes, probs.device, batch, heads, tq, tk, b.size + 1, kind)
+    work, work_ptr, work_bytes = _work("comp_ams_rel_bias_work_bytes", probs.device, batch, heads, tq, tk, b.size + 1, kind)
     _check(L.comp_ams_rel_bias_softmax_backward(ds.data_ptr(), dtable.data_ptr(), dprobs.data_ptr(), probs.data_ptr(), b.ctypes.data,
                                                 b.size + 1, _lengths(key_lengths, batch), batch, heads, tq, tk,
                                                 (C.c_int64 * 9)(*ds_strides, *dp_strides, *p_strides), offset, scale, 1 if causal else 0,
@@ -274,7 +285,7 @@ def token_logprobs(logits, tokens=None, k=0):
     top = torch.empty((rows, k), **f32)
     idx = torch.empty_like(top, dtype=torch.int32)
     L, kind = lib(), _type(logits)
-    work, work_ptr, work_bytes = _work(L.comp_ams_token_logprobs_work_bytes, logits.device, rows, vocab, k, kind)
+    work, work_ptr, work_bytes = _work("comp_ams_token_logprobs_work_bytes", logits.device, rows, vocab, k, kind)
     _check(L.comp_ams_token_logprobs(None if logp is None else logp.data_ptr(), entropy.data_ptr(), idx.data_ptr(), top.data_ptr(),
                                      logits.data_ptr(), None if tokens is None else tokens.data_ptr(), rows, vocab, stride, k, kind,
                                      work_ptr, work_bytes, s))
