@@ -165,7 +165,8 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_forward(T *p, const T 
     __shared__ int32_t at[COMP_AMS_MAX_BUCKETS];
     __shared__ float of_bucket[COMP_AMS_MAX_BUCKETS];
     const Team<kTeam> me;
-    const unsigned bh = blockIdx.x / (unsigned)pieces, piece = blockIdx.x % (unsigned)pieces;
+    // with a causal mask the last queries see most: they are taken first
+    const unsigned bh = blockIdx.x / (unsigned)pieces, turn_of = blockIdx.x % (unsigned)pieces, piece = a.causal ? pieces - 1 - turn_of : turn_of;
     const int64_t b = bh / (unsigned)a.heads, h = bh % (unsigned)a.heads;
     const int tk = (int)a.tk, i0 = (int)piece * rows_block, i1 = min(i0 + rows_block, (int)a.tq);
     const int64_t by_length = key_len ? min((int64_t)max(key_len[b], 0), a.tk) : a.tk;

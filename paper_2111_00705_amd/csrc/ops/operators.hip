@@ -177,9 +177,11 @@ int bias_strides(const char *what, const char *name, const void *p, int64_t batc
     return COMP_AMS_OK;
 }
 
-// Workgroups of the forward pass, each with its own layout of a head's bias in LDS.  16 x 12 x 512 x 512 bf16, us: 768 59, 1024 51,
-// 1536 41, 3072 45 (without streamed stores).
-constexpr int64_t kBiasForwardBlocks = 1536;
+// Workgroups of the forward pass, each with its own layout of a head's bias in LDS: more of them hide each other's latency, fewer lay out
+// less.  us at 1536 / 2048 / 3072: wavefronts over many rows 16 x 12 x 512 x 512 bf16 44 / 41 / 40, 8 x 12 x 1024 x 1024 100 / 100 / 90;
+// over few 8 x 8 x 300 x 300 12.3 / 12.3 / 13.6; teams of 16 lanes 64 x 8 x 128 x 128 10.0 / 11.1 / 11.3; workgroups 2 x 16 x 2000 x 2000
+// f16 120 / 144 / 126.
+int64_t bias_forward_blocks(int team, int64_t rows) { return team == 64 && rows >= 65536 ? 3072 : 1536; }
 
 // How the queries of a head and sequence are cut for the backward pass: the registers' form takes rows_team consecutive queries a team.
 struct BiasShape {
@@ -369,20 +371,25 @@ int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const 
     a.offset = offset, a.scale = scale, a.causal = causal != 0, a.stream_out = streamed_out(a.rows * tk, type);
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        const bool held = tk <= 1024 * kVec<T> && with_team<T>(tk, [&](auto shape) {
+        const int64_t vecs = ceil_div(tk, kVec<T>);
+        auto launch = [&](auto shape) {
             using S = decltype(shape);
-            if constexpr (S::threads <= 256) {
-                constexpr int kTeams = kTeamBlock<S::threads> / S::threads;
-                const int64_t share = std::max<int64_t>(1, ceil_div(a.rows, kBiasForwardBlocks * kTeams)) * kTeams;
-                const int rows_block = (int)std::min<int64_t>(tq, std::min<int64_t>(256, share));
-                const int64_t pieces = ceil_div(tq, rows_block);
-                const size_t lds = (size_t)(tk + rows_block - 1) * sizeof(float);
-                bias_forward<T, S::threads, S::vecs><<<(unsigned)(batch * heads * pieces), kTeamBlock<S::threads>, lds,
-                                                      static_cast<hipStream_t>(hip_stream)>>>(
-                    static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a, (int)pieces, rows_block);
-            }
-        });
-        if (held) return;
+            constexpr int kTeams = kTeamBlock<S::threads> / S::threads;
+            const int64_t share = std::max<int64_t>(1, ceil_div(a.rows, bias_forward_blocks(S::threads, a.rows) * kTeams)) * kTeams;
+            const int rows_block = (int)std::min<int64_t>(tq, std::min<int64_t>(256, share));
+            const int64_t pieces = ceil_div(tq, rows_block);
+            const size_t lds = (size_t)(tk + rows_block - 1) * sizeof(float);
+            bias_forward<T, S::threads, S::vecs><<<(unsigned)(batch * heads * pieces), kTeamBlock<S::threads>, lds,
+                                                  static_cast<hipStream_t>(hip_stream)>>>(
+                static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a, (int)pieces, rows_block);
+        };
+        // rows of more than 128 vectors by a workgroup: by a wavefront they take 150 registers (2 x 16 x 2000 x 2000 f16 172 us against 119)
+        if (tk >= kVec<T> && vecs <= 1024) {
+            if (vecs <= 32) with_vecs<16, 1, 2>((int)ceil_div(vecs, 16), launch);
+            else if (vecs <= 128) with_vecs<64, 1, 2>((int)ceil_div(vecs, 64), launch);
+            else with_vecs<256, 1, 4>((int)ceil_div(vecs, 256), launch);
+            return;
+        }
         bias_forward_any<T><<<(unsigned)a.rows, kBiasThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
             static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a);
     });
