@@ -226,10 +226,11 @@ __device__ __forceinline__ uint32_t kth_largest(const float *values, int groups,
 // elements that do are listed, and the list is ranked by counting.
 // A piece is longer than kVecs - 2 slabs (the shape's rule; the last one is shorter than the others by less than a slab).
 // With one piece per row the results are final; with more, statistics and keys go to work and logprobs_join follows.
+constexpr int kPieceThreads = 512, kPieceVecs = 8;
 constexpr int kMaxQueued = 256;           // vectors that reach the bound; more than that (rows of ties) are told apart by select_slow
 
 template <typename T, int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads, 8) void logprobs_regs(float *__restrict__ logp, float *__restrict__ entropy,
+__global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void logprobs_regs(float *__restrict__ logp, float *__restrict__ entropy,
                                                           int32_t *__restrict__ top_idx, float *__restrict__ top_logp,
                                                           const T *__restrict__ logits, const int64_t *__restrict__ tokens,
                                                           int64_t vocab, int64_t stride, int k, int groups, int n_pieces,
