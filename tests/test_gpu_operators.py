@@ -597,3 +597,61 @@ def test_a_raw_stream_of_the_callers():
     for a, b in ((y, want[0]), (mean, want[1]), (dx, want[3]), (grads[:, :192], want[4][:, :192]), (idx, want[9]), (top, want[10]), (loss, want[14]),
                  (dz, want[15])):
         assert R.same_bits(a, b)
+
+
+# --- every shape that holds a row in registers, at sizes that do not fill it ----------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [2050, 6001, 12_001, 16_000, 28_001, 40_001, 60_000, 120_001])
+def test_vocabulary_rows_of_every_register_shape(vocab, dtype):
+    print(f"[case] vocabulary shape {vocab} {dtype}", flush=True)
+    g = gen("vocabulary shape", vocab)
+    z = randn(g, 3, vocab, std=3.0).to(dtype)
+    check_logprobs(z, torch.randint(0, vocab, (3,), generator=g), 17, stride_pad=1)
+    idx, val = lists(g, 3, vocab, 9, False)
+    weight = torch.rand(3, generator=g) + 0.1
+    want = R.distill(z, idx, val, 2.0, weight)
+    zv, _ = strided(z, 1, 0)
+    loss, dz = P.distill_grad(zv, idx.cuda(), val.cuda(), weight.cuda(), temperature=2.0)
+    R.close(loss, want[0], want[3], "loss")
+    R.close(dz, want[2], want[5], "gradient")
+    assert R.same_bits(P.distill_grad(zv, idx.cuda(), val.cuda(), weight.cuda(), temperature=2.0, out=zv)[1], dz)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", [(1, 1, 9, 8, False, 0, None, 8), (2, 1, 20, 200, True, 180, [200, 77], 16), (1, 2, 9, 700, False, 3, None, 32),
+                                  (2, 1, 5, 1500, True, 1495, [1500, 1000], 32), (1, 1, 6, 3500, True, 3494, None, 32),
+                                  (1, 1, 5, 7001, False, 0, [6500], 32), (1, 1, 4, 8192, False, -9, None, 16)],
+                         ids=lambda c: "x".join(map(str, c[:4])))
+def test_score_rows_of_every_register_shape(case, dtype):
+    print(f"[case] score shape {case} {dtype}", flush=True)
+    b, h, tq, tk, causal, offset, lens, nb = case
+    g, s, bounds, table, ln = bias_inputs(case, dtype)
+    kw = dict(scale=0.25, causal=causal, offset=offset, key_lengths=None if ln is None else ln.cuda())
+    want, slack = R.bias_softmax(s, table, bounds, 0.25, causal, offset, lens)
+    p = P.rel_bias_softmax(s.cuda(), table.cuda(), bounds, **kw)
+    R.close(p, want, slack, "p")
+    dp = randn(g, b, h, tq, tk, std=0.5).to(dtype)
+    back = R.bias_softmax_backward(dp, p.cpu(), bounds, 0.25, causal, offset, lens, 1)
+    dtable = torch.zeros(1, nb, h, device="cuda")
+    ds = P.rel_bias_softmax_backward(dp.cuda(), p, bounds, dtable, **kw)
+    R.close(ds, back[0], back[2], "ds")
+    R.close(dtable, back[1], back[3], "dtable")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [20, 200, 400, 1100, 1600, 3001, 5000, 6500, 12_000])
+def test_norm_rows_of_every_register_shape(cols, dtype):
+    print(f"[case] norm shape {cols} {dtype}", flush=True)
+    g = gen("norm shape", cols)
+    x, dy = randn(g, 70, cols).to(dtype), randn(g, 70, cols, std=0.3).to(dtype)
+    gain = randn(g, cols) + 0.5
+    y, mean, rstd = P.layer_norm(x.cuda(), gain.cuda())
+    want = R.norm(x, gain, None, 1e-5)
+    R.close(y, want[0], R.norm_slack(x, gain, None, want[1], want[2])[0], "y")
+    back = R.norm_backward(dy, x, mean.cpu(), rstd.cpu(), gain, 2)
+    grads = torch.zeros(2, 2 * cols, device="cuda")
+    dx = P.layer_norm_backward(dy.cuda(), x.cuda(), mean, rstd, gain.cuda(), grads[:, :cols], grads[:, cols:])
+    R.close(dx, back[0], back[3], "dx")
+    R.close(grads[:, :cols], back[1], back[4], "dgain")
+    R.close(grads[:, cols:], back[2], back[5], "dshift")
