@@ -314,8 +314,15 @@ __device__ __forceinline__ Lse lse_join(const Lse &a, const Lse &b, float unit)
     return {top, a.sum * fa + b.sum * fb};
 }
 
-// Below this size of a maximum, distances to it may be formed from products with log2 e (and 1 / T up to 2^20): nothing leaves fp32.
+// Scores in units of log 2 below this size leave room for their distances within fp32.
 constexpr float kPlainMax = 1e31f;
+
+// A distance to the maximum, (x - top) unit, costs one instruction as fma(x, unit, -c) with c = top unit rounded to fp32.  Every such distance is
+// off by the same top unit - c, at most 1/2 while |c| < 2^24: sums of 2^distance are multiplied by kept_back() afterwards.  Beyond that (logits
+// masked with a large finite number, as far as some lanes see nothing else) it would leave fp32, and x - top is formed first.
+constexpr float kPlainProduct = 16777216.f;
+__device__ __forceinline__ bool plain_product(float c) { return fabsf(c) < kPlainProduct; }        // false for a NaN
+__device__ __forceinline__ float kept_back(float top, float unit, float c) { return __builtin_amdgcn_exp2f(fmaf(-top, unit, c)); }
 
 // log sum exp(z / T) of a row, or NaN where the row has no distribution: nothing but -infinity, or a +infinity.
 __device__ __forceinline__ float lse_value(const Lse &v, float inv_t)

@@ -276,10 +276,10 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
     }
     if (tid == 0) count = queued = strange = 0;
     const float m = team_reduce<MaxOp, kThreads>(top, scratch);
-    // exp(x - m) as 2^(x log2 e - c): the same rounding of c = m log2 e in every term and in the moment, and taken back in lse
     const float c = m * kLog2e;
+    const bool plain = plain_product(c);
     float s = 0.f, w = 0.f;
-    if (fabsf(m) < kPlainMax) {
+    if (plain) {
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
             rewiden(raw[v]);
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
         }
     } else {
 #pragma unroll 1
-        for (int q = tid + back; q < len; q += kThreads) {     // infinities, or nothing but -infinity and NaN, or near the end of fp32's range
+        for (int q = tid + back; q < len; q += kThreads) {     // infinities, or nothing but -infinity and NaN, or large finite masks
             const float x = widen1(z[q]), d = (x - m) * kLog2e, e = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
             s += e;
             w = fmaf(e, fmaxf(d, -1e30f), w);
@@ -317,8 +317,13 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
     const bool whole = n_pieces == 1;
     if (wave == 0) {
         const int q = tid & 15;
-        const Piece piece = {m, lanes_reduce<SumOp, 16>(q < kWaves ? sum_of[q] : 0.f),
-                             lanes_reduce<SumOp, 16>(q < kWaves ? moment_of[q] : 0.f)};
+        Piece piece = {m, lanes_reduce<SumOp, 16>(q < kWaves ? sum_of[q] : 0.f),
+                       lanes_reduce<SumOp, 16>(q < kWaves ? moment_of[q] : 0.f)};
+        if (plain) {                                    // the moment's distances are off by the same number
+            const float f = kept_back(m, kLog2e, c);
+            piece.sum *= f;
+            piece.moment = fmaf(fmaf(-m, kLog2e, c), piece.sum, piece.moment * f);
+        }
         if (tid == 0 && !whole) pieces[blockIdx.x] = piece;
         if (tid == 0 && whole) {
             const float lse = piece_lse(piece);
@@ -536,8 +541,7 @@ __device__ __forceinline__ void merge_list(Listed &e, int k)
     }
 }
 
-// kVecs vectors of this thread taken into its running maximum and sum.  The sum is in terms of 2^(z unit - c), c = top * unit rounded
-// once, as long as the maxima are of ordinary size.
+// kVecs vectors of this thread taken into its running maximum and sum.
 template <typename T, int kVecs>
 __device__ __forceinline__ void take(Lse &v, v4u (&raw)[kVecs], float unit)
 {
@@ -555,14 +559,16 @@ __device__ __forceinline__ void take(Lse &v, v4u (&raw)[kVecs], float unit)
     float s = v.sum * __builtin_amdgcn_exp2f((v.top - from) * unit);
 #pragma unroll
     for (int r = 0; r < kVecs; ++r) rewiden(raw[r]);
-    if (__all(fabsf(from) < kPlainMax)) {
+    if (__all(plain_product(c))) {
+        float part = 0.f;
 #pragma unroll
         for (int r = 0; r < kVecs; ++r) {
             float x[E];
             widen<T>(raw[r], x);
 #pragma unroll
-            for (int q = 0; q < E; ++q) s += __builtin_amdgcn_exp2f(fmaf(x[q], unit, -c));
+            for (int q = 0; q < E; ++q) part += __builtin_amdgcn_exp2f(fmaf(x[q], unit, -c));
         }
+        s = fmaf(part, kept_back(from, unit, c), s);
     } else {
 #pragma unroll
         for (int r = 0; r < kVecs; ++r) {
@@ -825,8 +831,9 @@ __global__ __launch_bounds__(kThreads, (kThreads <= 512 ? 6 : 4)) void distill_b
     const bool any = any_lds != 0;
     const float scale = w / v.sum;
     const float top = v.top, c = v.top * unit;
-    const bool plain = fabsf(top) < kPlainMax;
-    auto usual = [&](float x) { return scale * __builtin_amdgcn_exp2f(fmaf(x, unit, -c)); };
+    const bool plain = plain_product(c);
+    const float kept = scale * kept_back(top, unit, c);
+    auto usual = [&](float x) { return kept * __builtin_amdgcn_exp2f(fmaf(x, unit, -c)); };
     auto wide = [&](float x) { return scale * __builtin_amdgcn_exp2f((x - top) * unit); };
     auto none = [](float) { return 0.f; };
     if constexpr (kVecs > 0) {
