@@ -125,7 +125,9 @@ int comp_ams_token_logprobs_work_bytes(int64_t rows, int64_t vocab, int32_t k, i
  * A row whose list is empty has loss 0 and gradient 0.  Entries with val = -infinity are listed with q = 0.
  * idx: int32, val: fp32, dense [rows][k], 1 <= k <= COMP_AMS_MAX_TOP; 1 <= vocab < 2^31.
  *   comp_ams_distill           writes loss [rows] and lse [rows] (either may be NULL)
- *   comp_ams_distill_backward  writes dz [rows][vocab] from lse and dloss
+ *   comp_ams_distill_backward  writes dz [rows][vocab] from lse and dloss.  lse has been rounded to fp32, which the probabilities carry
+ *                              (|lse| 2^-24, relative): logits of 10^4 cost them three digits, and of rows beyond 2^24 - masked throughout
+ *                              with a large number - they are not known from it at all; comp_ams_distill_grad has no such limit
  *   comp_ams_distill_grad      both at once, for a loss whose weights (dloss) are known beforehand: one pass over the
  *                              logits; loss may be NULL
  * dlogits may be logits itself with the same stride.

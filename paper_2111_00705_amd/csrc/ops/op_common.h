@@ -324,10 +324,9 @@ constexpr float kPlainProduct = 16777216.f;
 __device__ __forceinline__ bool plain_product(float c) { return fabsf(c) < kPlainProduct; }        // false for a NaN
 __device__ __forceinline__ float kept_back(float top, float unit, float c) { return __builtin_amdgcn_exp2f(fmaf(-top, unit, c)); }
 
-// log sum exp(z / T) of a row, or NaN where the row has no distribution: nothing but -infinity, or a +infinity.
-__device__ __forceinline__ float lse_value(const Lse &v, float inv_t)
-{
-    return fabsf(v.top) == INFINITY ? NAN : fmaf(v.top, inv_t, logf(v.sum));
-}
+// log sum exp((z - top) / T) of a row, or NaN where the row has no distribution: nothing but -infinity, or a +infinity.  Log probabilities are
+// (z - top) / T - log_sum: lse = top / T + log_sum has lost what the size of top has no bits for.
+__device__ __forceinline__ float log_sum(float top, float sum) { return fabsf(top) == INFINITY ? NAN : logf(sum); }
+__device__ __forceinline__ float lse_value(const Lse &v, float inv_t) { return fmaf(v.top, inv_t, log_sum(v.top, v.sum)); }
 
 }  // namespace cams_ops

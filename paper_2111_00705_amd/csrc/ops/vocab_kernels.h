@@ -69,18 +69,18 @@ __global__ __launch_bounds__(kVocabThreads) void logprobs_any(float *__restrict_
         Lse v = {-INFINITY, 0.f};
         for (int64_t c = threadIdx.x; c < vocab; c += kVocabThreads) v = lse_join(v, {widen1(z[c]), 1.f}, kLog2e);
         v = block_lse<kVocabThreads>(v, kLog2e, lse_scratch);     // the entropy's barrier lies between two of these
-        const float lse = lse_value(v, 1.f);
-        float e = 0.f;
+        const float log_of = log_sum(v.top, v.sum);
+        float w = 0.f;
         for (int64_t c = threadIdx.x; c < vocab; c += kVocabThreads) {
-            const float zc = widen1(z[c]), p = __builtin_amdgcn_exp2f((zc - lse) * kLog2e);
-            if (p != 0.f) e = fmaf(p, lse - zc, e);
+            const float d = widen1(z[c]) - v.top, e = __builtin_amdgcn_exp2f(d * kLog2e);
+            if (e != 0.f) w = fmaf(e, d, w);
         }
-        e = team_reduce<SumOp, kVocabThreads>(e, scratch);      // block_lse's barriers lie between two of these
+        w = team_reduce<SumOp, kVocabThreads>(w, scratch);      // block_lse's barriers lie between two of these
         if (threadIdx.x == 0) {
-            if (entropy) entropy[row] = e;
+            if (entropy) entropy[row] = log_of - w / v.sum;
             if (logp) {
                 const int64_t t = tokens[row];
-                logp[row] = t >= 0 && t < vocab ? widen1(z[t]) - lse : 0.f;
+                logp[row] = t >= 0 && t < vocab ? (widen1(z[t]) - v.top) - log_of : 0.f;
             }
         }
         uint64_t last = ~0ull;
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kVocabThreads) void logprobs_any(float *__restrict_
             if (threadIdx.x == 0) {
                 const uint32_t t = ~(uint32_t)last;
                 top_idx[row * k + q] = (int32_t)t;
-                top_logp[row * k + q] = widen1(z[t]) - lse;
+                top_logp[row * k + q] = (widen1(z[t]) - v.top) - log_of;
             }
         }
     }
@@ -124,11 +124,7 @@ __device__ __forceinline__ Piece piece_join(const Piece &a, const Piece &b)
     return {top, a.sum * fa + b.sum * fb, ma + mb};
 }
 // NaN for a row of nothing but -infinity, or with a +infinity (or a NaN, which the sum shows).
-__device__ __forceinline__ float piece_lse(const Piece &p) { return fabsf(p.top) == INFINITY ? NAN : p.top + logf(p.sum); }
-__device__ __forceinline__ float piece_entropy(const Piece &p)
-{
-    return fabsf(p.top) == INFINITY ? NAN : logf(p.sum) - p.moment / p.sum * kLn2;
-}
+__device__ __forceinline__ float piece_entropy(const Piece &p) { return log_sum(p.top, p.sum) - p.moment / p.sum * kLn2; }
 
 constexpr int kMaxPieces = 32;            // of one row; longer vocabularies go to logprobs_any
 
@@ -242,7 +238,7 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
     __shared__ v4u queue[kMaxQueued];
     __shared__ int queue_at[kMaxQueued];
     __shared__ uint32_t count, queued, strange, bound_order;
-    __shared__ float lse_lds;
+    __shared__ float log_sum_lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int64_t row = blockIdx.x / (unsigned)n_pieces, begin = blockIdx.x % (unsigned)n_pieces * piece_len;
     // `back` elements before the row's first one take part in the loads and in nothing else; room: there is a place for one
@@ -326,12 +322,12 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
         }
         if (tid == 0 && !whole) pieces[blockIdx.x] = piece;
         if (tid == 0 && whole) {
-            const float lse = piece_lse(piece);
-            lse_lds = lse;
+            const float log_of = log_sum(m, piece.sum);
+            log_sum_lds = log_of;
             if (entropy) entropy[row] = piece_entropy(piece);
             if (logp) {
                 const int64_t t = tokens[row];
-                logp[row] = t >= 0 && t < vocab ? widen1(logits[row * stride + t]) - lse : 0.f;
+                logp[row] = t >= 0 && t < vocab ? (widen1(logits[row * stride + t]) - m) - log_of : 0.f;
             }
         }
     }
@@ -385,7 +381,7 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
     rank_keys<kThreads>(list, n, k, [&](uint64_t key, int rank) {
         if (whole) {
             top_idx[row * k + rank] = (int32_t)~(uint32_t)key;
-            top_logp[row * k + rank] = logit_of(key) - lse_lds;
+            top_logp[row * k + rank] = (logit_of(key) - m) - log_sum_lds;
         } else {
             keys[(int64_t)blockIdx.x * k + rank] = key;
         }
@@ -408,12 +404,12 @@ __global__ __launch_bounds__(kVocabThreads) void logprobs_join(float *__restrict
     for (int t = threadIdx.x; t < n; t += kVocabThreads) list[t] = keys[row * n + t];
     Piece p = pieces[row * n_pieces];
     for (int q = 1; q < n_pieces; ++q) p = piece_join(p, pieces[row * n_pieces + q]);
-    const float lse = piece_lse(p);
+    const float log_of = log_sum(p.top, p.sum);
     if (threadIdx.x == 0) {
         if (entropy) entropy[row] = piece_entropy(p);
         if (logp) {
             const int64_t t = tokens[row];
-            logp[row] = t >= 0 && t < vocab ? widen1(logits[row * stride + t]) - lse : 0.f;
+            logp[row] = t >= 0 && t < vocab ? (widen1(logits[row * stride + t]) - p.top) - log_of : 0.f;
         }
     }
     __syncthreads();
@@ -435,7 +431,7 @@ __global__ __launch_bounds__(kVocabThreads) void logprobs_join(float *__restrict
         }
         if (rank < k) {
             top_idx[row * k + rank] = (int32_t)~(uint32_t)key;
-            top_logp[row * k + rank] = logit_of(key) - lse;
+            top_logp[row * k + rank] = (logit_of(key) - p.top) - log_of;
         }
     }
 }
@@ -506,13 +502,14 @@ __device__ __forceinline__ Listed teacher_list(const RawList &r, const DistillAr
 }
 
 // T^2 sum q (log q - lp) of the row, by one wavefront.
-// z: the logits of the lane's entries.
-__device__ __forceinline__ float list_loss(const Listed &e, const float (&z)[2], float lse, const DistillArgs &a)
+// z: the logits of the lane's entries; v: the row's maximum and sum.
+__device__ __forceinline__ float list_loss(const Listed &e, const float (&z)[2], const Lse &v, const DistillArgs &a)
 {
+    const float log_of = log_sum(v.top, v.sum);
     float part = 0.f;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-        if (e.q[u] != 0.f) part += e.q[u] * (e.logq[u] - fmaf(z[u], a.inv_t, -lse));
+        if (e.q[u] != 0.f) part += e.q[u] * (e.logq[u] - fmaf(z[u] - v.top, a.inv_t, -log_of));
     return a.t * a.t * lanes_reduce<SumOp, kWave>(part);
 }
 
@@ -690,13 +687,13 @@ __global__ __launch_bounds__(kThreads) void distill_forward(float *__restrict__ 
         for (int u = 0; u < 2; ++u)
             if (e.token[u] >= 0) at[u] = widen1(z[e.token[u]]);
     }
-    const Lse v = take_row<T, kThreads>(z, a.vocab, a.inv_t * kLog2e, a.stream_in, step_back(z, row));
-    const float lse = lse_value(block_lse<kThreads>(v, a.inv_t * kLog2e, lse_scratch), a.inv_t);
+    Lse v = take_row<T, kThreads>(z, a.vocab, a.inv_t * kLog2e, a.stream_in, step_back(z, row));
+    v = block_lse<kThreads>(v, a.inv_t * kLog2e, lse_scratch);
     if (threadIdx.x < kWave) {
-        const float l = list_loss(e, at, lse, a);
+        const float l = list_loss(e, at, v, a);
         if (threadIdx.x == 0) {
             if (loss) loss[row] = e.any ? l : 0.f;
-            if (lse_out) lse_out[row] = lse;
+            if (lse_out) lse_out[row] = lse_value(v, a.inv_t);
         }
     }
 }
@@ -715,25 +712,25 @@ __global__ __launch_bounds__(kVocabThreads) void distill_any(float *__restrict__
     float listed[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) listed[u] = e.token[u] >= 0 ? widen1(z[e.token[u]]) : 0.f;
-    float lse;
+    Lse v = {-INFINITY, 0.f};
     if constexpr (kLoss) {
-        Lse v = {-INFINITY, 0.f};
         for (int c = 0; c < (int)a.vocab; ++c) v = lse_join(v, {widen1(z[c]), 1.f}, a.inv_t * kLog2e);
-        lse = lse_value(v, a.inv_t);
-        const float l = list_loss(e, listed, lse, a);
+        const float l = list_loss(e, listed, v, a);
         if (threadIdx.x == 0) {
             if (loss) loss[row] = e.any ? l : 0.f;
-            if (lse_out) lse_out[row] = lse;
+            if (lse_out) lse_out[row] = lse_value(v, a.inv_t);
         }
-    } else {
-        lse = lse_in[row];
     }
     if constexpr (kGrad) {
         T *out = dlogits + row * a.out_stride;
         const float w = dloss[row] * a.t;
         float p = 0.f, share = 0.f;
         const int lane = threadIdx.x;
-        if (lane < (int)a.vocab) p = __builtin_amdgcn_exp2f(fmaf(widen1(z[lane]), a.inv_t, -lse) * kLog2e);
+        if (lane < (int)a.vocab) {
+            const float x = widen1(z[lane]);
+            if constexpr (kLoss) p = __builtin_amdgcn_exp2f(fmaf(x - v.top, a.inv_t, -log_sum(v.top, v.sum)) * kLog2e);
+            else p = __builtin_amdgcn_exp2f(fmaf(x, a.inv_t, -lse_in[row]) * kLog2e);
+        }
         for (int t = 0; t < a.k; ++t) {
             const int32_t token = __builtin_amdgcn_readlane(t < kWave ? e.token[0] : e.token[1], t & (kWave - 1));
             const float q = lane_value(t < kWave ? e.q[0] : e.q[1], t & (kWave - 1));
@@ -858,7 +855,7 @@ __global__ __launch_bounds__(kThreads, (kThreads <= 512 ? 6 : 4)) void distill_b
             e.logq[u] = kept_logq[u][tid];
             listed[u] = kept_logit[u][tid];
         }
-        const float l = list_loss(e, listed, lse_value(v, a.inv_t), a);
+        const float l = list_loss(e, listed, v, a);
         if (tid == 0 && loss) loss[row] = any ? l : 0.f;
         merge_list(e, a.k);
 #pragma unroll

@@ -319,7 +319,8 @@ def distill(logits, idx, val, temperature=1.0):
 
 @_on_stream
 def distill_backward(dloss, logits, lse, idx, val, temperature=1.0, out=None):
-    """Gradient of the logits from the gradients dloss [rows] of distill's losses and the lse it returned.  out may be logits."""
+    """Gradient of the logits from the gradients dloss [rows] of distill's losses and the lse it returned, whose rounding to float32 the
+    probabilities carry: for rows of very large logits use distill_grad.  out may be logits."""
     import torch
     rows, vocab, stride, k = _teacher(logits, idx, val)
     _vector(dloss, rows, torch.float32, "dloss")

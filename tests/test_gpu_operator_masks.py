@@ -146,3 +146,46 @@ def test_gradients_and_entropies_of_rows_far_from_zero(vocab, offset):
     entropy = P.token_logprobs(z.cuda(), None, 0)[1]
     want = Want(z)
     R.close(entropy, want.entropy, want.s_sum[:, 0] * (2 + want.entropy), "entropy")
+
+
+def check_logprobs(z, want, k):
+    vocab = z.shape[1]
+    tokens = torch.tensor([0, vocab - 1])[:z.shape[0]]
+    logp, entropy, idx, top = P.token_logprobs(z.cuda(), tokens.cuda(), k)
+    R.close(logp, want.lp.gather(1, tokens[:, None])[:, 0], want.s_lp.gather(1, tokens[:, None])[:, 0], "logp")
+    R.close(entropy, want.entropy, want.s_sum[:, 0] * (2 + want.entropy), "entropy")
+    best = torch.sort(z.double(), dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(idx.cpu().long(), best)
+    R.close(top, want.lp.gather(1, best), want.s_lp.gather(1, best), "top")
+
+
+@pytest.mark.parametrize("dtype,offset", [(torch.float32, 1e3), (torch.float32, -1e4), (torch.float32, 3e6), (torch.float32, -5e8),
+                                          (torch.bfloat16, 300.0), (torch.bfloat16, -1e5), (torch.float16, 2000.0)])
+@pytest.mark.parametrize("vocab", VOCABS + [1_100_001])
+def test_log_probabilities_and_losses_of_rows_far_from_zero(vocab, dtype, offset):
+    print(f"[case] far {vocab} {offset} {dtype}", flush=True)
+    g = torch.Generator().manual_seed(vocab + 3)
+    z = (torch.randn(2, vocab, generator=g) * 3 * max(1.0, abs(offset) * 2.0 ** -10) + offset).to(dtype)
+    check_logprobs(z, Want(z), min(5, vocab))
+    idx, val = lists(g, torch.arange(vocab), 2, vocab, 9)
+    for temperature in (1.0, 3.0):
+        want = Want(z, temperature)
+        loss, grad, s_loss, s_grad = want.distill(idx, val, torch.ones(2))
+        R.close(P.distill(z.cuda(), idx.cuda(), val.cuda(), temperature=temperature)[0], loss, s_loss, "loss")
+        got, dz = P.distill_grad(z.cuda(), idx.cuda(), val.cuda(), torch.ones(2).cuda(), temperature=temperature)
+        R.close(got, loss, s_loss, "loss in one pass")
+        R.close(dz, grad, s_grad, "gradient in one pass")
+
+
+@pytest.mark.parametrize("vocab", VOCABS)
+@pytest.mark.parametrize("dtype,value", CASES + [(torch.float32, -3.4028234663852886e38), (torch.bfloat16, float(torch.finfo(torch.bfloat16).min)),
+                                                 (torch.float16, -65504.0)])
+def test_log_probabilities_and_losses_of_rows_masked_throughout(dtype, value, vocab):
+    z = torch.full((1, vocab), value).to(dtype)
+    check_logprobs(z, Want(z), min(5, vocab))
+    idx, val = torch.tensor([[vocab // 2, 0]], dtype=torch.int32), torch.tensor([[0.5, -0.5]])
+    loss, grad, s_loss, s_grad = Want(z, 2.0).distill(idx, val, torch.ones(1))
+    R.close(P.distill(z.cuda(), idx.cuda(), val.cuda(), temperature=2.0)[0], loss, s_loss, "loss")
+    got, dz = P.distill_grad(z.cuda(), idx.cuda(), val.cuda(), torch.ones(1).cuda(), temperature=2.0)
+    R.close(got, loss, s_loss, "loss in one pass")
+    R.close(dz, grad, s_grad, "gradient in one pass")
