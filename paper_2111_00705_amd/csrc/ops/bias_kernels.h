@@ -359,11 +359,12 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
             }
             team_reduce<SumOp, kTeam, kBatch>(total, scratch[turn]);       // the rows' reductions are independent: their steps interleave
             turn ^= 1;
-            // A key of probability zero takes no gradient whatever dp holds there.  While a row's sum is finite no product was NaN, so
-            // dp is finite there and the formula gives zero by itself; else such keys are cleared.
+            // A key of probability zero takes no gradient whatever dp holds there.  While a row's sum is of ordinary size no product was
+            // NaN, so dp is finite there, dp - total too, and the formula gives zero by itself; else such keys are cleared, and looked at
+            // once more below, for keys that do count may hold an infinity or a NaN.
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-                if (!(fabsf(total[u]) < INFINITY)) {
+                if (!(fabsf(total[u]) < kPlainMax)) {
 #pragma unroll
                     for (int v = 0; v < kVecs; ++v) {
                         float pw[E], dw[E];
@@ -381,6 +382,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
             for (int u = 0; u < kBatch; ++u) {
                 const int i = first + batch + u;
                 T *row = ds0 + i * a.o_q;
+                const bool usual = fabsf(total[u]) < kPlainMax;
 #pragma unroll
                 for (int v = 0; v < kVecs; ++v) {
                     const int slab = v * kTeam * E;
@@ -392,10 +394,16 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
                         widen<T>(pr[u][v], pw);
                         widen<T>(dr[u][v], dw);
 #pragma unroll
+                        for (int q = 0; q < E; ++q) dw[q] = pw[q] * (dw[q] - total[u]);
+                        if (!usual) {
+                            asm volatile("");                  // a branch that is not taken, not a selection for every element
+#pragma unroll
+                            for (int q = 0; q < E; ++q) dw[q] = pw[q] == 0.f ? 0.f : dw[q];
+                        }
+#pragma unroll
                         for (int q = 0; q < E; ++q) {
-                            const float dt = pw[q] * (dw[q] - total[u]);
-                            acc[v][q - (batch + u) + kStep - 1] += dt;
-                            dw[q] = dt * a.scale;
+                            acc[v][q - (batch + u) + kStep - 1] += dw[q];
+                            dw[q] *= a.scale;
                         }
                         out = narrow<T>(dw);
                     }

@@ -314,7 +314,8 @@ __device__ __forceinline__ Lse lse_join(const Lse &a, const Lse &b, float unit)
     return {top, a.sum * fa + b.sum * fb};
 }
 
-// Scores in units of log 2 below this size leave room for their distances within fp32.
+// Numbers below this size leave room within fp32 for their distances: scores in units of log 2 among each other; from any fp32 number, since half
+// a unit of the largest is 2^103.
 constexpr float kPlainMax = 1e31f;
 
 // A distance to the maximum, (x - top) unit, costs one instruction as fma(x, unit, -c) with c = top unit rounded to fp32.  Every such distance is
