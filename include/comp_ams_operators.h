@@ -12,8 +12,9 @@
  * Conventions
  *  - No handle.  Every call returns a status code of comp_ams.h, validates its arguments on the host before any
  *    device call, launches kernels on `hip_stream` (a hipStream_t of the current GPU, NULL = the null stream) and
- *    returns without waiting.  It allocates nothing, so it may be recorded into a HIP graph.  On failure nothing
- *    is launched and comp_ams_operators_last_error() describes the reason (per thread).
+ *    returns without waiting.  It allocates nothing, so it may be recorded into a HIP graph.  Of a call that is refused
+ *    (COMP_AMS_EINVAL) nothing is launched; where a launch fails (COMP_AMS_EDEVICE) what depends on it is not launched, and
+ *    outputs are undefined.  comp_ams_operators_last_error() describes the reason (per thread).
  *  - All pointers are device pointers of the current GPU unless they are named `host`.  Arrays of 16- and 32-bit
  *    elements need the alignment of their element only; strides are in elements and the last dimension is dense.
  *  - `type` is that of the activations (COMP_AMS_F32, COMP_AMS_BF16 or COMP_AMS_F16), `grad_type` that of the

@@ -30,6 +30,7 @@ struct BiasArgs {
     float scale;
     int32_t causal;
     bool stream_out;                      // p, ds are stored as a stream
+    unsigned first;                       // workgroups that earlier launches of the call have taken
 };
 
 constexpr int kBiasThreads = 256;
@@ -110,7 +111,8 @@ __global__ __launch_bounds__(kBiasAnyThreads) void bias_backward_any(T *ds, floa
     __shared__ int32_t at[COMP_AMS_MAX_BUCKETS];
     __shared__ float slot[COMP_AMS_MAX_BUCKETS * kBiasAnyThreads];
     const int lane = threadIdx.x;
-    const int64_t bh = blockIdx.x / pieces, piece = blockIdx.x % pieces;
+    const unsigned block = a.first + blockIdx.x;
+    const int64_t bh = block / pieces, piece = block % pieces;
     for (int q = lane; q < bounds.n; q += kBiasAnyThreads) at[q] = bounds.at[q];
     for (int q = 0; q <= bounds.n; ++q) slot[q * kBiasAnyThreads + lane] = 0.f;
     __syncthreads();
@@ -166,7 +168,8 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_forward(T *p, const T 
     __shared__ float of_bucket[COMP_AMS_MAX_BUCKETS];
     const Team<kTeam> me;
     // with a causal mask the last queries see most: they are taken first
-    const unsigned bh = blockIdx.x / (unsigned)pieces, turn_of = blockIdx.x % (unsigned)pieces, piece = a.causal ? pieces - 1 - turn_of : turn_of;
+    const unsigned block = a.first + blockIdx.x, bh = block / (unsigned)pieces, turn_of = block % (unsigned)pieces;
+    const unsigned piece = a.causal ? pieces - 1 - turn_of : turn_of;
     const int64_t b = bh / (unsigned)a.heads, h = bh % (unsigned)a.heads;
     const int tk = (int)a.tk, i0 = (int)piece * rows_block, i1 = min(i0 + rows_block, (int)a.tq);
     const int64_t by_length = key_len ? min((int64_t)max(key_len[b], 0), a.tk) : a.tk;
@@ -288,7 +291,8 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void bias_backward(T *ds, float 
     __shared__ int32_t at[COMP_AMS_MAX_BUCKETS];
     const Team<kTeam> me;
     // with a causal mask the last queries see most: they are taken first
-    const unsigned bh = blockIdx.x / (unsigned)pieces, turn_of = blockIdx.x % (unsigned)pieces, piece = a.causal ? pieces - 1 - turn_of : turn_of;
+    const unsigned block = a.first + blockIdx.x, bh = block / (unsigned)pieces, turn_of = block % (unsigned)pieces;
+    const unsigned piece = a.causal ? pieces - 1 - turn_of : turn_of;
     const unsigned b = bh / (unsigned)a.heads, h = bh % (unsigned)a.heads;
     const int tk = (int)a.tk, tq = (int)a.tq, span = kSlots + rows_team - 1;
     const int i0 = (int)piece * rows_team * kTeams, mine = i0 + me.id * rows_team, end = mine + rows_team;

@@ -275,11 +275,11 @@ constexpr int kJoinCols = 32, kJoinParts = kNormThreads / kJoinCols;
 template <typename G>
 __global__ __launch_bounds__(kNormThreads) void norm_param_join(G *__restrict__ dgain, G *__restrict__ dshift,
                                                                 const float *__restrict__ work, int64_t cols, int chunks,
-                                                                int64_t grad_stride)
+                                                                int64_t grad_stride, unsigned first)
 {
     __shared__ float parts[kJoinParts][kJoinCols];
     const int part = threadIdx.x / kJoinCols, lane = threadIdx.x % kJoinCols;
-    const int64_t c = (int64_t)blockIdx.x * kJoinCols + lane;
+    const int64_t c = (int64_t)(first + blockIdx.x) * kJoinCols + lane;
     float s = 0.f;
     if (c < 2 * cols) {
         const float *in = work + (int64_t)blockIdx.y * chunks * 2 * cols + c;

@@ -36,7 +36,19 @@ int launched(const char *what)
     return COMP_AMS_OK;
 }
 
-constexpr int64_t kMaxGrid = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 31) - 1;     // workgroups of a call, counted in 32 bits
+
+// Workgroups of one launch: HIP takes fewer than 2^32 threads.
+constexpr int64_t most_blocks(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+
+// launch(first, count) for the workgroups [first, first + count) of a call, which has up to kMaxBlocks of them: one launch unless they are
+// millions.
+template <typename F>
+void in_launches(int64_t blocks, int threads, F &&launch)
+{
+    const int64_t most = most_blocks(threads);
+    for (int64_t first = 0; first < blocks; first += most) launch((unsigned)first, (unsigned)std::min(blocks - first, most));
+}
 constexpr int64_t kMaxElements = (int64_t)1 << 60;    // rows * stride: offsets in bytes stay far below 2^63
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -250,7 +262,7 @@ PieceShape piece_shape(int64_t rows, int64_t vocab, int32_t type)
         return s;
     }
     const int64_t count = ceil_div(vocab, lanes * kPieceVecs);
-    if (count > kMaxPieces || rows * count > kMaxGrid) return {0, 0, 0, 0};
+    if (count > kMaxPieces || rows * count > kMaxBlocks) return {0, 0, 0, 0};
     s.count = (int32_t)count;
     if (count > 1) s.len = ceil_div(ceil_div(vocab, count), 64) * 64;
     s.vecs = (int32_t)ceil_div(s.len, lanes);
@@ -285,7 +297,7 @@ int comp_ams_layer_norm(void *y, float *mean, float *rstd, const void *x, const 
                 static_cast<T *>(y), mean, rstd, static_cast<const T *>(x), gain, shift, a);
         });
         if (!held)
-            norm_forward_any<T><<<(unsigned)std::min(rows, kMaxGrid), kNormThreads, 0, stream>>>(static_cast<T *>(y), mean, rstd,
+            norm_forward_any<T><<<(unsigned)std::min(rows, most_blocks(kNormThreads)), kNormThreads, 0, stream>>>(static_cast<T *>(y), mean, rstd,
                                                                                               static_cast<const T *>(x), gain, shift, a);
     });
     return launched(what);
@@ -339,13 +351,16 @@ int comp_ams_layer_norm_backward(void *dx, void *dgain, void *dshift, const void
         norm_param_any<T><<<dim3((unsigned)ceil_div(cols, kNormThreads), (unsigned)ch.count, (unsigned)n), kNormThreads, 0, stream>>>(
             sums, static_cast<const T *>(dy), static_cast<const T *>(x), mean, rstd, a, rows / n, ch.rows);
         if (rows > 0)
-            norm_backward_any<T><<<(unsigned)std::min(rows, kMaxGrid), kNormThreads, 0, stream>>>(
+            norm_backward_any<T><<<(unsigned)std::min(rows, most_blocks(kNormThreads)), kNormThreads, 0, stream>>>(
                 static_cast<T *>(dx), static_cast<const T *>(dy), static_cast<const T *>(x), mean, rstd, gain, a);
     });
+    if (const int rc = launched(what)) return rc;              // what the join would read has not been written
     with_type(grad_type, [&](auto t) {
         using G = decltype(t);
-        norm_param_join<G><<<dim3((unsigned)ceil_div(2 * cols, kJoinCols), (unsigned)n), kNormThreads, 0, stream>>>(
-            static_cast<G *>(dgain), static_cast<G *>(dshift), sums, cols, (int)ch.count, grad_stride);
+        in_launches(ceil_div(2 * cols, kJoinCols), kNormThreads, [&](unsigned first, unsigned count) {
+            norm_param_join<G><<<dim3(count, (unsigned)n), kNormThreads, 0, stream>>>(static_cast<G *>(dgain), static_cast<G *>(dshift), sums,
+                                                                                    cols, (int)ch.count, grad_stride, first);
+        });
     });
     return launched(what);
 }
@@ -378,9 +393,11 @@ int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const 
             const int rows_block = (int)std::min<int64_t>(tq, std::min<int64_t>(256, share));
             const int64_t pieces = ceil_div(tq, rows_block);
             const size_t lds = (size_t)(tk + rows_block - 1) * sizeof(float);
-            bias_forward<T, S::threads, S::vecs><<<(unsigned)(batch * heads * pieces), kTeamBlock<S::threads>, lds,
-                                                  static_cast<hipStream_t>(hip_stream)>>>(
-                static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a, (int)pieces, rows_block);
+            in_launches(batch * heads * pieces, kTeamBlock<S::threads>, [&](unsigned first, unsigned count) {
+                a.first = first;
+                bias_forward<T, S::threads, S::vecs><<<count, kTeamBlock<S::threads>, lds, static_cast<hipStream_t>(hip_stream)>>>(
+                    static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a, (int)pieces, rows_block);
+            });
         };
         // rows of more than 128 vectors by a workgroup: by a wavefront they take 150 registers (2 x 16 x 2000 x 2000 f16 172 us against 119)
         if (tk >= kVec<T> && vecs <= 1024) {
@@ -389,7 +406,7 @@ int comp_ams_rel_bias_softmax(void *p, const void *s, const float *table, const 
             else with_vecs<256, 1, 4>((int)ceil_div(vecs, 256), launch);
             return;
         }
-        bias_forward_any<T><<<(unsigned)a.rows, kBiasThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+        bias_forward_any<T><<<(unsigned)std::min(a.rows, most_blocks(kBiasThreads)), kBiasThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
             static_cast<T *>(p), static_cast<const T *>(s), table, bounds, key_len, a);
     });
     return launched(what);
@@ -444,10 +461,13 @@ int comp_ams_rel_bias_softmax_backward(void *ds, void *dtable, const void *dp, c
         a.offset = offset, a.scale = scale, a.causal = causal != 0, a.stream_out = streamed_out(a.rows * tk, type);
         with_type(type, [&](auto t) {
             using T = decltype(t);
-            const unsigned grid = (unsigned)(batch * heads * cut.pieces);
+            const int64_t blocks = batch * heads * cut.pieces;
             if (!cut.held) {
-                bias_backward_any<T><<<grid, kBiasAnyThreads, 0, stream>>>(static_cast<T *>(ds), sums, static_cast<const T *>(dp),
-                                                                          static_cast<const T *>(p), bounds, key_len, a, cut.pieces, batch / n);
+                in_launches(blocks, kBiasAnyThreads, [&](unsigned first, unsigned count) {
+                    a.first = first;
+                    bias_backward_any<T><<<count, kBiasAnyThreads, 0, stream>>>(static_cast<T *>(ds), sums, static_cast<const T *>(dp),
+                                                                               static_cast<const T *>(p), bounds, key_len, a, cut.pieces, batch / n);
+                });
                 return;
             }
             auto launch = [&](auto shape) {
@@ -457,15 +477,19 @@ int comp_ams_rel_bias_softmax_backward(void *ds, void *dtable, const void *dp, c
                 constexpr int kTeams = kTeamBlock<S::threads> / S::threads, kStep = 4, kBatch = S::vecs > 1 ? 1 : 2;
                 constexpr int kSlots = S::threads * S::vecs * kVec<T>;
                 const size_t lds = ((size_t)kTeams * (kSlots + cut.rows_team - 1) + (kTeams > 1 ? kSlots + cut.rows_block - 1 : 0)) * sizeof(float);
-                bias_backward<T, S::threads, S::vecs, kStep, kBatch><<<grid, kTeamBlock<S::threads>, lds, stream>>>(
-                    static_cast<T *>(ds), sums, static_cast<const T *>(dp), static_cast<const T *>(p), bounds, key_len, a,
-                    (int)cut.pieces, cut.rows_team, (unsigned)(batch / n));
+                in_launches(blocks, kTeamBlock<S::threads>, [&](unsigned first, unsigned count) {
+                    a.first = first;
+                    bias_backward<T, S::threads, S::vecs, kStep, kBatch><<<count, kTeamBlock<S::threads>, lds, stream>>>(
+                        static_cast<T *>(ds), sums, static_cast<const T *>(dp), static_cast<const T *>(p), bounds, key_len, a,
+                        (int)cut.pieces, cut.rows_team, (unsigned)(batch / n));
+                });
             };
             const int vecs = (int)ceil_div(tk, kVec<T>);
             if (cut.team == 16) with_vecs<16, 1, 2>(ceil_div(vecs, 16), launch);
             else if (cut.team == 64) with_vecs<64, 1, 2>(ceil_div(vecs, 64), launch);
             else with_vecs<256, 1, 4>(ceil_div(vecs, 256), launch);
         });
+        if (const int rc = launched(what)) return rc;          // what the join would read has not been written
     }
     with_type(grad_type, [&](auto t) {
         using G = decltype(t);
@@ -504,11 +528,12 @@ int comp_ams_token_logprobs(float *logp, float *entropy, int32_t *top_idx, float
     if (rows == 0) return COMP_AMS_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const PieceShape s = piece_shape(rows, vocab, type);
+    int rc = COMP_AMS_OK;
     with_type(type, [&](auto t) {
         using T = decltype(t);
         const T *z = static_cast<const T *>(logits);
         if (s.count == 0) {
-            logprobs_any<T><<<(unsigned)rows, kVocabThreads, 0, stream>>>(logp, entropy, top_idx, top_logp, z, tokens, rows, vocab, stride, k);
+            logprobs_any<T><<<(unsigned)std::min(rows, most_blocks(kVocabThreads)), kVocabThreads, 0, stream>>>(logp, entropy, top_idx, top_logp, z, tokens, rows, vocab, stride, k);
             return;
         }
         uint64_t *keys = static_cast<uint64_t *>(work);
@@ -516,17 +541,22 @@ int comp_ams_token_logprobs(float *logp, float *entropy, int32_t *top_idx, float
         const int groups = k <= 32 ? 64 : k <= 64 ? 128 : 256;
         auto launch = [&](auto shape) {
             using S = decltype(shape);
-            logprobs_regs<T, S::threads, S::vecs><<<(unsigned)(rows * s.count), S::threads, 0, stream>>>(
-                logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, groups, s.count, s.len,
-                s.len < (int64_t)S::threads * S::vecs * kVec<T> ? 1 : 0, pieces, keys);
+            in_launches(rows * s.count, S::threads, [&](unsigned first, unsigned count) {
+                logprobs_regs<T, S::threads, S::vecs><<<count, S::threads, 0, stream>>>(
+                    logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, groups, s.count, s.len,
+                    s.len < (int64_t)S::threads * S::vecs * kVec<T> ? 1 : 0, pieces, keys, first);
+            });
         };
         if (s.threads == kPieceThreads) with_vecs<kPieceThreads, 1, kPieceVecs>(s.vecs, launch);
         else launch(Shape<kPieceThreads / 2, 1>{});
-        if (s.count > 1)
-            logprobs_join<T><<<(unsigned)rows, kVocabThreads, (size_t)s.count * k * sizeof(uint64_t), stream>>>(
-                logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, s.count, pieces, keys);
+        rc = launched(what);                                   // unless it is good, what the join would read has not been written
+        if (rc == COMP_AMS_OK && s.count > 1)
+            in_launches(rows, kVocabThreads, [&](unsigned first, unsigned count) {
+                logprobs_join<T><<<count, kVocabThreads, (size_t)s.count * k * sizeof(uint64_t), stream>>>(
+                    logp, entropy, top_idx, top_logp, z, tokens, vocab, stride, k, s.count, pieces, keys, first);
+            });
     });
-    return launched(what);
+    return rc ? rc : launched(what);
 }
 
 int comp_ams_distill(float *loss, float *lse, const void *logits, const int32_t *idx, const float *val, int64_t rows, int64_t vocab,
@@ -536,17 +566,23 @@ int comp_ams_distill(float *loss, float *lse, const void *logits, const int32_t 
     if (const int rc = distill_check(what, logits, idx, val, rows, vocab, stride, k, temperature, type)) return rc;
     REQUIRE(aligned(loss, 4) && aligned(lse, 4), "%s: loss and lse must be 4-byte aligned", what);
     if (rows == 0) return COMP_AMS_OK;
-    const DistillArgs a = {rows, vocab, stride, 0, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type)};
+    DistillArgs a = {rows, vocab, stride, 0, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type), 0};
     with_type(type, [&](auto t) {
         using T = decltype(t);
         auto launch = [&](auto shape) {
             using S = decltype(shape);
-            distill_forward<T, S::threads><<<(unsigned)rows, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
-                loss, lse, static_cast<const T *>(logits), idx, val, a);
+            in_launches(rows, S::threads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                distill_forward<T, S::threads><<<count, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                    loss, lse, static_cast<const T *>(logits), idx, val, a);
+            });
         };
         if (vocab < kVec<T>)
-            distill_any<T, true, false><<<(unsigned)rows, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
-                loss, lse, nullptr, nullptr, static_cast<const T *>(logits), nullptr, idx, val, a);
+            in_launches(rows, kVocabThreads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                distill_any<T, true, false><<<count, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                    loss, lse, nullptr, nullptr, static_cast<const T *>(logits), nullptr, idx, val, a);
+            });
         else if (rows >= 1024 || vocab <= 4 * 256 * kVec<T>) launch(Shape<256, 0>{});
         else launch(Shape<1024, 0>{});
     });
@@ -563,20 +599,26 @@ int comp_ams_distill_backward(void *dlogits, const float *dloss, const void *log
     REQUIRE((dloss && lse) || rows == 0, "%s: dloss or lse is NULL", what);
     REQUIRE(aligned(dloss, 4) && aligned(lse, 4), "%s: dloss and lse must be 4-byte aligned", what);
     if (rows == 0) return COMP_AMS_OK;
-    const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type)};
+    DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type), 0};
     with_type(type, [&](auto t) {
         using T = decltype(t);
         if (vocab < kVec<T>) {
-            distill_any<T, false, true><<<(unsigned)rows, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
-                nullptr, nullptr, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), lse, idx, val, a);
+            in_launches(rows, kVocabThreads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                distill_any<T, false, true><<<count, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                    nullptr, nullptr, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), lse, idx, val, a);
+            });
             return;
         }
         const int64_t chunk = 4 * 256 * kVec<T>;
-        const int64_t pieces = std::max<int64_t>(1, std::min(ceil_div(vocab, 4 * chunk), kMaxGrid / rows));
+        const int64_t pieces = std::max<int64_t>(1, std::min(ceil_div(vocab, 4 * chunk), kMaxBlocks / rows));
         const int64_t len = ceil_div(ceil_div(vocab, pieces), chunk) * chunk;
         const int64_t count = ceil_div(vocab, len);
-        distill_gradient<T, 256><<<(unsigned)(rows * count), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(
-            static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), lse, idx, val, a, (int)count, len);
+        in_launches(rows * count, 256, [&](unsigned first, unsigned blocks) {
+            a.first = first;
+            distill_gradient<T, 256><<<blocks, 256, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), lse, idx, val, a, (int)count, len);
+        });
     });
     return launched(what);
 }
@@ -591,18 +633,24 @@ int comp_ams_distill_grad(float *loss, void *dlogits, const float *dloss, const 
     REQUIRE(dloss || rows == 0, "%s: dloss is NULL", what);
     REQUIRE(aligned(dloss, 4) && aligned(loss, 4), "%s: dloss and loss must be 4-byte aligned", what);
     if (rows == 0) return COMP_AMS_OK;
-    const DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type)};
+    DistillArgs a = {rows, vocab, stride, dlogits_stride, k, temperature, 1.f / temperature, streamed_in(rows * vocab, type), streamed_out(rows * vocab, type), 0};
     with_type(type, [&](auto t) {
         using T = decltype(t);
         auto launch = [&](auto shape) {
             using S = decltype(shape);
-            distill_both<T, S::threads, S::vecs, S::sure><<<(unsigned)rows, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
-                loss, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), idx, val, a);
+            in_launches(rows, S::threads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                distill_both<T, S::threads, S::vecs, S::sure><<<count, S::threads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                    loss, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), idx, val, a);
+            });
         };
         const int64_t vecs = ceil_div(vocab, kVec<T>);          // vectors of the row
         if (vocab < kVec<T>)
-            distill_any<T, true, true><<<(unsigned)rows, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
-                loss, nullptr, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), nullptr, idx, val, a);
+            in_launches(rows, kVocabThreads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                distill_any<T, true, true><<<count, kVocabThreads, 0, static_cast<hipStream_t>(hip_stream)>>>(
+                    loss, nullptr, static_cast<T *>(dlogits), dloss, static_cast<const T *>(logits), nullptr, idx, val, a);
+            });
         else if (vecs <= 256) launch(Shape<256, 1>{});
         else if (vecs <= 512 * 8) with_vecs<512, 1, 8>((int)ceil_div(vecs, 512), launch);
         else if (vecs <= 1024 * 8) with_vecs<1024, 5, 8>((int)ceil_div(vecs, 1024), launch);

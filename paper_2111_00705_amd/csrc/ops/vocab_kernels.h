@@ -230,7 +230,8 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
                                                           int32_t *__restrict__ top_idx, float *__restrict__ top_logp,
                                                           const T *__restrict__ logits, const int64_t *__restrict__ tokens,
                                                           int64_t vocab, int64_t stride, int k, int groups, int n_pieces,
-                                                          int64_t piece_len, int room, Piece *__restrict__ pieces, uint64_t *__restrict__ keys)
+                                                          int64_t piece_len, int room, Piece *__restrict__ pieces, uint64_t *__restrict__ keys,
+                                                          unsigned first)
 {
     constexpr int E = kVec<T>, kWaves = kThreads / kWave;
     __shared__ float scratch[kWaves], sum_of[kWaves], moment_of[kWaves], group_max[256];
@@ -240,7 +241,8 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
     __shared__ uint32_t count, queued, strange, bound_order;
     __shared__ float log_sum_lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int64_t row = blockIdx.x / (unsigned)n_pieces, begin = blockIdx.x % (unsigned)n_pieces * piece_len;
+    const unsigned block = first + blockIdx.x;           // first: workgroups that earlier launches of the call have taken
+    const int64_t row = block / (unsigned)n_pieces, begin = block % (unsigned)n_pieces * piece_len;
     // `back` elements before the row's first one take part in the loads and in nothing else; room: there is a place for one
     const int back = begin == 0 && room ? step_back(logits + row * stride, row) : 0;
     const int64_t lo = begin - back;
@@ -320,7 +322,7 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
             piece.sum *= f;
             piece.moment = fmaf(fmaf(-m, kLog2e, c), piece.sum, piece.moment * f);
         }
-        if (tid == 0 && !whole) pieces[blockIdx.x] = piece;
+        if (tid == 0 && !whole) pieces[block] = piece;
         if (tid == 0 && whole) {
             const float log_of = log_sum(m, piece.sum);
             log_sum_lds = log_of;
@@ -383,11 +385,11 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
             top_idx[row * k + rank] = (int32_t)~(uint32_t)key;
             top_logp[row * k + rank] = (logit_of(key) - m) - log_sum_lds;
         } else {
-            keys[(int64_t)blockIdx.x * k + rank] = key;
+            keys[(int64_t)block * k + rank] = key;
         }
     });
     if (!whole)
-        for (int t = n + tid; t < k; t += kThreads) keys[(int64_t)blockIdx.x * k + t] = 0;   // a short last piece
+        for (int t = n + tid; t < k; t += kThreads) keys[(int64_t)block * k + t] = 0;   // a short last piece
 }
 
 // The pieces of a row: statistics joined in order, their best tokens ranked against each other.
@@ -396,10 +398,11 @@ __global__ __launch_bounds__(kVocabThreads) void logprobs_join(float *__restrict
                                                                int32_t *__restrict__ top_idx, float *__restrict__ top_logp,
                                                                const T *__restrict__ logits, const int64_t *__restrict__ tokens,
                                                                int64_t vocab, int64_t stride, int k, int n_pieces,
-                                                               const Piece *__restrict__ pieces, const uint64_t *__restrict__ keys)
+                                                               const Piece *__restrict__ pieces, const uint64_t *__restrict__ keys,
+                                                               unsigned first)
 {
     extern __shared__ uint64_t list[];
-    const int64_t row = blockIdx.x;
+    const int64_t row = first + blockIdx.x;
     const int n = n_pieces * k;
     for (int t = threadIdx.x; t < n; t += kVocabThreads) list[t] = keys[row * n + t];
     Piece p = pieces[row * n_pieces];
@@ -443,6 +446,7 @@ struct DistillArgs {
     int32_t k;
     float t, inv_t;          // the temperature and its reciprocal
     bool stream_in, stream_out;
+    unsigned first;          // workgroups that earlier launches of the call have taken
 };
 
 // The teacher's list of one row, two entries in each lane of a wavefront: every wavefront that needs the list forms its shares for
@@ -677,7 +681,7 @@ __global__ __launch_bounds__(kThreads) void distill_forward(float *__restrict__ 
                                                             const float *__restrict__ val, DistillArgs a)
 {
     __shared__ float lse_scratch[2 * kThreads / kWave];
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.first + blockIdx.x;
     const T *z = logits + row * a.in_stride;
     Listed e = {};
     float at[2] = {0.f, 0.f};
@@ -705,7 +709,7 @@ __global__ __launch_bounds__(kVocabThreads) void distill_any(float *__restrict__
                                                              const float *__restrict__ lse_in, const int32_t *__restrict__ idx,
                                                              const float *__restrict__ val, DistillArgs a)
 {
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.first + blockIdx.x;
     const T *z = logits + row * a.in_stride;
     if (threadIdx.x >= kWave) return;
     Listed e = teacher_list(load_list(idx, val, row, a.k), a);
@@ -746,7 +750,8 @@ __global__ __launch_bounds__(kThreads) void distill_gradient(T *dlogits, const f
                                                              const float *__restrict__ lse_in, const int32_t *__restrict__ idx,
                                                              const float *__restrict__ val, DistillArgs a, int n_pieces, int64_t piece_len)
 {
-    const int64_t row = blockIdx.x / (unsigned)n_pieces, lo = blockIdx.x % (unsigned)n_pieces * piece_len;
+    const unsigned block = a.first + blockIdx.x;
+    const int64_t row = block / (unsigned)n_pieces, lo = block % (unsigned)n_pieces * piece_len;
     const int64_t hi = min(lo + piece_len, a.vocab);
     const T *z = logits + row * a.in_stride;
     T *out = dlogits + row * a.out_stride;
@@ -786,7 +791,7 @@ __global__ __launch_bounds__(kThreads, (kThreads <= 512 ? 6 : 4)) void distill_b
 {
     constexpr int E = kVec<T>, kHeld = kVecs ? kVecs : 1;
     __shared__ float lse_scratch[2 * kThreads / kWave];
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.first + blockIdx.x;
     const int tid = threadIdx.x;
     const T *z = logits + row * a.in_stride;
     T *out = dlogits + row * a.out_stride;
