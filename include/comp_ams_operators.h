@@ -123,7 +123,8 @@ int comp_ams_token_logprobs_work_bytes(int64_t rows, int64_t vocab, int32_t k, i
  *   loss = T^2 sum_j q_j (log q_j - lp_{idx_j})
  * and, for a gradient dloss of the row's loss,
  *   dz_v = dloss T (exp(lp_v) - sum of q_j over the j with idx_j = v).
- * A row whose list is empty has loss 0 and gradient 0.  Entries with val = -infinity are listed with q = 0.
+ * A row whose list is empty has loss 0 and gradient 0.  Entries with val = -infinity are listed with q = 0; if all are, the loss is 0 and
+ * the gradient that of the probabilities alone.
  * idx: int32, val: fp32, dense [rows][k], 1 <= k <= COMP_AMS_MAX_TOP; 1 <= vocab < 2^31.
  *   comp_ams_distill           writes loss [rows] and lse [rows] (either may be NULL)
  *   comp_ams_distill_backward  writes dz [rows][vocab] from lse and dloss.  lse has been rounded to fp32, which the probabilities carry

@@ -495,7 +495,8 @@ __device__ __forceinline__ Listed teacher_list(const RawList &r, const DistillAr
     const float top = lanes_reduce<MaxOp, kWave>(MaxOp::apply(v[0], v[1]));
     float x[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) x[u] = e.token[u] >= 0 ? __builtin_amdgcn_exp2f((v[u] - top) * kLog2e) : 0.f;
+    for (int u = 0; u < 2; ++u)                  // -infinity is listed with nothing, beside others and beside its like
+        x[u] = e.token[u] >= 0 && v[u] != -INFINITY ? __builtin_amdgcn_exp2f((v[u] - top) * kLog2e) : 0.f;
     const float sum = lanes_reduce<SumOp, kWave>(x[0] + x[1]), log_sum = logf(sum);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
