@@ -489,19 +489,22 @@ __device__ __forceinline__ Listed teacher_list(const RawList &r, const DistillAr
     for (int u = 0; u < 2; ++u) {
         const bool there = r.token[u] >= 0 && r.token[u] < a.vocab;
         e.token[u] = there ? r.token[u] : -1;
-        v[u] = there ? r.val[u] * a.inv_t : -INFINITY;
+        v[u] = there ? r.val[u] : -INFINITY;
     }
     e.any = __ballot(e.token[0] >= 0 || e.token[1] >= 0) != 0;
     const float top = lanes_reduce<MaxOp, kWave>(MaxOp::apply(v[0], v[1]));
-    float x[2];
+    float d[2], x[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)                  // -infinity is listed with nothing, beside others and beside its like
-        x[u] = e.token[u] >= 0 && v[u] != -INFINITY ? __builtin_amdgcn_exp2f((v[u] - top) * kLog2e) : 0.f;
+    for (int u = 0; u < 2; ++u) {
+        d[u] = (v[u] - top) * a.inv_t;           // the difference first: values of any size keep their distances
+        // -infinity is listed with nothing, beside others and beside its like
+        x[u] = e.token[u] >= 0 && v[u] != -INFINITY ? __builtin_amdgcn_exp2f(d[u] * kLog2e) : 0.f;
+    }
     const float sum = lanes_reduce<SumOp, kWave>(x[0] + x[1]), log_sum = logf(sum);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         e.q[u] = x[u] == 0.f ? 0.f : x[u] / sum;
-        e.logq[u] = e.q[u] == 0.f ? 0.f : (v[u] - top) - log_sum;
+        e.logq[u] = e.q[u] == 0.f ? 0.f : d[u] - log_sum;
     }
     return e;
 }
