@@ -196,7 +196,9 @@ __device__ __forceinline__ void rank_keys(const uint64_t *list, int n, int k, F 
 }
 
 // The k-th largest of `groups` (64, 128 or 256) values in LDS as its place in the order, by one wavefront: bisection over the bits of the
-// order, counting by ballots.  kBits: how many of them, from the top, tell values of the type apart.
+// order, counting by ballots.  kBits: how many of them, from the top, tell values of the type apart in fp32's form: all; those of bfloat16; sign,
+// eight bits of exponent (subnormal numbers are normal ones in fp32) and ten of fraction of half precision.
+template <typename T> constexpr int kOrderBits = sizeof(T) == 4 ? 32 : __is_same(T, bf16_t) ? 16 : 19;
 template <int kBits>
 __device__ __forceinline__ uint32_t kth_largest(const float *values, int groups, int k)
 {
@@ -308,7 +310,7 @@ __global__ __launch_bounds__(kThreads, kThreads == kPieceThreads ? 8 : 4) void l
         if (!(fabsf(s) < INFINITY)) strange = 1;        // a NaN or an infinity: the bound says nothing then
     }
     if (k > 0 && wave == kWaves - 1) {
-        const uint32_t o = kth_largest<8 * (int)sizeof(T)>(group_max, groups, k);
+        const uint32_t o = kth_largest<kOrderBits<T>>(group_max, groups, k);
         if ((tid & (kWave - 1)) == 0) bound_order = o;
     }
     __syncthreads();

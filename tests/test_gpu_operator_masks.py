@@ -189,3 +189,30 @@ def test_log_probabilities_and_losses_of_rows_masked_throughout(dtype, value, vo
     got, dz = P.distill_grad(z.cuda(), idx.cuda(), val.cuda(), torch.ones(1).cuda(), temperature=2.0)
     R.close(got, loss, s_loss, "loss in one pass")
     R.close(dz, grad, s_grad, "gradient in one pass")
+
+
+def time_of(call, repeats=7):
+    call()
+    best = math.inf
+    for _ in range(repeats):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        call()
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("k", [32, 128])
+def test_alternatives_of_half_precision_logits_far_from_zero_take_no_longer(k):
+    """The bound that a row's k best values reach is as fine as half precision there: rows do not go to the search by bisection, which
+    reads them 60 times."""
+    g = torch.Generator(device="cuda").manual_seed(k)
+    near = torch.randn(1024, 32_000, device="cuda", generator=g) * 2.5
+    far = (near + 400.0).half()
+    near = near.half()
+    idx = P.token_logprobs(far, None, k)[2]
+    first = torch.sort(far[:8].cpu().double(), dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(idx[:8].cpu().long(), first)
+    assert time_of(lambda: P.token_logprobs(far, None, k)) < 2 * time_of(lambda: P.token_logprobs(near, None, k))
