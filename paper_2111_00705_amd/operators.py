@@ -206,7 +206,11 @@ def _bounds(bounds):
     if type(bounds) is np.ndarray and bounds.dtype == np.int32 and bounds.flags.c_contiguous:
         b = bounds
     else:
-        b = np.ascontiguousarray(bounds, dtype=np.int32)
+        b = np.asarray(bounds)
+        if b.size:
+            _need(b.dtype.kind in "iuf" and np.isfinite(b).all() and (b == np.floor(b)).all() and -2 ** 31 <= b.min() and b.max() < 2 ** 31,
+                  "bounds must be whole numbers of 32 bits")
+        b = np.ascontiguousarray(b, dtype=np.int32)
     _need(b.ndim == 1, "bounds must be one-dimensional")
     return b
 
