@@ -283,13 +283,13 @@ def token_logprobs(logits, tokens=None, k=0):
     if tokens is not None:
         _vector(tokens, rows, torch.int64, "tokens")
     s = _stream(logits, tokens)
+    L, kind = lib(), _type(logits)
+    work, work_ptr, work_bytes = _work("comp_ams_token_logprobs_work_bytes", logits.device, rows, vocab, k, kind)      # looks at k
     f32 = dict(dtype=torch.float32, device=logits.device)
     logp = None if tokens is None else torch.empty(rows, **f32)
     entropy = torch.empty(rows, **f32) if logp is None else torch.empty_like(logp)
     top = torch.empty((rows, k), **f32)
     idx = torch.empty_like(top, dtype=torch.int32)
-    L, kind = lib(), _type(logits)
-    work, work_ptr, work_bytes = _work("comp_ams_token_logprobs_work_bytes", logits.device, rows, vocab, k, kind)
     _check(L.comp_ams_token_logprobs(None if logp is None else logp.data_ptr(), entropy.data_ptr(), idx.data_ptr(), top.data_ptr(),
                                      logits.data_ptr(), None if tokens is None else tokens.data_ptr(), rows, vocab, stride, k, kind,
                                      work_ptr, work_bytes, s))
