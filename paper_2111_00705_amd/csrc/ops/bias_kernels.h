@@ -6,9 +6,10 @@
 // HBM-bound: scores are read once and probabilities written once; backward reads p and dp once, writes ds, and sums the table's gradient
 // on the way.  Bias and gradient belong to relative positions, that is to diagonals: forward finds a row's biases side by side in LDS,
 // backward adds up diagonals in registers.  Only the keys that a row sees are read.
-// Measured (us, TB/s of what a pass cannot do without; a copy reaches 6.1): 16 x 12 x 512 x 512 bf16, lengths 0 to 512, forward 33 (4.5),
-// backward 48 with the join (4.1); causal 2 x 16 x 1999 x 1999 f16 backward 112 (4.5).  Backward spends 25 of its 46 us in vector
-// instructions (19 for each element, the reductions of a row among them); the rest is latency that two rows in flight a wavefront leave.
+// Measured (us of a pass among others, TB/s of what it cannot do without; a copy reaches 6.1): 16 x 12 x 512 x 512 bf16, lengths 0 to 512, forward
+// 31.7 (4.6), backward 47.6 with the join (4.1); causal 2 x 16 x 1999 x 1999 f16 forward 113 (3.4), backward 113 (4.5).  Backward spends 25 of its
+// 45 us in vector instructions (19 for each element, the reductions of a row among them); the rest is latency that two rows in flight a wavefront
+// leave.
 #pragma once
 #include "op_common.h"
 #include "../../../include/comp_ams_operators.h"

@@ -5,8 +5,8 @@
 //
 // HBM-bound: a row is read once and kept in registers, the variance is taken from the differences (no cancellation), and a lane keeps
 // its columns' gradient sums in registers over all rows of its chunk, so that x and dy are read once for dx and both parameter
-// gradients.  Measured (us, and TB/s of what a pass cannot do without): forward 16384 x 768 bf16 13.5 (3.7; 50 MB, half of it in the
-// memory-side cache), backward 19.3 with the join of the chunks (3.9); backward 20000 x 2047 fp32, n = 20 112 (4.4), of which the join 8.
+// gradients.  Measured (us of a pass among others, TB/s of what it cannot do without): forward 16384 x 768 bf16 12.2 (4.1; 50 MB, half of it in
+// the memory-side cache), backward 18.9 with the join of the chunks (4.0); backward 20000 x 2047 fp32, n = 20 112 (4.4), of which the join 8.
 // A copy reaches 6.1 TB/s.  One kernel per chunk of rows and a join in fixed order instead of atomics: results never vary.
 #pragma once
 #include "op_common.h"

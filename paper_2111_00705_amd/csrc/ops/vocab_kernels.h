@@ -6,9 +6,9 @@
 // HBM-bound, with vector instructions close behind where logits have 16 bits: an element costs 8.5 issue slots (widening, maximum,
 // fused multiply-add, exponential (two), sum, moment) where HBM leaves about 13.  So rows are read once and held in registers between
 // the passes over them, and exponentials are taken as 2^(z log2(e) / T - c) with one fused multiply-add.
-// Measured (us, TB/s of what a pass cannot do without; a copy reaches 6.1, reading alone 6.2): log probabilities with 32
-// alternatives 4096 x 100000 bf16 179 (4.6), of which their selection 17 and the join of four pieces 14; loss and gradient 4096 x 32768
-// bf16 107 (5.0); loss 2048 x 50001 f16 41 (5.0); gradient 1024 x 131072 fp32 190 (5.6).
+// Measured (us of a pass among others, TB/s of what it cannot do without; a copy reaches 6.1, reading alone 6.2): log probabilities with 32
+// alternatives 4096 x 100000 bf16 174 (4.7), of which the alternatives 32, 11 of them the join of four pieces; loss and gradient 4096 x 32768
+// bf16 113 (4.8); loss 2048 x 50001 f16 39 (5.3); gradient 1024 x 131072 fp32 188 (5.7).
 #pragma once
 #include "op_common.h"
 #include "../../../include/comp_ams_operators.h"

@@ -10,6 +10,9 @@ worker, as a rule views of the gradient buffer [n, d] that CompAms.step takes:
     y, mean, rstd = layer_norm(x, gain, shift)
     dx = layer_norm_backward(dy, x, mean, rstd, gain, grads[:, a:a + c], grads[:, a + c:a + 2 * c])
 
+No graph is recorded for automatic differentiation: results do not require a gradient, also where inputs do, and each
+backward pass is a call of its own.
+
 Arguments that the library would not take raise ValueError before anything is launched; what the library itself refuses
 raises CompAmsError.
 """
