@@ -238,8 +238,8 @@ int distill_check(const char *what, const void *logits, const int32_t *idx, cons
 {
     if (const int rc = vocab_check(what, logits, rows, vocab, stride, type)) return rc;
     REQUIRE(k >= 1 && k <= COMP_AMS_MAX_TOP, "%s: k=%d must be in [1, %d]", what, k, COMP_AMS_MAX_TOP);
-    REQUIRE(std::isfinite(temperature) && temperature > 0.f && std::isfinite(1.f / temperature),
-            "%s: temperature must be positive and finite", what);
+    REQUIRE(std::isfinite(temperature) && temperature > 0.f && std::isfinite(1.f / temperature * kLog2e),
+            "%s: temperature must be positive and finite, and so must its reciprocal in units of log 2", what);
     REQUIRE((idx && val) || rows == 0, "%s: idx or val is NULL", what);
     REQUIRE(aligned(idx, 4) && aligned(val, 4), "%s: idx and val must be 4-byte aligned", what);
     return COMP_AMS_OK;

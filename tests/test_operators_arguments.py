@@ -1,4 +1,6 @@
 """What the operators' Python entry points make of their arguments before they ask for a GPU."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -30,3 +32,12 @@ def test_bounds_have_one_dimension():
     for bounds in ([[1, 2]], np.zeros((2, 2), dtype=np.int32)):
         with pytest.raises(ValueError, match="one-dimensional"):
             operators._bounds(bounds)
+
+
+def test_a_temperature_whose_reciprocal_leaves_fp32_in_units_of_log_2_is_refused():
+    rows = C.c_int64(0)                                          # nothing to do: what is not refused returns at once
+    for call in (lambda t: P.lib().comp_ams_distill(None, None, None, None, None, rows, 100, 100, 5, t, 0, None),
+                 lambda t: P.lib().comp_ams_distill_backward(None, None, None, None, None, None, rows, 100, 100, 100, 5, t, 0, None),
+                 lambda t: P.lib().comp_ams_distill_grad(None, None, None, None, None, None, rows, 100, 100, 100, 5, t, 0, None)):
+        assert call(3.5e-39) == P.EINVAL and call(1e-45) == P.EINVAL
+        assert call(1e-38) == P.OK and call(1.0) == P.OK
