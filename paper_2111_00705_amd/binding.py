@@ -38,6 +38,9 @@ EXPORTS = [
     "comp_ams_rel_bias_softmax_backward", "comp_ams_rel_bias_work_bytes", "comp_ams_token_logprobs",
     "comp_ams_token_logprobs_work_bytes", "comp_ams_distill", "comp_ams_distill_backward",
     "comp_ams_distill_grad", "comp_ams_operators_last_error",
+    "comp_ams_quantize_rows", "comp_ams_restore_rows", "comp_ams_rms_norm", "comp_ams_rms_norm_q8", "comp_ams_rms_norm_backward",
+    "comp_ams_rms_norm_work_bytes", "comp_ams_linear_q8", "comp_ams_linear_q8_work_bytes", "comp_ams_linear_weight_grad",
+    "comp_ams_linear_weight_grad_work_bytes",
 ]
 
 
@@ -117,6 +120,16 @@ def lib():
         L.comp_ams_distill.argtypes = [vp] * 5 + [i64] * 3 + [i32, f32, i32, vp]
         L.comp_ams_distill_backward.argtypes = [vp] * 6 + [i64] * 4 + [i32, f32, i32, vp]
         L.comp_ams_distill_grad.argtypes = [vp] * 6 + [i64] * 4 + [i32, f32, i32, vp]
+        L.comp_ams_quantize_rows.argtypes = [vp] * 3 + [i64] * 4 + [i32, i32, vp]
+        L.comp_ams_restore_rows.argtypes = [vp] * 3 + [i64] * 4 + [i32, vp]
+        L.comp_ams_rms_norm.argtypes = [vp] * 6 + [i64] * 6 + [f32, i32, vp]
+        L.comp_ams_rms_norm_q8.argtypes = [vp] * 7 + [i64] * 6 + [f32, i32, i32, vp]
+        L.comp_ams_rms_norm_backward.argtypes = [vp] * 8 + [i64] * 6 + [i32, i64, i32, i32, vp, u64, vp]
+        L.comp_ams_rms_norm_work_bytes.argtypes = [i64, i64, i32, C.POINTER(u64)]
+        L.comp_ams_linear_q8.argtypes = [vp] * 6 + [i64] * 6 + [i32, vp, u64, vp]
+        L.comp_ams_linear_q8_work_bytes.argtypes = [i64, i64, i64, C.POINTER(u64)]
+        L.comp_ams_linear_weight_grad.argtypes = [vp] * 5 + [i64] * 5 + [i32, i64, i32, i32, i32, i32, vp, u64, vp]
+        L.comp_ams_linear_weight_grad_work_bytes.argtypes = [i64, i64, i64, i32, i32, i32, C.POINTER(u64)]
         L.comp_ams_operators_last_error.argtypes = []
         L.comp_ams_operators_last_error.restype = C.c_char_p
         _lib = L

@@ -9,12 +9,14 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcomp_ams.so")
 OPS = os.path.join(CSRC, "ops")
-SOURCES = [os.path.join(CSRC, "comp_ams.hip"), os.path.join(OPS, "operators.hip")]
+SOURCES = [os.path.join(CSRC, "comp_ams.hip"), os.path.join(OPS, "operators.hip"), os.path.join(OPS, "rows8.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in ("device_utils.h", "blocksign_kernels.h", "topk_kernels.h", "plain_kernels.h", "launch_rules.h")] + [
     os.path.join(os.path.dirname(HERE), "include", "comp_ams.h"),
     os.path.join(os.path.dirname(HERE), "include", "comp_ams_tuning.h"),
-    os.path.join(os.path.dirname(HERE), "include", "comp_ams_operators.h")] + [
-    os.path.join(OPS, f) for f in ("op_common.h", "norm_kernels.h", "bias_kernels.h", "vocab_kernels.h")]
+    os.path.join(os.path.dirname(HERE), "include", "comp_ams_operators.h"),
+    os.path.join(os.path.dirname(HERE), "include", "comp_ams_rows8.h")] + [
+    os.path.join(OPS, f) for f in ("op_common.h", "norm_kernels.h", "bias_kernels.h", "vocab_kernels.h", "op_host.h", "rows8.h", "rms_kernels.h",
+                                    "product8_kernels.h", "weight_kernels.h")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

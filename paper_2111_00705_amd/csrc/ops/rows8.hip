@@ -1,0 +1,503 @@
+// Host side of include/comp_ams_rows8.h: argument validation, the choice of kernels, launches.
+#include "../../../include/comp_ams_rows8.h"
+
+#include "op_host.h"
+
+#include "product8_kernels.h"
+#include "rms_kernels.h"
+#include "rows8.h"
+#include "weight_kernels.h"
+
+using namespace cams_ops;
+
+namespace {
+
+// Rows of int8: any alignment.
+#define REQUIRE_BYTE_ROWS(what, name, p, rows, cols, stride)                                                                   \
+    do {                                                                                                                       \
+        REQUIRE((p) != nullptr || (rows) == 0 || (cols) == 0, "%s: %s is NULL", what, name);                                   \
+        REQUIRE((stride) >= (cols) || (rows) <= 1, "%s: the rows of %s overlap (stride %lld < %lld)", what, name,              \
+                (long long)(stride), (long long)(cols));                                                                       \
+        REQUIRE((stride) >= 0 && ((rows) <= 1 || (stride) < kMaxElements / (rows)), "%s: %s is out of range", what, name);     \
+    } while (0)
+
+constexpr int64_t kLimit31 = (int64_t)1 << 31;
+
+int rows8_check(const char *what, int64_t rows, int64_t cols, const float *scale, int32_t type)
+{
+    REQUIRE(known_type(type), "%s: unknown type %d", what, type);
+    REQUIRE(rows >= 0 && rows < kLimit31, "%s: rows=%lld must be in [0, 2^31)", what, (long long)rows);
+    REQUIRE(cols >= 0 && cols < kLimit31, "%s: cols=%lld must be in [0, 2^31)", what, (long long)cols);
+    REQUIRE(scale || rows == 0, "%s: scale is NULL", what);
+    REQUIRE(aligned(scale, 4), "%s: scale must be 4-byte aligned", what);
+    return COMP_AMS_OK;
+}
+
+// --- the norm --------------------------------------------------------------------------------------------------------
+
+int rms_check(const char *what, int64_t rows, int64_t cols, int32_t type)
+{
+    REQUIRE(known_type(type), "%s: unknown type %d", what, type);
+    REQUIRE(rows >= 0 && rows < (int64_t)1 << 40, "%s: rows=%lld must be in [0, 2^40)", what, (long long)rows);
+    REQUIRE(cols >= 1 && cols < kLimit31, "%s: cols=%lld must be in [1, 2^31)", what, (long long)cols);
+    return COMP_AMS_OK;
+}
+
+constexpr int64_t kRmsBlocks = 2048;         // workgroups of the forward pass
+constexpr int64_t kRmsChunkBlocks = 1024;    // workgroups that the rows of all workers are cut into in the backward pass
+
+// How a worker's rows are cut for the gain's gradients: chunks of rows with one set of column sums each.
+struct RmsChunks {
+    int64_t rows, count;     // rows of a chunk; chunks of a worker
+};
+RmsChunks rms_chunks(int64_t worker_rows, int32_t n)
+{
+    const int64_t want = std::max<int64_t>(1, ceil_div(kRmsChunkBlocks, n));
+    const int64_t rows = std::max<int64_t>(16, ceil_div(worker_rows, want));
+    return {rows, std::max<int64_t>(1, ceil_div(worker_rows, rows))};
+}
+
+int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rstd, const void *x, const void *residual, const float *gain,
+                     const RmsArgs &a, bool q8, int32_t type, hipStream_t stream)
+{
+    if (a.rows == 0) return COMP_AMS_OK;
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        auto call = [&](auto eight) {
+            constexpr bool k8 = decltype(eight)::value;
+            const bool held = with_team<T>(a.cols, [&](auto shape) {
+                using S = decltype(shape);
+                const int64_t teams = kTeamBlock<S::threads> / S::threads;
+                rms_forward<T, S::threads, S::vecs, k8><<<(unsigned)std::min<int64_t>(ceil_div(a.rows, teams), kRmsBlocks), kTeamBlock<S::threads>, 0, stream>>>(
+                    y, scale, static_cast<T *>(h), rstd, static_cast<const T *>(x), static_cast<const T *>(residual), gain, a);
+            });
+            if (!held)
+                rms_forward_any<T, k8><<<(unsigned)std::min(a.rows, most_blocks(kRmsThreads)), kRmsThreads, 0, stream>>>(
+                    y, scale, static_cast<T *>(h), rstd, static_cast<const T *>(x), static_cast<const T *>(residual), gain, a);
+        };
+        if (q8) call(std::true_type{});
+        else call(std::false_type{});
+    });
+    return launched(what);
+}
+
+#define REQUIRE_RMS_FORWARD(what)                                                                                              \
+    do {                                                                                                                       \
+        if (const int rc = rms_check(what, rows, cols, type)) return rc;                                                       \
+        REQUIRE_ROWS(what, "x", x, rows, cols, x_stride, type);                                                                \
+        if (residual) REQUIRE_ROWS(what, "residual", residual, rows, cols, residual_stride, type);                             \
+        if (h) REQUIRE_ROWS(what, "h", h, rows, cols, h_stride, type);                                                         \
+        REQUIRE(gain, "%s: gain is NULL", what);                                                                               \
+        REQUIRE(aligned(gain, 4) && aligned(rstd, 4), "%s: gain and rstd must be 4-byte aligned", what);                       \
+        REQUIRE(std::isfinite(eps) && eps >= 0.f, "%s: eps must be finite and not negative", what);                            \
+    } while (0)
+
+// --- the product -----------------------------------------------------------------------------------------------------
+
+// Which kernel takes a product, and into how many pieces k is cut.
+struct ProductShape {
+    int few;                 // tokens in sixteens for product8_few, or 0
+    int tile;                // tokens and channels of a tile
+    int splits, k_split;
+    int64_t tiles_m, tiles_n;
+};
+ProductShape product_shape(int64_t rows, int64_t cols, int64_t outs)
+{
+    if (rows <= 64) return {rows <= 16 ? 1 : rows <= 32 ? 2 : 4, 0, 1, 0, 1, ceil_div(outs, 16)};
+    ProductShape s = {0, 256, 1, 0, ceil_div(rows, 256), ceil_div(outs, 256)};
+    if (s.tiles_m * s.tiles_n < 200) s = {0, 128, 1, 0, ceil_div(rows, 128), ceil_div(outs, 128)};
+    const int64_t tiles = s.tiles_m * s.tiles_n, steps = ceil_div(std::max<int64_t>(cols, 1), kProductStep);
+    int64_t pieces = 1;
+    if (s.tile == 128 && tiles < 256) pieces = std::max<int64_t>(1, std::min(512 / tiles, steps / 4));
+    s.k_split = (int)(ceil_div(steps, pieces) * kProductStep);
+    s.splits = (int)ceil_div(steps * kProductStep, s.k_split);
+    return s;
+}
+
+int product_check(const char *what, int64_t rows, int64_t cols, int64_t outs)
+{
+    REQUIRE(rows >= 0 && rows < kLimit31, "%s: rows=%lld must be in [0, 2^31)", what, (long long)rows);
+    REQUIRE(outs >= 0 && outs < kLimit31, "%s: outs=%lld must be in [0, 2^31)", what, (long long)outs);
+    REQUIRE(cols >= 0 && cols < COMP_AMS_MAX_Q8_COLS, "%s: cols=%lld must be in [0, %d)", what, (long long)cols, COMP_AMS_MAX_Q8_COLS);
+    const ProductShape s = product_shape(rows, cols, outs);
+    REQUIRE(s.tiles_m * s.tiles_n * s.splits <= kMaxBlocks, "%s: rows and outs are too many for one call", what);
+    return COMP_AMS_OK;
+}
+
+// --- weight gradients --------------------------------------------------------------------------------------------------
+
+struct WeightShape {
+    int tile;                // input and output channels of a tile
+    int64_t tiles_i, tiles_o;
+    int64_t splits, split_rows;          // pieces of a worker's rows, rows of a piece
+    int64_t bias_chunks, bias_rows;      // the same for the bias
+};
+WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n)
+{
+    const int64_t per = rows / n;
+    WeightShape s = {256, ceil_div(cols, 256), ceil_div(outs, 256), 1, 0, 1, 0};
+    if (s.tiles_i * s.tiles_o * n < 200) s.tile = 128, s.tiles_i = ceil_div(cols, 128), s.tiles_o = ceil_div(outs, 128);
+    const int64_t tiles = s.tiles_i * s.tiles_o * n, steps = std::max<int64_t>(1, ceil_div(per, kWeightStep));
+    int64_t pieces = 1;
+    if (s.tile == 128 && tiles > 0 && tiles < 256) pieces = std::max<int64_t>(1, std::min(512 / tiles, steps / 8));
+    s.split_rows = ceil_div(steps, pieces) * kWeightStep;
+    s.splits = std::max<int64_t>(1, ceil_div(per, s.split_rows));
+    const int64_t want = std::max<int64_t>(1, 1024 / (n * ceil_div(std::max<int64_t>(outs, 1), kRmsThreads)));
+    s.bias_rows = std::max<int64_t>(16, ceil_div(per, want));
+    s.bias_chunks = std::max<int64_t>(1, ceil_div(per, s.bias_rows));
+    return s;
+}
+uint64_t weight_bias_bytes(const WeightShape &s, int64_t outs, int32_t n)
+{
+    return (uint64_t)(ceil_div(s.bias_chunks * n * outs, 4) * 16);
+}
+
+int weight_check(const char *what, int64_t rows, int64_t cols, int64_t outs, int32_t n, int32_t type)
+{
+    REQUIRE(known_type(type), "%s: unknown type %d", what, type);
+    REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
+    REQUIRE(rows >= 0 && rows < (int64_t)1 << 40 && rows / n < kLimit31 - 65536, "%s: rows=%lld are too many", what, (long long)rows);
+    REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
+    REQUIRE(cols >= 0 && cols < kLimit31 && outs >= 0 && outs < kLimit31 && cols * outs < (int64_t)1 << 40,
+            "%s: cols=%lld or outs=%lld is out of range", what, (long long)cols, (long long)outs);
+    const WeightShape s = weight_shape(rows, cols, outs, n);
+    REQUIRE(s.tiles_i * s.tiles_o <= kMaxBlocks / n / s.splits, "%s: cols, outs and n are too many for one call", what);
+    return COMP_AMS_OK;
+}
+
+// Which kernel, and its launch, for a result of type G.
+template <typename G>
+void weight_launch(G *out, const void *dy, const int8_t *q, const float *scale, WeightArgs a, int tile, bool in_first, bool binary, int32_t type,
+                   hipStream_t stream)
+{
+    const int64_t blocks = (int64_t)a.tiles_i * a.tiles_o * a.n * a.splits;
+    auto run = [&](auto t, auto one, auto first_in) {
+        using T = decltype(t);
+        constexpr bool kOne = decltype(one)::value, kIn = decltype(first_in)::value;
+        auto go = [&](auto kernel, int threads) {
+            in_launches(blocks, threads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                kernel<<<count, threads, 0, stream>>>(out, static_cast<const T *>(dy), q, scale, a);
+            });
+        };
+        if (tile == 256) go(weight_grad<T, G, kOne, kIn, 256, 256, 2, 4>, 512);
+        else go(weight_grad<T, G, kOne, kIn, 128, 128, 2, 2>, 256);
+    };
+    auto sided = [&](auto t, auto one) {
+        if (in_first) run(t, one, std::true_type{});
+        else run(t, one, std::false_type{});
+    };
+    if (type == COMP_AMS_BF16) {
+        if (binary) sided(bf16_t{}, std::true_type{});
+        else sided(bf16_t{}, std::false_type{});
+    } else if (type == COMP_AMS_F16) {
+        sided(f16_t{}, std::false_type{});
+    } else {
+        sided(float{}, std::false_type{});
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+int comp_ams_quantize_rows(int8_t *q, float *scale, const void *x, int64_t rows, int64_t cols, int64_t q_stride, int64_t x_stride,
+                           int32_t binary, int32_t type, void *hip_stream)
+{
+    const char *what = "quantize_rows";
+    if (const int rc = rows8_check(what, rows, cols, scale, type)) return rc;
+    REQUIRE_BYTE_ROWS(what, "q", q, rows, cols, q_stride);
+    REQUIRE_ROWS(what, "x", x, cols ? rows : 0, cols, x_stride, type);
+    if (rows == 0) return COMP_AMS_OK;
+    QuantArgs a = {rows, cols, x_stride, q_stride, binary != 0, streamed_in(rows * cols, type), 0};
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        const bool held = with_team<T>(cols, [&](auto shape) {
+            using S = decltype(shape);
+            in_launches(ceil_div(rows, kTeamBlock<S::threads> / S::threads), kTeamBlock<S::threads>, [&](unsigned first, unsigned count) {
+                a.first = first;
+                quantize<T, S::threads, S::vecs><<<count, kTeamBlock<S::threads>, 0, stream>>>(q, scale, static_cast<const T *>(x), a);
+            });
+        });
+        if (!held)
+            quantize_any<T><<<(unsigned)std::min(rows, most_blocks(kQuantThreads)), kQuantThreads, 0, stream>>>(q, scale, static_cast<const T *>(x), a);
+    });
+    return launched(what);
+}
+
+int comp_ams_restore_rows(void *x, const int8_t *q, const float *scale, int64_t rows, int64_t cols, int64_t x_stride, int64_t q_stride,
+                          int32_t type, void *hip_stream)
+{
+    const char *what = "restore_rows";
+    if (const int rc = rows8_check(what, rows, cols, scale, type)) return rc;
+    REQUIRE_BYTE_ROWS(what, "q", q, rows, cols, q_stride);
+    REQUIRE_ROWS(what, "x", x, cols ? rows : 0, cols, x_stride, type);
+    if (rows == 0 || cols == 0) return COMP_AMS_OK;
+    QuantArgs a = {rows, cols, x_stride, q_stride, false, streamed_out(rows * cols, type), 0};
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        const bool held = with_team<T>(cols, [&](auto shape) {
+            using S = decltype(shape);
+            in_launches(ceil_div(rows, kTeamBlock<S::threads> / S::threads), kTeamBlock<S::threads>, [&](unsigned first, unsigned count) {
+                a.first = first;
+                restore<T, S::threads, S::vecs><<<count, kTeamBlock<S::threads>, 0, stream>>>(static_cast<T *>(x), q, scale, a);
+            });
+        });
+        if (!held)
+            restore_any<T><<<(unsigned)std::min(rows, most_blocks(kQuantThreads)), kQuantThreads, 0, stream>>>(static_cast<T *>(x), q, scale, a);
+    });
+    return launched(what);
+}
+
+int comp_ams_rms_norm(void *y, void *h, float *rstd, const void *x, const void *residual, const float *gain, int64_t rows, int64_t cols,
+                      int64_t y_stride, int64_t h_stride, int64_t x_stride, int64_t residual_stride, float eps, int32_t type,
+                      void *hip_stream)
+{
+    const char *what = "rms_norm";
+    REQUIRE_RMS_FORWARD(what);
+    REQUIRE_ROWS(what, "y", y, rows, cols, y_stride, type);
+    REQUIRE(!h || h != y || rows == 0, "%s: y and h are the same array", what);
+    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, y_stride, eps, (float)(1.0 / (double)cols), false, streamed_out(rows * cols, type)};
+    return rms_forward_call(what, y, nullptr, h, rstd, x, residual, gain, a, false, type, static_cast<hipStream_t>(hip_stream));
+}
+
+int comp_ams_rms_norm_q8(int8_t *q, float *scale, void *h, float *rstd, const void *x, const void *residual, const float *gain,
+                         int64_t rows, int64_t cols, int64_t q_stride, int64_t h_stride, int64_t x_stride, int64_t residual_stride,
+                         float eps, int32_t binary, int32_t type, void *hip_stream)
+{
+    const char *what = "rms_norm_q8";
+    REQUIRE_RMS_FORWARD(what);
+    REQUIRE_BYTE_ROWS(what, "q", q, rows, cols, q_stride);
+    REQUIRE(scale || rows == 0, "%s: scale is NULL", what);
+    REQUIRE(aligned(scale, 4), "%s: scale must be 4-byte aligned", what);
+    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, q_stride, eps, (float)(1.0 / (double)cols), binary != 0, streamed_out(rows * cols, type)};
+    return rms_forward_call(what, q, scale, h, rstd, x, residual, gain, a, true, type, static_cast<hipStream_t>(hip_stream));
+}
+
+int comp_ams_rms_norm_work_bytes(int64_t rows, int64_t cols, int32_t n, uint64_t *bytes)
+{
+    const char *what = "rms_norm_work_bytes";
+    if (const int rc = rms_check(what, rows, cols, COMP_AMS_F32)) return rc;
+    REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
+    REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
+    REQUIRE(bytes, "%s: bytes is NULL", what);
+    *bytes = (uint64_t)rms_chunks(rows / n, n).count * (uint64_t)n * (uint64_t)cols * sizeof(float);
+    return COMP_AMS_OK;
+}
+
+int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void *h, const float *h_scale, const float *rstd,
+                               const float *gain, const void *dresidual, int64_t rows, int64_t cols, int64_t dx_stride,
+                               int64_t dy_stride, int64_t h_stride, int64_t dresidual_stride, int32_t n, int64_t grad_stride,
+                               int32_t type, int32_t grad_type, void *work, uint64_t work_bytes, void *hip_stream)
+{
+    const char *what = "rms_norm_backward";
+    if (const int rc = rms_check(what, rows, cols, type)) return rc;
+    REQUIRE(known_type(grad_type), "%s: unknown gradient type %d", what, grad_type);
+    REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
+    REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
+    if (h_scale) REQUIRE_BYTE_ROWS(what, "h", h, rows, cols, h_stride);
+    else REQUIRE_ROWS(what, "h", h, rows, cols, h_stride, type);
+    REQUIRE_ROWS(what, "dy", dy, rows, cols, dy_stride, type);
+    REQUIRE_ROWS(what, "dx", dx, rows, cols, dx_stride, type);
+    if (dresidual) REQUIRE_ROWS(what, "dresidual", dresidual, rows, cols, dresidual_stride, type);
+    REQUIRE_ROWS(what, "dgain", dgain, (int64_t)n, cols, grad_stride, grad_type);
+    REQUIRE(gain && (rstd || rows == 0), "%s: rstd or gain is NULL", what);
+    REQUIRE(aligned(gain, 4) && aligned(rstd, 4) && aligned(h_scale, 4), "%s: rstd, gain and h_scale must be 4-byte aligned", what);
+    uint64_t need = 0;
+    if (const int rc = comp_ams_rms_norm_work_bytes(rows, cols, n, &need)) return rc;
+    REQUIRE(work && work_bytes >= need, "%s: needs %llu bytes of work memory", what, (unsigned long long)need);
+    REQUIRE(aligned(work, 16), "%s: work must be 16-byte aligned", what);
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const RmsBackArgs a = {rows, cols, dx_stride, dy_stride, h_stride, dresidual_stride, (float)(1.0 / (double)cols), streamed_out(rows * cols, type)};
+    const RmsChunks ch = rms_chunks(rows / n, n);
+    float *sums = static_cast<float *>(work);
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        auto call = [&](auto kept) {
+            using H = decltype(kept);
+            const T *dyt = static_cast<const T *>(dy), *rt = static_cast<const T *>(dresidual);
+            const H *ht = static_cast<const H *>(h);
+            const bool held = with_team<T>(cols, [&](auto shape) {
+                using S = decltype(shape);
+                rms_backward<T, H, S::threads, S::vecs><<<dim3((unsigned)ch.count, (unsigned)n), kTeamBlock<S::threads>, 0, stream>>>(
+                    static_cast<T *>(dx), sums, dyt, ht, h_scale, rstd, gain, rt, a, rows / n, ch.rows);
+            });
+            if (held) return;
+            // the gain's gradients first: dx may replace dy or h
+            rms_param_any<T, H><<<dim3((unsigned)ceil_div(cols, kRmsThreads), (unsigned)ch.count, (unsigned)n), kRmsThreads, 0, stream>>>(
+                sums, dyt, ht, h_scale, rstd, a, rows / n, ch.rows);
+            if (rows > 0)
+                rms_backward_any<T, H><<<(unsigned)std::min(rows, most_blocks(kRmsThreads)), kRmsThreads, 0, stream>>>(static_cast<T *>(dx), dyt, ht,
+                                                                                                                      h_scale, rstd, gain, rt, a);
+        };
+        if (h_scale) call(int8_t{});
+        else call(T{});
+    });
+    if (const int rc = launched(what)) return rc;              // what the join would read has not been written
+    with_type(grad_type, [&](auto t) {
+        using G = decltype(t);
+        in_launches(ceil_div(cols, kColumnsJoin), kRmsThreads, [&](unsigned first, unsigned count) {
+            columns_join<G><<<dim3(count, (unsigned)n), kRmsThreads, 0, stream>>>(static_cast<G *>(dgain), sums, cols, (int)ch.count, grad_stride, first);
+        });
+    });
+    return launched(what);
+}
+
+int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, uint64_t *bytes)
+{
+    const char *what = "linear_q8_work_bytes";
+    if (const int rc = product_check(what, rows, cols, outs)) return rc;
+    REQUIRE(bytes, "%s: bytes is NULL", what);
+    const ProductShape s = product_shape(rows, cols, outs);
+    *bytes = s.splits > 1 ? (uint64_t)s.splits * (uint64_t)rows * (uint64_t)outs * sizeof(int32_t) : 0;
+    return COMP_AMS_OK;
+}
+
+int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_t *w, const float *w_scale, const float *bias,
+                       int64_t rows, int64_t cols, int64_t outs, int64_t y_stride, int64_t q_stride, int64_t w_stride, int32_t type,
+                       void *work, uint64_t work_bytes, void *hip_stream)
+{
+    const char *what = "linear_q8";
+    REQUIRE(known_type(type), "%s: unknown type %d", what, type);
+    if (const int rc = product_check(what, rows, cols, outs)) return rc;
+    REQUIRE_BYTE_ROWS(what, "q", q, rows, cols, q_stride);
+    REQUIRE_BYTE_ROWS(what, "w", w, outs, cols, w_stride);
+    REQUIRE_ROWS(what, "y", y, outs ? rows : 0, outs, y_stride, type);
+    REQUIRE((scale || rows == 0) && (w_scale || outs == 0), "%s: a scale is NULL", what);
+    REQUIRE(aligned(scale, 4) && aligned(w_scale, 4) && aligned(bias, 4), "%s: scales and bias must be 4-byte aligned", what);
+    uint64_t need = 0;
+    if (const int rc = comp_ams_linear_q8_work_bytes(rows, cols, outs, &need)) return rc;
+    REQUIRE(need == 0 || (work && work_bytes >= need && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
+            (unsigned long long)need);
+    if (rows == 0 || outs == 0) return COMP_AMS_OK;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const ProductShape s = product_shape(rows, cols, outs);
+    ProductArgs a = {rows, outs, q_stride, w_stride, y_stride, (int)cols, (int)s.tiles_m, (int)s.tiles_n, s.splits, s.k_split, 0};
+    const int64_t blocks = s.tiles_m * s.tiles_n * s.splits;
+    // memory to LDS without registers: whole 16-byte chunks, and a tile's rows within 31 bits
+    const int64_t most_stride = kLimit31 / 512;
+    const bool direct = aligned(q, 16) && aligned(w, 16) && cols % 16 == 0 && (rows == 1 || (q_stride % 16 == 0 && q_stride < most_stride)) &&
+                        (outs == 1 || (w_stride % 16 == 0 && w_stride < most_stride));
+    int rc = COMP_AMS_OK;
+    with_type(type, [&](auto t) {
+        using Y = decltype(t);
+        Y *yt = static_cast<Y *>(y);
+        if (s.few) {
+            auto go = [&](auto kernel) {
+                in_launches(blocks, kFewWaves * kWave, [&](unsigned first, unsigned count) {
+                    a.first = first;
+                    kernel<<<count, kFewWaves * kWave, 0, stream>>>(yt, q, scale, w, w_scale, bias, a);
+                });
+            };
+            if (s.few == 1) go(product8_few<Y, 1>);
+            else if (s.few == 2) go(product8_few<Y, 2>);
+            else go(product8_few<Y, 4>);
+            return;
+        }
+        auto go = [&](auto kernel, int threads) {
+            in_launches(blocks, threads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                kernel<<<count, threads, 0, stream>>>(yt, static_cast<int *>(work), q, scale, w, w_scale, bias, a);
+            });
+        };
+        if (s.splits > 1) {
+            if (direct) go(product8<Y, 128, 128, 2, 2, true, true>, 256);
+            else go(product8<Y, 128, 128, 2, 2, false, true>, 256);
+            rc = launched(what);                               // unless it is good, what the join would read has not been written
+            if (rc) return;
+            in_launches(ceil_div(ceil_div(outs, 4) * rows, kProductThreads), kProductThreads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                product8_join<Y><<<count, kProductThreads, 0, stream>>>(yt, static_cast<const int *>(work), scale, w_scale, bias, a);
+            });
+        } else if (s.tile == 256) {
+            if (direct) go(product8<Y, 256, 256, 2, 4, true, false>, 512);
+            else go(product8<Y, 256, 256, 2, 4, false, false>, 512);
+        } else {
+            if (direct) go(product8<Y, 128, 128, 2, 2, true, false>, 256);
+            else go(product8<Y, 128, 128, 2, 2, false, false>, 256);
+        }
+    });
+    return rc ? rc : launched(what);
+}
+
+int comp_ams_linear_weight_grad_work_bytes(int64_t rows, int64_t cols, int64_t outs, int32_t n, int32_t binary, int32_t type, uint64_t *bytes)
+{
+    const char *what = "linear_weight_grad_work_bytes";
+    (void)binary;
+    if (const int rc = weight_check(what, rows, cols, outs, n, type)) return rc;
+    REQUIRE(bytes, "%s: bytes is NULL", what);
+    const WeightShape s = weight_shape(rows, cols, outs, n);
+    *bytes = weight_bias_bytes(s, outs, n) + (s.splits > 1 ? (uint64_t)(s.splits * n) * (uint64_t)(cols * outs) * sizeof(float) : 0);
+    return COMP_AMS_OK;
+}
+
+int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, const int8_t *q, const float *scale, int64_t rows,
+                                int64_t cols, int64_t outs, int64_t dy_stride, int64_t q_stride, int32_t n, int64_t grad_stride,
+                                int32_t in_first, int32_t binary, int32_t type, int32_t grad_type, void *work, uint64_t work_bytes,
+                                void *hip_stream)
+{
+    const char *what = "linear_weight_grad";
+    if (const int rc = weight_check(what, rows, cols, outs, n, type)) return rc;
+    REQUIRE(known_type(grad_type), "%s: unknown gradient type %d", what, grad_type);
+    REQUIRE_BYTE_ROWS(what, "q", q, rows, cols, q_stride);
+    REQUIRE_ROWS(what, "dy", dy, outs ? rows : 0, outs, dy_stride, type);
+    REQUIRE_ROWS(what, "dweight", dweight, cols && outs ? (int64_t)n : 0, cols * outs, grad_stride, grad_type);
+    if (dbias) REQUIRE_ROWS(what, "dbias", dbias, (int64_t)n, outs, grad_stride, grad_type);
+    REQUIRE(scale || rows == 0, "%s: scale is NULL", what);
+    REQUIRE(aligned(scale, 4), "%s: scale must be 4-byte aligned", what);
+    uint64_t need = 0;
+    if (const int rc = comp_ams_linear_weight_grad_work_bytes(rows, cols, outs, n, binary, type, &need)) return rc;
+    REQUIRE(need == 0 || (work && work_bytes >= need && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
+            (unsigned long long)need);
+    if (outs == 0) return COMP_AMS_OK;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const WeightShape s = weight_shape(rows, cols, outs, n);
+    float *bias_sums = static_cast<float *>(work);
+    float *sums = reinterpret_cast<float *>(static_cast<char *>(work) + weight_bias_bytes(s, outs, n));
+    const int64_t cells = cols * outs, per = rows / n;
+    if (cells) {
+        WeightArgs a = {};
+        a.cols = cols, a.outs = outs, a.dy_stride = dy_stride, a.q_stride = q_stride;
+        a.worker_rows = per, a.split_rows = s.split_rows;
+        a.out_stride = in_first ? outs : cols;
+        a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.splits = (int)s.splits;
+        if (s.splits > 1) {
+            a.worker_stride = cells, a.piece_stride = cells * n;
+            weight_launch<float>(sums, dy, q, scale, a, s.tile, in_first != 0, binary != 0, type, stream);
+            if (const int rc = launched(what)) return rc;      // what the join would read has not been written
+        } else {
+            a.worker_stride = grad_stride;
+        }
+        with_type(grad_type, [&](auto t) {
+            using G = decltype(t);
+            if (s.splits == 1) {
+                weight_launch<G>(static_cast<G *>(dweight), dy, q, scale, a, s.tile, in_first != 0, binary != 0, type, stream);
+                return;
+            }
+            in_launches(ceil_div(cells, 4 * kWeightJoinThreads), kWeightJoinThreads, [&](unsigned first, unsigned count) {
+                weight_join<G><<<dim3(count, (unsigned)n), kWeightJoinThreads, 0, stream>>>(static_cast<G *>(dweight), sums, cells, (int)s.splits,
+                                                                                          cells * n, grad_stride, first);
+            });
+        });
+        if (const int rc = launched(what)) return rc;
+    }
+    if (!dbias) return COMP_AMS_OK;
+    with_type(type, [&](auto t) {
+        using T = decltype(t);
+        column_sums<T><<<dim3((unsigned)ceil_div(outs, kRmsThreads), (unsigned)s.bias_chunks, (unsigned)n), kRmsThreads, 0, stream>>>(
+            bias_sums, static_cast<const T *>(dy), outs, dy_stride, per, s.bias_rows);
+    });
+    if (const int rc = launched(what)) return rc;
+    with_type(grad_type, [&](auto t) {
+        using G = decltype(t);
+        in_launches(ceil_div(outs, kColumnsJoin), kRmsThreads, [&](unsigned first, unsigned count) {
+            columns_join<G><<<dim3(count, (unsigned)n), kRmsThreads, 0, stream>>>(static_cast<G *>(dbias), bias_sums, outs, (int)s.bias_chunks, grad_stride,
+                                                                                 first);
+        });
+    });
+    return launched(what);
+}
+
+}  // extern "C"
