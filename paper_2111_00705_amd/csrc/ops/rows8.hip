@@ -126,74 +126,103 @@ int product_check(const char *what, int64_t rows, int64_t cols, int64_t outs)
 
 // --- weight gradients --------------------------------------------------------------------------------------------------
 
+constexpr int64_t kMostChannels = (int64_t)1 << 23;      // a step's rows lie within 31 bits
+
+// How a call is cut, and where its work memory holds what.
 struct WeightShape {
     int tile;                // input and output channels of a tile
+    int planes;              // of dy
+    bool copied;             // dy is written anew
     int64_t tiles_i, tiles_o;
-    int64_t splits, split_rows;          // pieces of a worker's rows, rows of a piece
-    int64_t bias_chunks, bias_rows;      // the same for the bias
+    int64_t splits, split_steps;         // pieces of the sum over planes and steps of rows, steps of a piece
+    int64_t bias_chunks, bias_rows;      // pieces of a worker's rows for the bias, rows of a piece
+    int64_t a_ld, b_ld;
+    uint64_t a_at, b_at, sums_at, bias_at, bytes;
 };
-WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n)
+WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bool binary, int32_t type, bool dy_aligned)
 {
     const int64_t per = rows / n;
-    WeightShape s = {256, ceil_div(cols, 256), ceil_div(outs, 256), 1, 0, 1, 0};
+    WeightShape s = {};
+    s.planes = type == COMP_AMS_F32 ? 3 : type == COMP_AMS_BF16 && binary ? 1 : 2;
+    s.copied = s.planes > 1 || !dy_aligned || outs % 8 != 0;
+    s.tile = 256, s.tiles_i = ceil_div(cols, 256), s.tiles_o = ceil_div(outs, 256);
     if (s.tiles_i * s.tiles_o * n < 200) s.tile = 128, s.tiles_i = ceil_div(cols, 128), s.tiles_o = ceil_div(outs, 128);
-    const int64_t tiles = s.tiles_i * s.tiles_o * n, steps = std::max<int64_t>(1, ceil_div(per, kWeightStep));
+    const int64_t tiles = s.tiles_i * s.tiles_o * n, steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.planes);
     int64_t pieces = 1;
-    if (s.tile == 128 && tiles > 0 && tiles < 256) pieces = std::max<int64_t>(1, std::min(512 / tiles, steps / 8));
-    s.split_rows = ceil_div(steps, pieces) * kWeightStep;
-    s.splits = std::max<int64_t>(1, ceil_div(per, s.split_rows));
+    if (s.tile == 128 && tiles > 0 && tiles < 256) pieces = std::max<int64_t>(1, std::min(512 / tiles, steps / 4));
+    s.split_steps = ceil_div(steps, pieces);
+    s.splits = ceil_div(steps, s.split_steps);
     const int64_t want = std::max<int64_t>(1, 1024 / (n * ceil_div(std::max<int64_t>(outs, 1), kRmsThreads)));
     s.bias_rows = std::max<int64_t>(16, ceil_div(per, want));
     s.bias_chunks = std::max<int64_t>(1, ceil_div(per, s.bias_rows));
+    s.a_ld = ceil_div(cols, 8) * 8, s.b_ld = ceil_div(outs, 8) * 8;
+    const uint64_t a_bytes = (uint64_t)(rows * s.a_ld) * 2, b_bytes = s.copied ? (uint64_t)(s.planes * rows * s.b_ld) * 2 : 0;
+    const uint64_t sums = s.splits > 1 ? (uint64_t)(s.splits * n) * (uint64_t)(cols * outs) * sizeof(float) : 0;
+    s.a_at = 0;
+    s.b_at = s.a_at + a_bytes;
+    s.sums_at = s.b_at + b_bytes;
+    s.bias_at = s.sums_at + (sums + 15) / 16 * 16;
+    s.bytes = s.bias_at + (uint64_t)(s.bias_chunks * n * outs) * sizeof(float);
     return s;
 }
-uint64_t weight_bias_bytes(const WeightShape &s, int64_t outs, int32_t n)
-{
-    return (uint64_t)(ceil_div(s.bias_chunks * n * outs, 4) * 16);
-}
 
-int weight_check(const char *what, int64_t rows, int64_t cols, int64_t outs, int32_t n, int32_t type)
+int weight_check(const char *what, int64_t rows, int64_t cols, int64_t outs, int32_t n, int32_t binary, int32_t type)
 {
     REQUIRE(known_type(type), "%s: unknown type %d", what, type);
     REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
-    REQUIRE(rows >= 0 && rows < (int64_t)1 << 40 && rows / n < kLimit31 - 65536, "%s: rows=%lld are too many", what, (long long)rows);
+    REQUIRE(rows >= 0 && rows < (int64_t)1 << 35 && rows / n < kLimit31 / 4, "%s: rows=%lld are too many", what, (long long)rows);
     REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
-    REQUIRE(cols >= 0 && cols < kLimit31 && outs >= 0 && outs < kLimit31 && cols * outs < (int64_t)1 << 40,
-            "%s: cols=%lld or outs=%lld is out of range", what, (long long)cols, (long long)outs);
-    const WeightShape s = weight_shape(rows, cols, outs, n);
+    REQUIRE(cols >= 0 && cols <= kMostChannels && outs >= 0 && outs <= kMostChannels, "%s: cols=%lld or outs=%lld is out of range", what,
+            (long long)cols, (long long)outs);
+    const WeightShape s = weight_shape(rows, cols, outs, n, binary != 0, type, true);
     REQUIRE(s.tiles_i * s.tiles_o <= kMaxBlocks / n / s.splits, "%s: cols, outs and n are too many for one call", what);
     return COMP_AMS_OK;
 }
 
-// Which kernel, and its launch, for a result of type G.
+// Lanes that share a row of `eights` chunks.
+int prepare_lanes(int64_t eights)
+{
+    int lanes = 8;
+    while (lanes < kPrepareThreads && lanes < eights) lanes *= 2;
+    return lanes;
+}
+
+void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, const int8_t *q, const float *scale, int64_t rows, int64_t cols,
+                           int64_t outs, int64_t dy_stride, int64_t q_stride, bool binary, int32_t type, hipStream_t stream)
+{
+    PrepareArgs a = {rows, cols, outs, q_stride, dy_stride, s.a_ld, s.b_ld, rows * s.b_ld, prepare_lanes(s.a_ld / 8), prepare_lanes(s.b_ld / 8), 0, 0};
+    const int64_t blocks_a = ceil_div(rows, kPrepareThreads / a.lanes_a), blocks_b = s.copied ? ceil_div(rows, kPrepareThreads / a.lanes_b) : 0;
+    a.blocks_a = (unsigned)blocks_a;
+    auto go = [&](auto t, auto planes) {
+        using T = decltype(t);
+        in_launches(blocks_a + blocks_b, kPrepareThreads, [&](unsigned first, unsigned count) {
+            a.first = first;
+            weight_prepare<T, decltype(planes)::value><<<count, kPrepareThreads, 0, stream>>>(
+                reinterpret_cast<bf16_t *>(work + s.a_at), reinterpret_cast<bf16_t *>(work + s.b_at), static_cast<const T *>(dy), q, scale, a);
+        });
+    };
+    if (type == COMP_AMS_F32) go(float{}, std::integral_constant<int, 3>{});
+    else if (type == COMP_AMS_F16) go(f16_t{}, std::integral_constant<int, 2>{});
+    else if (binary) go(bf16_t{}, std::integral_constant<int, 1>{});
+    else go(bf16_t{}, std::integral_constant<int, 2>{});
+}
+
 template <typename G>
-void weight_launch(G *out, const void *dy, const int8_t *q, const float *scale, WeightArgs a, int tile, bool in_first, bool binary, int32_t type,
-                   hipStream_t stream)
+void weight_launch(G *out, const bf16_t *a_rows, const bf16_t *b_rows, WeightArgs a, int tile, bool in_first, hipStream_t stream)
 {
     const int64_t blocks = (int64_t)a.tiles_i * a.tiles_o * a.n * a.splits;
-    auto run = [&](auto t, auto one, auto first_in) {
-        using T = decltype(t);
-        constexpr bool kOne = decltype(one)::value, kIn = decltype(first_in)::value;
-        auto go = [&](auto kernel, int threads) {
-            in_launches(blocks, threads, [&](unsigned first, unsigned count) {
-                a.first = first;
-                kernel<<<count, threads, 0, stream>>>(out, static_cast<const T *>(dy), q, scale, a);
-            });
-        };
-        if (tile == 256) go(weight_grad<T, G, kOne, kIn, 256, 256, 2, 4>, 512);
-        else go(weight_grad<T, G, kOne, kIn, 128, 128, 2, 2>, 256);
+    auto go = [&](auto kernel, int threads) {
+        in_launches(blocks, threads, [&](unsigned first, unsigned count) {
+            a.first = first;
+            kernel<<<count, threads, 0, stream>>>(out, a_rows, b_rows, a);
+        });
     };
-    auto sided = [&](auto t, auto one) {
-        if (in_first) run(t, one, std::true_type{});
-        else run(t, one, std::false_type{});
-    };
-    if (type == COMP_AMS_BF16) {
-        if (binary) sided(bf16_t{}, std::true_type{});
-        else sided(bf16_t{}, std::false_type{});
-    } else if (type == COMP_AMS_F16) {
-        sided(f16_t{}, std::false_type{});
+    if (tile == 256) {
+        if (in_first) go(weight_grad<G, true, 256, 256, 2, 4>, 512);
+        else go(weight_grad<G, false, 256, 256, 2, 4>, 512);
     } else {
-        sided(float{}, std::false_type{});
+        if (in_first) go(weight_grad<G, true, 128, 128, 2, 2>, 256);
+        else go(weight_grad<G, false, 128, 128, 2, 2>, 256);
     }
 }
 
@@ -422,14 +451,13 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
     return rc ? rc : launched(what);
 }
 
-int comp_ams_linear_weight_grad_work_bytes(int64_t rows, int64_t cols, int64_t outs, int32_t n, int32_t binary, int32_t type, uint64_t *bytes)
+int comp_ams_linear_weight_grad_work_bytes(int64_t rows, int64_t cols, int64_t outs, int32_t n, int32_t binary, int32_t type, int32_t dy_aligned,
+                                           uint64_t *bytes)
 {
     const char *what = "linear_weight_grad_work_bytes";
-    (void)binary;
-    if (const int rc = weight_check(what, rows, cols, outs, n, type)) return rc;
+    if (const int rc = weight_check(what, rows, cols, outs, n, binary, type)) return rc;
     REQUIRE(bytes, "%s: bytes is NULL", what);
-    const WeightShape s = weight_shape(rows, cols, outs, n);
-    *bytes = weight_bias_bytes(s, outs, n) + (s.splits > 1 ? (uint64_t)(s.splits * n) * (uint64_t)(cols * outs) * sizeof(float) : 0);
+    *bytes = weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned != 0).bytes;
     return COMP_AMS_OK;
 }
 
@@ -439,7 +467,7 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
                                 void *hip_stream)
 {
     const char *what = "linear_weight_grad";
-    if (const int rc = weight_check(what, rows, cols, outs, n, type)) return rc;
+    if (const int rc = weight_check(what, rows, cols, outs, n, binary, type)) return rc;
     REQUIRE(known_type(grad_type), "%s: unknown gradient type %d", what, grad_type);
     REQUIRE_BYTE_ROWS(what, "q", q, rows, cols, q_stride);
     REQUIRE_ROWS(what, "dy", dy, outs ? rows : 0, outs, dy_stride, type);
@@ -447,25 +475,30 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
     if (dbias) REQUIRE_ROWS(what, "dbias", dbias, (int64_t)n, outs, grad_stride, grad_type);
     REQUIRE(scale || rows == 0, "%s: scale is NULL", what);
     REQUIRE(aligned(scale, 4), "%s: scale must be 4-byte aligned", what);
-    uint64_t need = 0;
-    if (const int rc = comp_ams_linear_weight_grad_work_bytes(rows, cols, outs, n, binary, type, &need)) return rc;
-    REQUIRE(need == 0 || (work && work_bytes >= need && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
-            (unsigned long long)need);
+    const bool dy_aligned = aligned(dy, 16) && (rows <= 1 || (dy_stride % 8 == 0 && dy_stride <= kMostChannels));
+    const WeightShape s = weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned);
+    REQUIRE(s.bytes == 0 || (work && work_bytes >= s.bytes && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
+            (unsigned long long)s.bytes);
     if (outs == 0) return COMP_AMS_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const WeightShape s = weight_shape(rows, cols, outs, n);
-    float *bias_sums = static_cast<float *>(work);
-    float *sums = reinterpret_cast<float *>(static_cast<char *>(work) + weight_bias_bytes(s, outs, n));
+    char *memory = static_cast<char *>(work);
+    float *sums = reinterpret_cast<float *>(memory + s.sums_at), *bias_sums = reinterpret_cast<float *>(memory + s.bias_at);
     const int64_t cells = cols * outs, per = rows / n;
     if (cells) {
+        if (rows > 0) {
+            weight_prepare_launch(s, memory, dy, q, scale, rows, cols, outs, dy_stride, q_stride, binary != 0, type, stream);
+            if (const int rc = launched(what)) return rc;      // what the product would read has not been written
+        }
         WeightArgs a = {};
-        a.cols = cols, a.outs = outs, a.dy_stride = dy_stride, a.q_stride = q_stride;
-        a.worker_rows = per, a.split_rows = s.split_rows;
-        a.out_stride = in_first ? outs : cols;
-        a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.splits = (int)s.splits;
+        a.cols = cols, a.outs = outs, a.a_ld = s.a_ld, a.b_ld = s.copied ? s.b_ld : dy_stride, a.b_plane = rows * s.b_ld;
+        a.worker_rows = per, a.out_stride = in_first ? outs : cols;
+        a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.planes = s.planes;
+        a.splits = (int)s.splits, a.split_steps = (int)s.split_steps;
+        const bf16_t *a_rows = reinterpret_cast<const bf16_t *>(memory + s.a_at);
+        const bf16_t *b_rows = s.copied ? reinterpret_cast<const bf16_t *>(memory + s.b_at) : static_cast<const bf16_t *>(dy);
         if (s.splits > 1) {
             a.worker_stride = cells, a.piece_stride = cells * n;
-            weight_launch<float>(sums, dy, q, scale, a, s.tile, in_first != 0, binary != 0, type, stream);
+            weight_launch<float>(sums, a_rows, b_rows, a, s.tile, in_first != 0, stream);
             if (const int rc = launched(what)) return rc;      // what the join would read has not been written
         } else {
             a.worker_stride = grad_stride;
@@ -473,7 +506,7 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
         with_type(grad_type, [&](auto t) {
             using G = decltype(t);
             if (s.splits == 1) {
-                weight_launch<G>(static_cast<G *>(dweight), dy, q, scale, a, s.tile, in_first != 0, binary != 0, type, stream);
+                weight_launch<G>(static_cast<G *>(dweight), a_rows, b_rows, a, s.tile, in_first != 0, stream);
                 return;
             }
             in_launches(ceil_div(cells, 4 * kWeightJoinThreads), kWeightJoinThreads, [&](unsigned first, unsigned count) {

@@ -2,13 +2,15 @@
 //
 //   dW[w][o][i] = sum over worker w's rows r of dy[r][o] (q[r][i] scale[r])
 //
-// Both operands lie across the sum (their rows are the sum's index): a step's 32 rows go to LDS as they lie, and the transposing LDS reads
-// hand every lane its column's values.  The matrix instruction takes bfloat16, which holds q exactly (7 bits); what it cannot hold goes in several
-// planes whose products are added up:
-//   dy in bfloat16, scales powers of two     q scale and dy, both exact: one product
+// The matrix instruction takes bfloat16, which holds q exactly (7 bits); what it cannot hold goes in several planes whose products are added up:
+//   dy in bfloat16, scales powers of two     q scale and dy, both exact: one plane
 //   dy in bfloat16, any scale; in float16    fl32(dy scale) in two planes of 8 bits: 2^-17 of each product is lost, nothing where the
-//                                            scale is a power of two
+//                                            scale is a power of two and dy half precision
 //   dy in float32                            the same in three planes: all 24 bits
+// A first kernel writes q and the planes of dy as rows of bfloat16 (dy itself is read where one plane does and its rows are aligned), so that
+// each number is widened once and not once for every tile that it meets.  The sum runs over planes and rows.  Both operands lie across it (their rows are the sum's
+// index): a step's rows go from memory to LDS as they lie, without registers, and the transposing LDS reads hand every lane its column's
+// values.
 #pragma once
 #include "product8_kernels.h"
 
@@ -17,23 +19,9 @@ namespace cams_ops {
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
-
-struct WeightArgs {
-    int64_t cols, outs, dy_stride, q_stride;
-    int64_t worker_rows, split_rows;                 // rows of a worker, and of one of its pieces (a multiple of kWeightStep)
-    int64_t out_stride, worker_stride, piece_stride; // of the result, in elements: its rows', the workers', the pieces'
-    int tiles_i, tiles_o, n, splits;
-    unsigned first;
-};
-
-constexpr int kWeightStep = 32, kWeightPad = 16;
 
 template <typename T, bool kBinary> constexpr int kPlanes = sizeof(T) == 4 ? 3 : 2;
 template <> constexpr int kPlanes<bf16_t, true> = 1;
-
-// Eight values in bfloat16.
-__device__ __forceinline__ v4u pack8(const float (&x)[8]) { return narrow<bf16_t>(x); }
 
 // x = hi + rest with 8 bits in hi.  Of an infinity nothing is left.
 __device__ __forceinline__ float take_plane(float &x)
@@ -43,93 +31,150 @@ __device__ __forceinline__ float take_plane(float &x)
     return hi;
 }
 
-// A tile of kI input channels x kO output channels by kWavesI x kWavesO wavefronts.  kInFirst: the result is [i][o], otherwise [o][i].
-template <typename T, typename G, bool kBinary, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
-__global__ __launch_bounds__(kWavesI *kWavesO *kWave) void weight_grad(G *__restrict__ out, const T *__restrict__ dy, const int8_t *__restrict__ q,
-                                                                       const float *__restrict__ scale, WeightArgs a)
+constexpr int kPrepareThreads = 256;
+
+struct PrepareArgs {
+    int64_t rows, cols, outs, q_stride, dy_stride;
+    int64_t a_ld, b_ld, b_plane;                     // rows of the results, elements apart, and planes of dy
+    int lanes_a, lanes_b;                            // lanes that share a row, powers of two up to 256
+    unsigned blocks_a;                               // workgroups for q; the others are for dy
+    unsigned first;
+};
+
+// Rows of bfloat16 whose length is a multiple of eight (zeros behind the row): q scale (one plane) or q; the planes of dy scale, or dy itself.
+template <typename T, int kP>
+__global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__restrict__ a_out, bf16_t *__restrict__ b_out, const T *__restrict__ dy,
+                                                                  const int8_t *__restrict__ q, const float *__restrict__ scale, PrepareArgs a)
 {
-    constexpr int kThreads = kWavesI * kWavesO * kWave, kP = kPlanes<T, kBinary>, E = kVec<T>;
+    unsigned block = a.first + blockIdx.x;
+    const bool of_q = block < a.blocks_a;
+    if (!of_q) block -= a.blocks_a;
+    const int lanes = of_q ? a.lanes_a : a.lanes_b;
+    const int64_t row = (int64_t)block * (kPrepareThreads / lanes) + threadIdx.x / lanes;
+    if (row >= a.rows) return;
+    const int lane = threadIdx.x % lanes;
+    const float s = scale[row];
+    if (of_q) {
+        const int8_t *qr = q + row * a.q_stride;
+        for (int64_t c = lane * 8; c < a.cols; c += lanes * 8) {
+            uint64_t raw = 0;
+            if (c + 8 <= a.cols) {
+                raw = load_bytes<8>(qr + c);
+            } else {
+                for (int u = 0; c + u < a.cols; ++u) raw |= (uint64_t)(uint8_t)qr[c + u] << (8 * u);
+            }
+            float x[8];
+            from_bytes<8>(raw, x);
+            if constexpr (kP == 1) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] *= s;
+            }
+            *reinterpret_cast<v4u *>(a_out + row * a.a_ld + c) = narrow<bf16_t>(x);
+        }
+        return;
+    }
+    constexpr int E = kVec<T>;
+    const T *dr = dy + row * a.dy_stride;
+    for (int64_t c = lane * 8; c < a.outs; c += lanes * 8) {
+        float x[8] = {};
+        if (c + 8 <= a.outs) {
+#pragma unroll
+            for (int u = 0; u < 8; u += E) {
+                float part[E];
+                widen<T>(load_vec(dr + c + u), part);
+#pragma unroll
+                for (int v = 0; v < E; ++v) x[u + v] = part[v];
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (c + u < a.outs) x[u] = widen1(dr[c + u]);
+        }
+        if constexpr (kP > 1) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] *= s;
+        }
+#pragma unroll
+        for (int p = 0; p < kP; ++p) {
+            float plane[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) plane[u] = p < kP - 1 ? take_plane(x[u]) : x[u];
+            *reinterpret_cast<v4u *>(b_out + p * a.b_plane + row * a.b_ld + c) = narrow<bf16_t>(plane);
+        }
+    }
+}
+
+struct WeightArgs {
+    int64_t cols, outs, a_ld, b_ld, b_plane;
+    int64_t worker_rows;
+    int64_t out_stride, worker_stride, piece_stride; // of the result, in elements: its rows', the workers', the pieces'
+    int tiles_i, tiles_o, n, planes;
+    int splits, split_steps;                         // pieces of the sum over planes and steps of rows, and their length
+    unsigned first;
+};
+
+constexpr int kWeightStep = 64;          // rows in LDS at a time
+
+// A tile of kI input channels x kO output channels by kWavesI x kWavesO wavefronts.  kInFirst: the result is [i][o], otherwise [o][i].
+//
+// In LDS a row's 32-byte blocks (the 16 columns of a fragment) stand at place block ^ (row & 7): a transposing read takes 32 bytes from each of
+// four rows at a time, and these lie in different banks.
+template <typename G, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
+__global__ __launch_bounds__(kWavesI *kWavesO *kWave) void weight_grad(G *__restrict__ out, const bf16_t *__restrict__ a_rows,
+                                                                       const bf16_t *__restrict__ b_rows, WeightArgs a)
+{
+    constexpr int kWaves = kWavesI * kWavesO;
     constexpr int kIi = kI / kWavesI / 16, kOi = kO / kWavesO / 16;
-    constexpr int kLdI = kI + kWeightPad, kLdO = kO + kWeightPad;
-    constexpr int kRowI = kI / 16, kRowO = kO / E;                           // 16-byte chunks of a row
-    constexpr int kLoadsI = kWeightStep * kRowI / kThreads, kLoadsO = kWeightStep * kRowO / kThreads;
-    static_assert(kLoadsI * kThreads == kWeightStep * kRowI && kLoadsO * kThreads == kWeightStep * kRowO, "whole loads");
-    __shared__ __attribute__((aligned(16))) uint16_t q_lds[2][kWeightStep * kLdI];
-    __shared__ __attribute__((aligned(16))) uint16_t dy_lds[2][kP][kWeightStep * kLdO];
+    constexpr int kBytesI = kI * 2, kBytesO = kO * 2;                        // of a row in LDS
+    constexpr int kRowsI = 1024 / kBytesI, kRowsO = 1024 / kBytesO;          // rows of a wavefront-wide load
+    constexpr int kLoadsI = kWeightStep / kRowsI / kWaves, kLoadsO = kWeightStep / kRowsO / kWaves;
+    static_assert(kLoadsI * kRowsI * kWaves == kWeightStep && kLoadsO * kRowsO * kWaves == kWeightStep, "whole loads");
+    constexpr int kStage = kWeightStep * (kBytesI + kBytesO);
+    __shared__ __attribute__((aligned(1024))) int8_t tile[2][kStage];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     int set, ti, to;
     grouped_tile(a.first + blockIdx.x, (unsigned)(a.n * a.splits), a.tiles_i, a.tiles_o, set, ti, to);
     const int worker = set / a.splits, piece = set % a.splits;
     const int64_t i0 = (int64_t)ti * kI, o0 = (int64_t)to * kO;
-    const int64_t r0 = (int64_t)piece * a.split_rows;
-    const int rows = (int)min(a.split_rows, a.worker_rows - r0);
-    const int64_t base = worker * a.worker_rows + r0;
-    const int8_t *qt = q + base * a.q_stride;
-    const T *dyt = dy + base * a.dy_stride;
-    const float *st = scale + base;
+    const bf16_t *at = a_rows + worker * a.worker_rows * a.a_ld + i0, *bt = b_rows + worker * a.worker_rows * a.b_ld + o0;
+    const int rows = (int)a.worker_rows, steps = (rows + kWeightStep - 1) / kWeightStep;
+    const int begin = piece * a.split_steps, end = min(steps * a.planes, begin + a.split_steps);
 
-    v4i qreg[kLoadsI], dyreg[kLoadsO];
-    float qs[kLoadsI], dys[kLoadsO];
-    auto load = [&](int r) {
-#pragma unroll
-        for (int j = 0; j < kLoadsI; ++j) {
-            const int id = threadIdx.x + j * kThreads, row = r + id / kRowI;
-            qreg[j] = v4i{0, 0, 0, 0};
-            qs[j] = 0.f;
-            if (row < rows) {
-                qreg[j] = load_row16(qt + row * a.q_stride + i0, id % kRowI * 16, (int)min(a.cols - i0, (int64_t)kI));
-                if constexpr (kP == 1) qs[j] = st[row];
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kLoadsO; ++j) {
-            const int id = threadIdx.x + j * kThreads, row = r + id / kRowO;
-            dyreg[j] = v4i{0, 0, 0, 0};
-            dys[j] = 0.f;
-            if (row < rows) {
-                dyreg[j] = load_row16(reinterpret_cast<const int8_t *>(dyt + row * a.dy_stride + o0), id % kRowO * 16,
-                                      (int)min(a.outs - o0, (int64_t)kO) * (int)sizeof(T));
-                if constexpr (kP > 1) dys[j] = st[row];
-            }
-        }
+    // a lane's part of each load: its row, and the 16 bytes that belong to its place there
+    constexpr uint32_t kNowhere = 0x80000000u;       // past the end of any buffer: reads zeros
+    uint32_t off_i[kLoadsI], off_o[kLoadsO];
+    auto offset = [&](int first, int row_bytes, int64_t left, int64_t ld) {
+        const int row = first + lane / (row_bytes / 16), place = lane % (row_bytes / 16);
+        const int column = ((place >> 1) ^ (row & 7)) * 16 + (place & 1) * 8;
+        return column < left ? (uint32_t)((row * ld + column) * 2) : kNowhere;
     };
-    auto put = [&](int stage) {
+#pragma unroll
+    for (int j = 0; j < kLoadsI; ++j) off_i[j] = offset((j * kWaves + wave) * kRowsI, kBytesI, a.cols - i0, a.a_ld);
+#pragma unroll
+    for (int j = 0; j < kLoadsO; ++j) off_o[j] = offset((j * kWaves + wave) * kRowsO, kBytesO, a.outs - o0, a.b_ld);
+    int step = begin % max(steps, 1), plane = begin / max(steps, 1);
+    auto send = [&](int stage) {                     // the next step's rows, asynchronous
+        const int64_t first = (int64_t)step * kWeightStep;
+        const __amdgpu_buffer_rsrc_t asrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(at + first * a.a_ld), 0, 0x7fffffff, 0x00020000);
+        const __amdgpu_buffer_rsrc_t bsrc =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(bt + plane * a.b_plane + first * a.b_ld), 0, 0x7fffffff, 0x00020000);
+        const int left = rows - step * kWeightStep;
 #pragma unroll
         for (int j = 0; j < kLoadsI; ++j) {
-            const int id = threadIdx.x + j * kThreads;
-            uint16_t *to_lds = &q_lds[stage][id / kRowI * kLdI + id % kRowI * 16];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float x[8];
-                from_bytes<8>(((uint64_t)(uint32_t)qreg[j][2 * h + 1] << 32) | (uint32_t)qreg[j][2 * h], x);
-                if constexpr (kP == 1) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) x[c] *= qs[j];
-                }
-                *reinterpret_cast<v4u *>(to_lds + 8 * h) = pack8(x);
-            }
+            const int row = (j * kWaves + wave) * kRowsI;
+            uint32_t from = off_i[j];
+            if (left < kWeightStep && row + lane / (kBytesI / 16) >= left) from = kNowhere;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(asrc, (lds_bytes *)&tile[stage][row * kBytesI], 16, from, 0, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < kLoadsO; ++j) {
-            const int id = threadIdx.x + j * kThreads, at = id / kRowO * kLdO + id % kRowO * E;
-            if constexpr (kP == 1) {
-                *reinterpret_cast<v4i *>(&dy_lds[stage][0][at]) = dyreg[j];
-            } else {
-                float x[E], plane[8] = {};
-                widen<T>(__builtin_bit_cast(v4u, dyreg[j]), x);
-#pragma unroll
-                for (int c = 0; c < E; ++c) x[c] *= dys[j];
-#pragma unroll
-                for (int p = 0; p < kP; ++p) {
-#pragma unroll
-                    for (int c = 0; c < E; ++c) plane[c] = p < kP - 1 ? take_plane(x[c]) : x[c];
-                    const v4u bits = pack8(plane);
-                    if constexpr (E == 8) *reinterpret_cast<v4u *>(&dy_lds[stage][p][at]) = bits;
-                    else *reinterpret_cast<uint64_t *>(&dy_lds[stage][p][at]) = ((uint64_t)bits[1] << 32) | bits[0];
-                }
-            }
+            const int row = (j * kWaves + wave) * kRowsO;
+            uint32_t from = off_o[j];
+            if (left < kWeightStep && row + lane / (kBytesO / 16) >= left) from = kNowhere;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(bsrc, (lds_bytes *)&tile[stage][kWeightStep * kBytesI + row * kBytesO], 16, from, 0, 0, 0);
         }
+        if (++step == steps) step = 0, ++plane;
     };
 
     v4f acc[kIi][kOi];
@@ -140,41 +185,42 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave) void weight_grad(G *__rest
     const int wi = wave / kWavesO, wo = wave % kWavesO;
     const int frow = lane & 15, fgroup = lane >> 4;
     // Transposing read: the 16 lanes of a group point at four rows of 16 columns, 8 bytes each; lane c of them receives column c of the four.
-    const int trow = fgroup * 8 + frow / 4, tcol = frow % 4 * 4;
-    auto fragment = [&](const uint16_t *p, int ld) {
-        typedef __attribute__((address_space(3))) v4s *lds_v4s;
-        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(__attribute__((address_space(3))) void *)(void *)p);
-        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(__attribute__((address_space(3))) void *)(void *)(p + 4 * ld));
+    // A lane's eight values of the sum's index are rows 8 g .. 8 g + 7 for its group g.
+    const int trow = fgroup * 8 + frow / 4;
+    auto fragment = [&](const int8_t *base, int row_bytes, int block) {
+        typedef __attribute__((address_space(3))) v4s lds_v4s;
+        const int low = trow * row_bytes + ((block ^ (frow / 4)) * 32) + frow % 4 * 8;
+        const int high = (trow + 4) * row_bytes + ((block ^ (frow / 4 + 4)) * 32) + frow % 4 * 8;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(base + low));
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(base + high));
         return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     auto work_on = [&](int stage) {
-        v8bf qf[kIi];
 #pragma unroll
-        for (int i = 0; i < kIi; ++i) qf[i] = fragment(&q_lds[stage][trow * kLdI + (wi * kIi + i) * 16 + tcol], kLdI);
+        for (int kk = 0; kk < kWeightStep / 32; ++kk) {
+            const int8_t *ib = &tile[stage][kk * 32 * kBytesI], *ob = &tile[stage][kWeightStep * kBytesI + kk * 32 * kBytesO];
+            v8bf af[kIi], bf[kOi];
 #pragma unroll
-        for (int p = kP - 1; p >= 0; --p)
+            for (int i = 0; i < kIi; ++i) af[i] = fragment(ib, kBytesI, wi * kIi + i);
 #pragma unroll
-            for (int o = 0; o < kOi; ++o) {
-                const v8bf df = fragment(&dy_lds[stage][p][trow * kLdO + (wo * kOi + o) * 16 + tcol], kLdO);
+            for (int o = 0; o < kOi; ++o) bf[o] = fragment(ob, kBytesO, wo * kOi + o);
+#pragma unroll
+            for (int o = 0; o < kOi; ++o)
 #pragma unroll
                 for (int i = 0; i < kIi; ++i) {
-                    if constexpr (kInFirst) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(df, qf[i], acc[i][o], 0, 0, 0);
-                    else acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[i], df, acc[i][o], 0, 0, 0);
+                    if constexpr (kInFirst) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[o], af[i], acc[i][o], 0, 0, 0);
+                    else acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[i], bf[o], acc[i][o], 0, 0, 0);
                 }
-            }
+        }
     };
 
-    if (rows > 0) {
-        load(0);
-        put(0);
-    }
+    if (begin < end) send(0);
     int stage = 0;
-    for (int r = 0; r < rows; r += kWeightStep, stage ^= 1) {
-        __syncthreads();
-        const bool more = r + kWeightStep < rows;
-        if (more) load(r + kWeightStep);
+    for (int c = begin; c < end; ++c, stage ^= 1) {
+        // this stage has arrived, for every wavefront, and nobody reads the other one any more
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (c + 1 < end) send(stage ^ 1);
         work_on(stage);
-        if (more) put(stage ^ 1);
     }
 
     G *ot = out + worker * a.worker_stride + piece * a.piece_stride;
@@ -184,19 +230,19 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave) void weight_grad(G *__rest
 #pragma unroll
         for (int o = 0; o < kOi; ++o) {
             const int64_t ci = i0 + (wi * kIi + i) * 16, co = o0 + (wo * kOi + o) * 16;
-            const int64_t row = (kInFirst ? ci : co) + frow, at = (kInFirst ? co : ci) + fgroup * 4;
-            if (row >= across || at >= along) continue;
-            G *p = ot + row * a.out_stride + at;
+            const int64_t row = (kInFirst ? ci : co) + frow, col = (kInFirst ? co : ci) + fgroup * 4;
+            if (row >= across || col >= along) continue;
+            G *p = ot + row * a.out_stride + col;
             G four[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) four[c] = narrow1<G>(acc[i][o][c]);
-            if (at + 4 <= along) {
+            if (col + 4 <= along) {
                 if constexpr (sizeof(G) == 4) *reinterpret_cast<v4u_any *>(p) = v4u{bits1(four[0]), bits1(four[1]), bits1(four[2]), bits1(four[3])};
                 else *reinterpret_cast<v2u_any *>(p) = v2u_any{bits1(four[0]) | (bits1(four[1]) << 16), bits1(four[2]) | (bits1(four[3]) << 16)};
             } else {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    if (at + c < along) p[c] = four[c];
+                    if (col + c < along) p[c] = four[c];
             }
         }
 }

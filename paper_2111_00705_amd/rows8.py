@@ -188,6 +188,7 @@ def linear_weight_grad(dy, q, scale, dweight, dbias=None, binary=False):
         _need(dbias.dtype == dweight.dtype and tuple(dbias.shape) == (n, outs) and (_param_grad(dbias, (outs,), "dbias") == stride or n == 1),
               "dbias must be [n, outs] with the type and worker stride of dweight")
     s = _stream(dy, q, scale, dweight, dbias)
-    work, work_ptr, work_bytes = _work("comp_ams_linear_weight_grad_work_bytes", dy.device, rows, cols, outs, n, 1 if binary else 0, kind)
+    work, work_ptr, work_bytes = _work("comp_ams_linear_weight_grad_work_bytes", dy.device, rows, cols, outs, n, 1 if binary else 0, kind,
+                                       1 if dy.data_ptr() % 16 == 0 and dy_stride % 8 == 0 else 0)
     _check(lib().comp_ams_linear_weight_grad(dweight.data_ptr(), _ptr(dbias), dy.data_ptr(), q.data_ptr(), scale.data_ptr(), rows, cols, outs, dy_stride,
                                              q_stride, n, stride, 1 if in_first else 0, 1 if binary else 0, kind, _type(dweight), work_ptr, work_bytes, s))

@@ -75,10 +75,10 @@ def test_work_bytes():
     assert L.comp_ams_rms_norm_work_bytes(4097, 768, 8, C.byref(n)) == P.EINVAL and L.comp_ams_rms_norm_work_bytes(4096, 768, 8, None) == P.EINVAL
     assert L.comp_ams_linear_q8_work_bytes(4, 4096, 4096, C.byref(n)) == P.OK and n.value == 0
     assert L.comp_ams_linear_q8_work_bytes(4, 131_072, 4096, C.byref(n)) == P.EINVAL and L.comp_ams_linear_q8_work_bytes(4, 5, 6, None) == P.EINVAL
-    assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 8, 1, 1, C.byref(n)) == P.OK
-    assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 7, 1, 1, C.byref(n)) == P.EINVAL
-    assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 8, 1, 7, C.byref(n)) == P.EINVAL
-    assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 8, 1, 1, None) == P.EINVAL
+    assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 8, 1, 1, 1, C.byref(n)) == P.OK
+    assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 7, 1, 1, 1, C.byref(n)) == P.EINVAL
+    assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 8, 1, 7, 1, C.byref(n)) == P.EINVAL
+    assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 8, 1, 1, 0, None) == P.EINVAL
 
 
 def test_the_python_entry_points_refuse():
