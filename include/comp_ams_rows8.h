@@ -71,12 +71,14 @@ int comp_ams_rms_norm_work_bytes(int64_t rows, int64_t cols, int32_t n, uint64_t
  * q: int8 [rows][cols], w: int8 [outs][cols] (any values, -128 too), bias: fp32 [outs] or NULL.  The sum is exact, scales and bias are
  * applied in fp32 from left to right, y is rounded once to `type`.  0 <= rows, outs < 2^31, 0 <= cols < COMP_AMS_MAX_Q8_COLS.
  * With cols = 0 y is the bias.  The input's gradient is another such product: of dy in 8 bits with the transposed weight in 8 bits.
- * work: comp_ams_linear_q8_work_bytes() bytes of device memory, 16-byte aligned, which may be 0 (then NULL will do).
+ * work: comp_ams_linear_q8_work_bytes() bytes of device memory, 16-byte aligned, which may be 0 (then NULL will do); fewer where, as q_aligned
+ * and w_aligned != 0 promise, the array's address and stride are multiples of 16 and its stride is below 2^22.  (More than 64 rows are then read
+ * where they stand, if cols is a multiple of 16 too.)
  */
 int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_t *w, const float *w_scale, const float *bias,
                        int64_t rows, int64_t cols, int64_t outs, int64_t y_stride, int64_t q_stride, int64_t w_stride, int32_t type,
                        void *work, uint64_t work_bytes, void *hip_stream);
-int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, uint64_t *bytes);
+int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, int32_t q_aligned, int32_t w_aligned, uint64_t *bytes);
 
 /*
  * Weight gradients of a linear layer y = x W^T + bias from its input in 8 bits, per worker:

@@ -127,7 +127,7 @@ def lib():
         L.comp_ams_rms_norm_backward.argtypes = [vp] * 8 + [i64] * 6 + [i32, i64, i32, i32, vp, u64, vp]
         L.comp_ams_rms_norm_work_bytes.argtypes = [i64, i64, i32, C.POINTER(u64)]
         L.comp_ams_linear_q8.argtypes = [vp] * 6 + [i64] * 6 + [i32, vp, u64, vp]
-        L.comp_ams_linear_q8_work_bytes.argtypes = [i64, i64, i64, C.POINTER(u64)]
+        L.comp_ams_linear_q8_work_bytes.argtypes = [i64] * 3 + [i32, i32, C.POINTER(u64)]
         L.comp_ams_linear_weight_grad.argtypes = [vp] * 5 + [i64] * 5 + [i32, i64, i32, i32, i32, i32, vp, u64, vp]
         L.comp_ams_linear_weight_grad_work_bytes.argtypes = [i64] * 3 + [i32] * 4 + [C.POINTER(u64)]
         L.comp_ams_operators_last_error.argtypes = []

@@ -3,16 +3,14 @@
 //   y[m][n] = (sum_k x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n]
 //
 // The sums are 32-bit integers and exact in any order (fewer than 2^17 products of at most 2^14).
-// Both operands lie along k, so a tile's rows go to LDS as they are, 128 bytes a row in eight 16-byte chunks; chunk c of row r stands at
-// place c ^ (r & 7), which spreads the 16 rows of a fragment over all banks.  The matrix instruction takes the channels as its rows: a lane then
-// holds four neighbouring channels of one token, which leave in one store.
+// Both operands lie along k, so a tile's rows go to LDS as they are.  The matrix instruction takes the channels as its rows: a lane then holds
+// four neighbouring channels of one token, which leave in one store.
 #pragma once
 #include "rows8.h"
 
 namespace cams_ops {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) int8_t lds_bytes;
 
 struct ProductArgs {
     int64_t rows, outs, x_stride, w_stride, y_stride;
@@ -22,8 +20,22 @@ struct ProductArgs {
     unsigned first;
 };
 
-constexpr int kProductStep = 128;        // bytes of k that a tile's rows hold in LDS
+constexpr int kProductStep = 64;         // bytes of k in a stage of LDS
 constexpr int kXcds = 8;
+
+// Memory to LDS without registers, asynchronous: a lane's 16 bytes at `offset` of a buffer (base, size in bytes; zeros from its end on) go to `to` +
+// 16 lane, `to` and the buffer being the wavefront's.  vmcnt counts it.  In assembly, because the compiler takes every read of LDS for one of
+// what is still on its way and waits for memory before it; there is no output that it could take for written.
+__device__ __forceinline__ v4u raw_buffer(const void *base, uint32_t bytes)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    return v4u{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+__device__ __forceinline__ void to_lds(const v4u &buffer, uint32_t offset, const int8_t *to)
+{
+    const uint32_t lds = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) int8_t *)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer) : "memory");
+}
 
 // 16 bytes of a row of `cols`, from k on; zero past the row.  Any alignment.
 __device__ __forceinline__ v4i load_row16(const int8_t *row, int k, int cols)
@@ -99,20 +111,46 @@ __device__ __forceinline__ void grouped_tile(unsigned block, unsigned sets, int 
     tn = (int)(within / high);
 }
 
-// A tile of kM tokens x kN channels by kWavesM x kWavesN wavefronts.  kAsync: rows, strides and sizes are multiples of 16 bytes, and the tiles
-// go from memory to LDS without registers; otherwise through registers, by loads of any alignment.
-// kSplit: a piece of k; the sums go to work[piece][rows][outs].
-template <typename Y, int kM, int kN, int kWavesM, int kWavesN, bool kAsync, bool kSplit>
-__global__ __launch_bounds__(kWavesM *kWavesN *kWave) void product8(Y *__restrict__ y, int *__restrict__ work, const int8_t *__restrict__ x,
+constexpr int kPackThreads = 256;
+
+struct PackArgs {
+    int64_t rows, outs, x_stride, w_stride, ld;      // ld: cols rounded up to 16
+    int cols, lanes;                                 // lanes that share a row, a power of two up to kPackThreads
+    unsigned blocks_x;                               // workgroups for x; the others are for w
+    unsigned first;
+};
+
+// Rows of x and of w written anew, 16 bytes by 16 bytes, zeros behind the row: what product8 takes, from rows of any length, stride and address.
+static __global__ __launch_bounds__(kPackThreads) void product8_pack(int8_t *__restrict__ x_out, int8_t *__restrict__ w_out, const int8_t *__restrict__ x,
+                                                                     const int8_t *__restrict__ w, PackArgs a)
+{
+    unsigned block = a.first + blockIdx.x;
+    const bool of_x = block < a.blocks_x;
+    if (!of_x) block -= a.blocks_x;
+    const int64_t row = (int64_t)block * (kPackThreads / a.lanes) + threadIdx.x / a.lanes;
+    if (row >= (of_x ? a.rows : a.outs)) return;
+    const int8_t *from = of_x ? x + row * a.x_stride : w + row * a.w_stride;
+    int8_t *to = (of_x ? x_out : w_out) + row * a.ld;
+    for (int k = threadIdx.x % a.lanes * 16; k < a.cols; k += a.lanes * 16) *reinterpret_cast<v4i *>(to + k) = load_row16(from, k, a.cols);
+}
+
+// A tile of kM tokens x kN channels by kWavesM x kWavesN wavefronts.  Rows, strides and addresses are multiples of 16 bytes: memory goes to LDS
+// without registers.  kSplit: a piece of k; the sums go to work[piece][rows][outs].
+//
+// A step is 64 bytes of k.  Of four stages in LDS two are on their way from memory, one has arrived and is read into registers while the matrix
+// instructions work on what was read before: one barrier a step, and nothing waits for memory or LDS within it.  A step's row is four
+// 16-byte chunks; chunk c of row r stands at place c ^ (r / 2 & 3), so that eight rows at one chunk lie in different banks.
+template <typename Y, int kM, int kN, int kWavesM, int kWavesN, bool kSplit>
+__global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__restrict__ y, int *__restrict__ work, const int8_t *__restrict__ x,
                                                                     const float *__restrict__ x_scale, const int8_t *__restrict__ w,
                                                                     const float *__restrict__ w_scale, const float *__restrict__ bias,
                                                                     ProductArgs a)
 {
-    constexpr int kWaves = kWavesM * kWavesN, kRows = kM + kN;
+    constexpr int kWaves = kWavesM * kWavesN, kRows = kM + kN, kStep = kProductStep, kStages = 4;
     constexpr int kMi = kM / kWavesM / 16, kNi = kN / kWavesN / 16;
-    constexpr int kLoads = kRows / 8 / kWaves, kLoadsX = kM / 8 / kWaves;     // wavefront-wide loads of eight rows each
-    static_assert(kM % (8 * kWaves) == 0 && kN % (8 * kWaves) == 0, "whole loads");
-    __shared__ __attribute__((aligned(16))) int8_t tile[2][kRows * kProductStep];
+    constexpr int kLoads = kRows / 16 / kWaves, kLoadsX = kM / 16 / kWaves;     // wavefront-wide loads of 16 rows each
+    static_assert(kM % (16 * kWaves) == 0 && kN % (16 * kWaves) == 0, "whole loads");
+    __shared__ __attribute__((aligned(1024))) int8_t tile[kStages][kRows * kStep];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const unsigned block = a.first + blockIdx.x;
@@ -123,53 +161,31 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void product8(Y *__restric
     const int k_begin = kSplit ? piece * a.k_split : 0, k_end = kSplit ? min(a.cols, k_begin + a.k_split) : a.cols;
     const int8_t *xt = x + m0 * a.x_stride, *wt = w + n0 * a.w_stride;
 
-    // lane's part of a load: row lane / 8 of the eight, the chunk that belongs to place lane % 8
-    const int sub = lane >> 3, chunk = (lane & 7) ^ sub;
+    // a lane's part of each load: row lane / 4 of the sixteen, the chunk that belongs to place lane % 4
+    const int chunk = (lane & 3) ^ ((lane >> 3) & 3);
     constexpr uint32_t kNowhere = 0x80000000u;       // past the end of any tile: reads zeros
     uint32_t off[kLoads];
-    // raw buffers of 32-bit data that end with the tile's last row
-    const __amdgpu_buffer_rsrc_t xsrc =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(xt), 0, (uint32_t)((rows_m - 1) * a.x_stride + a.cols), 0x00020000);
-    const __amdgpu_buffer_rsrc_t wsrc =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(wt), 0, (uint32_t)((rows_n - 1) * a.w_stride + a.cols), 0x00020000);
-    v4i regs[kAsync ? 1 : kLoads];
-    if constexpr (kAsync) {
+    const v4u xsrc = raw_buffer(xt, 0x7fffffff), wsrc = raw_buffer(wt, 0x7fffffff);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const bool of_x = j < kLoadsX;
-            const int row = ((of_x ? j : j - kLoadsX) * kWaves + wave) * 8 + sub;
-            off[j] = row < (of_x ? rows_m : rows_n) ? (uint32_t)(row * (of_x ? a.x_stride : a.w_stride) + chunk * 16) : kNowhere;
-        }
+    for (int j = 0; j < kLoads; ++j) {
+        const bool of_x = j < kLoadsX;
+        const int row = ((of_x ? j : j - kLoadsX) * kWaves + wave) * 16 + (lane >> 2);
+        off[j] = row < (of_x ? rows_m : rows_n) ? (uint32_t)(row * (of_x ? a.x_stride : a.w_stride) + chunk * 16 + k_begin) : kNowhere;
     }
     auto place = [&](int j) {                        // first byte in LDS of load j
-        return ((j < kLoadsX ? j * kWaves : kM / 8 + (j - kLoadsX) * kWaves) + wave) * 8 * kProductStep;
+        return ((j < kLoadsX ? j * kWaves : kM / 16 + (j - kLoadsX) * kWaves) + wave) * 1024;
     };
-    auto send = [&](int stage, int k) {              // memory to LDS, asynchronous
-        const bool whole = k + kProductStep <= k_end;
+    int k_next = k_begin;
+    auto send = [&](int stage) {                     // the next step, memory to LDS, asynchronous
+        const bool whole = k_next + kStep <= k_end;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            uint32_t at = off[j] + (uint32_t)k;
-            if (!whole && k + chunk * 16 >= k_end) at = kNowhere;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(j < kLoadsX ? xsrc : wsrc, (lds_bytes *)&tile[stage][place(j)], 16, at, 0, 0, 0);
+            uint32_t at = off[j];
+            if (!whole && k_next + chunk * 16 >= k_end) at = kNowhere;
+            to_lds(j < kLoadsX ? xsrc : wsrc, at, &tile[stage][place(j)]);
+            off[j] += kStep;
         }
-    };
-    auto load = [&](int k) {                         // memory to registers
-        if constexpr (!kAsync) {
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                const bool of_x = j < kLoadsX;
-                const int row = ((of_x ? j : j - kLoadsX) * kWaves + wave) * 8 + sub;
-                regs[j] = v4i{0, 0, 0, 0};
-                if (row < (of_x ? rows_m : rows_n))
-                    regs[j] = load_row16(of_x ? xt + row * a.x_stride : wt + row * a.w_stride, k + chunk * 16, k_end);
-            }
-        }
-    };
-    auto put = [&](int stage) {                      // registers to LDS
-        if constexpr (!kAsync) {
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j) *reinterpret_cast<v4i *>(&tile[stage][place(j) + lane * 16]) = regs[j];
-        }
+        k_next += kStep;
     };
 
     v4i acc[kNi][kMi];
@@ -178,45 +194,57 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void product8(Y *__restric
 #pragma unroll
         for (int m = 0; m < kMi; ++m) acc[n][m] = v4i{0, 0, 0, 0};
     const int wm = wave / kWavesN, wn = wave % kWavesN;
-    const int frow = lane & 15, fgroup = lane >> 4, fswap = frow & 7;
-    auto work_on = [&](int stage) {
-        const int8_t *xs = &tile[stage][(wm * kMi * 16 + frow) * kProductStep];
-        const int8_t *ws = &tile[stage][(kM + wn * kNi * 16 + frow) * kProductStep];
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            const int at = ((kk * 4 + fgroup) ^ fswap) * 16;
-            v4i wf[kNi], xf[kMi];
-#pragma unroll
-            for (int n = 0; n < kNi; ++n) wf[n] = *reinterpret_cast<const v4i *>(ws + n * 16 * kProductStep + at);
-#pragma unroll
-            for (int m = 0; m < kMi; ++m) xf[m] = *reinterpret_cast<const v4i *>(xs + m * 16 * kProductStep + at);
-#pragma unroll
-            for (int n = 0; n < kNi; ++n)
-#pragma unroll
-                for (int m = 0; m < kMi; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[n], xf[m], acc[n][m], 0, 0, 0);
-        }
+    const int frow = lane & 15, fgroup = lane >> 4;
+    const int fat = frow * kStep + (fgroup ^ ((frow >> 1) & 3)) * 16;
+    struct Frags {
+        v4i w[kNi], x[kMi];
     };
-
-    int stage = 0;
-    if constexpr (kAsync) {
-        send(0, k_begin);
-        for (int k = k_begin; k < k_end; k += kProductStep, stage ^= 1) {
-            // this stage has arrived, for every wavefront, and nobody reads the other one any more
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (k + kProductStep < k_end) send(stage ^ 1, k + kProductStep);
-            work_on(stage);
+    auto read = [&](Frags &f, int stage) {
+        const int8_t *xs = &tile[stage][wm * kMi * 16 * kStep + fat];
+        const int8_t *ws = &tile[stage][(kM + wn * kNi * 16) * kStep + fat];
+#pragma unroll
+        for (int n = 0; n < kNi; ++n) f.w[n] = *reinterpret_cast<const v4i *>(ws + n * 16 * kStep);
+#pragma unroll
+        for (int m = 0; m < kMi; ++m) f.x[m] = *reinterpret_cast<const v4i *>(xs + m * 16 * kStep);
+    };
+    auto multiply = [&](const Frags &f) {
+#pragma unroll
+        for (int m = 0; m < kMi; ++m)
+#pragma unroll
+            for (int n = 0; n < kNi; ++n) acc[n][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.w[n], f.x[m], acc[n][m], 0, 0, 0);
+    };
+    constexpr int kPer = kMi * kNi / (kMi + kNi);
+    auto mixed = [&]() {
+#pragma unroll
+        for (int u = 0; u < kMi + kNi; ++u) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);          // a read from LDS
+            __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);       // matrix instructions
         }
-    } else {
-        load(k_begin);
-        put(0);
-        for (int k = k_begin; k < k_end; k += kProductStep, stage ^= 1) {
-            __syncthreads();
-            const bool more = k + kProductStep < k_end;
-            if (more) load(k + kProductStep);
-            work_on(stage);
-            if (more) put(stage ^ 1);
-        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kMi * kNi - kPer * (kMi + kNi), 0);
+    };
+    // One step: the next stage has arrived, for every wavefront (of three that were sent the youngest may still be on its way), and nobody
+    // reads the one before any more, which the step after the next but one takes.  Steps past the end read zeros.
+    auto step = [&](int u, const Frags &now, Frags &next) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+        send((u + 3) % kStages);
+        read(next, (u + 1) % kStages);
+        multiply(now);
+        mixed();
+    };
+    Frags even, odd;
+    const int steps = (k_end - k_begin + kStep - 1) / kStep;
+    send(0);
+    send(1);
+    send(2);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
+    read(even, 0);
+    for (int s = 0; s < steps; s += kStages) {
+        step(0, even, odd);
+        step(1, odd, even);
+        step(2, even, odd);
+        step(3, odd, even);
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");         // LDS belongs to the next workgroup after this one
 
 #pragma unroll
     for (int n = 0; n < kNi; ++n) {

@@ -22,6 +22,15 @@ namespace {
     } while (0)
 
 constexpr int64_t kLimit31 = (int64_t)1 << 31;
+constexpr int64_t kMostStride = kLimit31 / 512;      // bytes between rows, of which a tile has 256
+
+// Lanes of a workgroup of 256 that share a row of `chunks`, when it is written anew.
+int shared_lanes(int64_t chunks)
+{
+    int lanes = 8;
+    while (lanes < 256 && lanes < chunks) lanes *= 2;
+    return lanes;
+}
 
 int rows8_check(const char *what, int64_t rows, int64_t cols, const float *scale, int32_t type)
 {
@@ -94,23 +103,37 @@ int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rs
 
 // --- the product -----------------------------------------------------------------------------------------------------
 
-// Which kernel takes a product, and into how many pieces k is cut.
+// Which kernel takes a product, into how many pieces k is cut, and where the work memory holds what.
 struct ProductShape {
     int few;                 // tokens in sixteens for product8_few, or 0
     int tile;                // tokens and channels of a tile
     int splits, k_split;
-    int64_t tiles_m, tiles_n;
+    int64_t tiles_m, tiles_n, ld;
+    uint64_t x_at, w_at, sums_at, bytes;
 };
-ProductShape product_shape(int64_t rows, int64_t cols, int64_t outs)
+ProductShape product_shape(int64_t rows, int64_t cols, int64_t outs, bool x_aligned, bool w_aligned)
 {
-    if (rows <= 64) return {rows <= 16 ? 1 : rows <= 32 ? 2 : 4, 0, 1, 0, 1, ceil_div(outs, 16)};
-    ProductShape s = {0, 256, 1, 0, ceil_div(rows, 256), ceil_div(outs, 256)};
-    if (s.tiles_m * s.tiles_n < 200) s = {0, 128, 1, 0, ceil_div(rows, 128), ceil_div(outs, 128)};
+    ProductShape s = {};
+    s.splits = 1;
+    if (rows <= 64) {
+        s.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+        s.tiles_m = 1, s.tiles_n = ceil_div(outs, 16);
+        return s;
+    }
+    for (s.tile = 256;; s.tile /= 2) {
+        s.tiles_m = ceil_div(rows, s.tile), s.tiles_n = ceil_div(outs, s.tile);
+        if (s.tile == 64 || s.tiles_m * s.tiles_n >= 200) break;
+    }
     const int64_t tiles = s.tiles_m * s.tiles_n, steps = ceil_div(std::max<int64_t>(cols, 1), kProductStep);
-    int64_t pieces = 1;
-    if (s.tile == 128 && tiles < 256) pieces = std::max<int64_t>(1, std::min(512 / tiles, steps / 4));
+    const int64_t pieces = tiles > 0 && tiles < 128 ? std::max<int64_t>(1, std::min(256 / tiles, steps / 16)) : 1;
     s.k_split = (int)(ceil_div(steps, pieces) * kProductStep);
     s.splits = (int)ceil_div(steps * kProductStep, s.k_split);
+    s.ld = ceil_div(cols, 16) * 16;
+    if (cols % 16) x_aligned = w_aligned = false;
+    s.x_at = 0;
+    s.w_at = s.x_at + (x_aligned ? 0 : (uint64_t)(rows * s.ld));
+    s.sums_at = s.w_at + (w_aligned ? 0 : (uint64_t)(outs * s.ld));
+    s.bytes = s.sums_at + (s.splits > 1 ? (uint64_t)s.splits * (uint64_t)rows * (uint64_t)outs * sizeof(int32_t) : 0);
     return s;
 }
 
@@ -119,7 +142,7 @@ int product_check(const char *what, int64_t rows, int64_t cols, int64_t outs)
     REQUIRE(rows >= 0 && rows < kLimit31, "%s: rows=%lld must be in [0, 2^31)", what, (long long)rows);
     REQUIRE(outs >= 0 && outs < kLimit31, "%s: outs=%lld must be in [0, 2^31)", what, (long long)outs);
     REQUIRE(cols >= 0 && cols < COMP_AMS_MAX_Q8_COLS, "%s: cols=%lld must be in [0, %d)", what, (long long)cols, COMP_AMS_MAX_Q8_COLS);
-    const ProductShape s = product_shape(rows, cols, outs);
+    const ProductShape s = product_shape(rows, cols, outs, true, true);
     REQUIRE(s.tiles_m * s.tiles_n * s.splits <= kMaxBlocks, "%s: rows and outs are too many for one call", what);
     return COMP_AMS_OK;
 }
@@ -145,11 +168,13 @@ WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bo
     WeightShape s = {};
     s.planes = type == COMP_AMS_F32 ? 3 : type == COMP_AMS_BF16 && binary ? 1 : 2;
     s.copied = s.planes > 1 || !dy_aligned || outs % 8 != 0;
-    s.tile = 256, s.tiles_i = ceil_div(cols, 256), s.tiles_o = ceil_div(outs, 256);
-    if (s.tiles_i * s.tiles_o * n < 200) s.tile = 128, s.tiles_i = ceil_div(cols, 128), s.tiles_o = ceil_div(outs, 128);
+    for (s.tile = 256;; s.tile /= 2) {
+        s.tiles_i = ceil_div(cols, s.tile), s.tiles_o = ceil_div(outs, s.tile);
+        if (s.tile == 64 || s.tiles_i * s.tiles_o * n >= 200) break;
+    }
     const int64_t tiles = s.tiles_i * s.tiles_o * n, steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.planes);
     int64_t pieces = 1;
-    if (s.tile == 128 && tiles > 0 && tiles < 256) pieces = std::max<int64_t>(1, std::min(512 / tiles, steps / 4));
+    if (tiles > 0 && tiles < 200) pieces = std::max<int64_t>(1, std::min(512 / tiles, steps / 16));
     s.split_steps = ceil_div(steps, pieces);
     s.splits = ceil_div(steps, s.split_steps);
     const int64_t want = std::max<int64_t>(1, 1024 / (n * ceil_div(std::max<int64_t>(outs, 1), kRmsThreads)));
@@ -179,18 +204,10 @@ int weight_check(const char *what, int64_t rows, int64_t cols, int64_t outs, int
     return COMP_AMS_OK;
 }
 
-// Lanes that share a row of `eights` chunks.
-int prepare_lanes(int64_t eights)
-{
-    int lanes = 8;
-    while (lanes < kPrepareThreads && lanes < eights) lanes *= 2;
-    return lanes;
-}
-
 void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, const int8_t *q, const float *scale, int64_t rows, int64_t cols,
                            int64_t outs, int64_t dy_stride, int64_t q_stride, bool binary, int32_t type, hipStream_t stream)
 {
-    PrepareArgs a = {rows, cols, outs, q_stride, dy_stride, s.a_ld, s.b_ld, rows * s.b_ld, prepare_lanes(s.a_ld / 8), prepare_lanes(s.b_ld / 8), 0, 0};
+    PrepareArgs a = {rows, cols, outs, q_stride, dy_stride, s.a_ld, s.b_ld, rows * s.b_ld, shared_lanes(s.a_ld / 8), shared_lanes(s.b_ld / 8), 0, 0};
     const int64_t blocks_a = ceil_div(rows, kPrepareThreads / a.lanes_a), blocks_b = s.copied ? ceil_div(rows, kPrepareThreads / a.lanes_b) : 0;
     a.blocks_a = (unsigned)blocks_a;
     auto go = [&](auto t, auto planes) {
@@ -220,9 +237,12 @@ void weight_launch(G *out, const bf16_t *a_rows, const bf16_t *b_rows, WeightArg
     if (tile == 256) {
         if (in_first) go(weight_grad<G, true, 256, 256, 2, 4>, 512);
         else go(weight_grad<G, false, 256, 256, 2, 4>, 512);
-    } else {
+    } else if (tile == 128) {
         if (in_first) go(weight_grad<G, true, 128, 128, 2, 2>, 256);
         else go(weight_grad<G, false, 128, 128, 2, 2>, 256);
+    } else {
+        if (in_first) go(weight_grad<G, true, 64, 64, 2, 2>, 256);
+        else go(weight_grad<G, false, 64, 64, 2, 2>, 256);
     }
 }
 
@@ -374,13 +394,12 @@ int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void
     return launched(what);
 }
 
-int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, uint64_t *bytes)
+int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, int32_t q_aligned, int32_t w_aligned, uint64_t *bytes)
 {
     const char *what = "linear_q8_work_bytes";
     if (const int rc = product_check(what, rows, cols, outs)) return rc;
     REQUIRE(bytes, "%s: bytes is NULL", what);
-    const ProductShape s = product_shape(rows, cols, outs);
-    *bytes = s.splits > 1 ? (uint64_t)s.splits * (uint64_t)rows * (uint64_t)outs * sizeof(int32_t) : 0;
+    *bytes = product_shape(rows, cols, outs, q_aligned != 0, w_aligned != 0).bytes;
     return COMP_AMS_OK;
 }
 
@@ -396,19 +415,32 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
     REQUIRE_ROWS(what, "y", y, outs ? rows : 0, outs, y_stride, type);
     REQUIRE((scale || rows == 0) && (w_scale || outs == 0), "%s: a scale is NULL", what);
     REQUIRE(aligned(scale, 4) && aligned(w_scale, 4) && aligned(bias, 4), "%s: scales and bias must be 4-byte aligned", what);
-    uint64_t need = 0;
-    if (const int rc = comp_ams_linear_q8_work_bytes(rows, cols, outs, &need)) return rc;
-    REQUIRE(need == 0 || (work && work_bytes >= need && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
-            (unsigned long long)need);
+    // memory to LDS without registers: whole 16-byte chunks, and a tile's rows within 31 bits
+    const bool q_aligned = cols % 16 == 0 && aligned(q, 16) && (rows <= 1 || (q_stride % 16 == 0 && q_stride < kMostStride));
+    const bool w_aligned = cols % 16 == 0 && aligned(w, 16) && (outs <= 1 || (w_stride % 16 == 0 && w_stride < kMostStride));
+    const ProductShape s = product_shape(rows, cols, outs, q_aligned, w_aligned);
+    REQUIRE(s.bytes == 0 || (work && work_bytes >= s.bytes && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
+            (unsigned long long)s.bytes);
     if (rows == 0 || outs == 0) return COMP_AMS_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const ProductShape s = product_shape(rows, cols, outs);
     ProductArgs a = {rows, outs, q_stride, w_stride, y_stride, (int)cols, (int)s.tiles_m, (int)s.tiles_n, s.splits, s.k_split, 0};
     const int64_t blocks = s.tiles_m * s.tiles_n * s.splits;
-    // memory to LDS without registers: whole 16-byte chunks, and a tile's rows within 31 bits
-    const int64_t most_stride = kLimit31 / 512;
-    const bool direct = aligned(q, 16) && aligned(w, 16) && cols % 16 == 0 && (rows == 1 || (q_stride % 16 == 0 && q_stride < most_stride)) &&
-                        (outs == 1 || (w_stride % 16 == 0 && w_stride < most_stride));
+    int8_t *memory = static_cast<int8_t *>(work);
+    if (!s.few && cols && !(q_aligned && w_aligned)) {
+        PackArgs pa = {rows, outs, q_stride, w_stride, s.ld, (int)cols, shared_lanes(s.ld / 16), 0, 0};
+        const int64_t blocks_x = q_aligned ? 0 : ceil_div(rows, kPackThreads / pa.lanes), blocks_w = w_aligned ? 0 : ceil_div(outs, kPackThreads / pa.lanes);
+        REQUIRE(blocks_x + blocks_w <= kMaxBlocks, "%s: rows and outs are too many for one call", what);
+        pa.blocks_x = (unsigned)blocks_x;
+        in_launches(blocks_x + blocks_w, kPackThreads, [&](unsigned first, unsigned count) {
+            pa.first = first;
+            product8_pack<<<count, kPackThreads, 0, stream>>>(memory + s.x_at, memory + s.w_at, q, w, pa);
+        });
+        if (const int rc = launched(what)) return rc;          // what the product would read has not been written
+        if (!q_aligned) q = memory + s.x_at, a.x_stride = s.ld;
+        if (!w_aligned) w = memory + s.w_at, a.w_stride = s.ld;
+        a.cols = (int)s.ld;
+    }
+    int *sums = reinterpret_cast<int *>(memory + s.sums_at);
     int rc = COMP_AMS_OK;
     with_type(type, [&](auto t) {
         using Y = decltype(t);
@@ -428,24 +460,23 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
         auto go = [&](auto kernel, int threads) {
             in_launches(blocks, threads, [&](unsigned first, unsigned count) {
                 a.first = first;
-                kernel<<<count, threads, 0, stream>>>(yt, static_cast<int *>(work), q, scale, w, w_scale, bias, a);
+                kernel<<<count, threads, 0, stream>>>(yt, sums, q, scale, w, w_scale, bias, a);
             });
         };
         if (s.splits > 1) {
-            if (direct) go(product8<Y, 128, 128, 2, 2, true, true>, 256);
-            else go(product8<Y, 128, 128, 2, 2, false, true>, 256);
+            go(product8<Y, 64, 64, 2, 2, true>, 256);
             rc = launched(what);                               // unless it is good, what the join would read has not been written
             if (rc) return;
             in_launches(ceil_div(ceil_div(outs, 4) * rows, kProductThreads), kProductThreads, [&](unsigned first, unsigned count) {
                 a.first = first;
-                product8_join<Y><<<count, kProductThreads, 0, stream>>>(yt, static_cast<const int *>(work), scale, w_scale, bias, a);
+                product8_join<Y><<<count, kProductThreads, 0, stream>>>(yt, sums, scale, w_scale, bias, a);
             });
         } else if (s.tile == 256) {
-            if (direct) go(product8<Y, 256, 256, 2, 4, true, false>, 512);
-            else go(product8<Y, 256, 256, 2, 4, false, false>, 512);
+            go(product8<Y, 256, 256, 2, 4, false>, 512);
+        } else if (s.tile == 128) {
+            go(product8<Y, 128, 128, 2, 2, false>, 256);
         } else {
-            if (direct) go(product8<Y, 128, 128, 2, 2, true, false>, 256);
-            else go(product8<Y, 128, 128, 2, 2, false, false>, 256);
+            go(product8<Y, 64, 64, 2, 2, false>, 256);
         }
     });
     return rc ? rc : launched(what);

@@ -113,14 +113,15 @@ struct WeightArgs {
     unsigned first;
 };
 
-constexpr int kWeightStep = 64;          // rows in LDS at a time
+constexpr int kWeightStep = 32;          // rows in a stage of LDS
 
 // A tile of kI input channels x kO output channels by kWavesI x kWavesO wavefronts.  kInFirst: the result is [i][o], otherwise [o][i].
 //
-// In LDS a row's 32-byte blocks (the 16 columns of a fragment) stand at place block ^ (row & 7): a transposing read takes 32 bytes from each of
-// four rows at a time, and these lie in different banks.
+// A transposing read takes 32 bytes, the 16 columns of a fragment, from each of four rows at a time, and these are to lie in different banks: a
+// row's 32-byte blocks stand at place block ^ (row & 3); where a load's 1024 bytes are two rows only, at block ^ (row & 1), and loads stand 64
+// bytes further apart.  All fragments of a lane then lie at a few addresses and constant distances from them.  Four stages as in product8.
 template <typename G, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
-__global__ __launch_bounds__(kWavesI *kWavesO *kWave) void weight_grad(G *__restrict__ out, const bf16_t *__restrict__ a_rows,
+__global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__restrict__ out, const bf16_t *__restrict__ a_rows,
                                                                        const bf16_t *__restrict__ b_rows, WeightArgs a)
 {
     constexpr int kWaves = kWavesI * kWavesO;
@@ -129,8 +130,10 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave) void weight_grad(G *__rest
     constexpr int kRowsI = 1024 / kBytesI, kRowsO = 1024 / kBytesO;          // rows of a wavefront-wide load
     constexpr int kLoadsI = kWeightStep / kRowsI / kWaves, kLoadsO = kWeightStep / kRowsO / kWaves;
     static_assert(kLoadsI * kRowsI * kWaves == kWeightStep && kLoadsO * kRowsO * kWaves == kWeightStep, "whole loads");
-    constexpr int kStage = kWeightStep * (kBytesI + kBytesO);
-    __shared__ __attribute__((aligned(1024))) int8_t tile[2][kStage];
+    constexpr int kSwapI = kRowsI == 2 ? 1 : 3, kSwapO = kRowsO == 2 ? 1 : 3;
+    constexpr int kLoadI = kRowsI == 2 ? 1088 : 1024, kLoadO = kRowsO == 2 ? 1088 : 1024;      // bytes from load to load in LDS
+    constexpr int kPartI = kWeightStep / kRowsI * kLoadI, kPartO = kWeightStep / kRowsO * kLoadO, kStages = 4;
+    __shared__ __attribute__((aligned(1024))) int8_t tile[kStages][kPartI + kPartO];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     int set, ti, to;
@@ -144,37 +147,36 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave) void weight_grad(G *__rest
     // a lane's part of each load: its row, and the 16 bytes that belong to its place there
     constexpr uint32_t kNowhere = 0x80000000u;       // past the end of any buffer: reads zeros
     uint32_t off_i[kLoadsI], off_o[kLoadsO];
-    auto offset = [&](int first, int row_bytes, int64_t left, int64_t ld) {
+    auto offset = [&](int first, int row_bytes, int swap, int64_t left, int64_t ld) {
         const int row = first + lane / (row_bytes / 16), place = lane % (row_bytes / 16);
-        const int column = ((place >> 1) ^ (row & 7)) * 16 + (place & 1) * 8;
+        const int column = ((place >> 1) ^ (row & swap)) * 16 + (place & 1) * 8;
         return column < left ? (uint32_t)((row * ld + column) * 2) : kNowhere;
     };
 #pragma unroll
-    for (int j = 0; j < kLoadsI; ++j) off_i[j] = offset((j * kWaves + wave) * kRowsI, kBytesI, a.cols - i0, a.a_ld);
+    for (int j = 0; j < kLoadsI; ++j) off_i[j] = offset((j * kWaves + wave) * kRowsI, kBytesI, kSwapI, a.cols - i0, a.a_ld);
 #pragma unroll
-    for (int j = 0; j < kLoadsO; ++j) off_o[j] = offset((j * kWaves + wave) * kRowsO, kBytesO, a.outs - o0, a.b_ld);
-    int step = begin % max(steps, 1), plane = begin / max(steps, 1);
-    auto send = [&](int stage) {                     // the next step's rows, asynchronous
-        const int64_t first = (int64_t)step * kWeightStep;
-        const __amdgpu_buffer_rsrc_t asrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(at + first * a.a_ld), 0, 0x7fffffff, 0x00020000);
-        const __amdgpu_buffer_rsrc_t bsrc =
-            __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(bt + plane * a.b_plane + first * a.b_ld), 0, 0x7fffffff, 0x00020000);
-        const int left = rows - step * kWeightStep;
+    for (int j = 0; j < kLoadsO; ++j) off_o[j] = offset((j * kWaves + wave) * kRowsO, kBytesO, kSwapO, a.outs - o0, a.b_ld);
+    int step = begin % max(steps, 1), unsent = end - begin;
+    const bf16_t *a_next = at + (int64_t)step * kWeightStep * a.a_ld;
+    const bf16_t *b_next = bt + begin / max(steps, 1) * a.b_plane + (int64_t)step * kWeightStep * a.b_ld;
+    const int64_t a_back = (int64_t)steps * kWeightStep * a.a_ld, b_back = (int64_t)steps * kWeightStep * a.b_ld - a.b_plane;
+    auto send = [&](int stage) {                     // the next step's rows, memory to LDS, asynchronous; zeros after the last one
+        // buffers that end with the worker's last row
+        const int left = unsent > 0 ? min(rows - step * kWeightStep, kWeightStep) : 0;
+        --unsent;
+        const v4u asrc = raw_buffer(a_next, (uint32_t)left * (uint32_t)a.a_ld * 2u);
+        const v4u bsrc = raw_buffer(b_next, (uint32_t)left * (uint32_t)a.b_ld * 2u);
 #pragma unroll
-        for (int j = 0; j < kLoadsI; ++j) {
-            const int row = (j * kWaves + wave) * kRowsI;
-            uint32_t from = off_i[j];
-            if (left < kWeightStep && row + lane / (kBytesI / 16) >= left) from = kNowhere;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(asrc, (lds_bytes *)&tile[stage][row * kBytesI], 16, from, 0, 0, 0);
+        for (int j = 0; j < kLoadsI; ++j) to_lds(asrc, off_i[j], &tile[stage][(j * kWaves + wave) * kLoadI]);
+#pragma unroll
+        for (int j = 0; j < kLoadsO; ++j) to_lds(bsrc, off_o[j], &tile[stage][kPartI + (j * kWaves + wave) * kLoadO]);
+        a_next += kWeightStep * a.a_ld;
+        b_next += kWeightStep * a.b_ld;
+        if (++step == steps) {                       // the next plane
+            step = 0;
+            a_next -= a_back;
+            b_next -= b_back;
         }
-#pragma unroll
-        for (int j = 0; j < kLoadsO; ++j) {
-            const int row = (j * kWaves + wave) * kRowsO;
-            uint32_t from = off_o[j];
-            if (left < kWeightStep && row + lane / (kBytesO / 16) >= left) from = kNowhere;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(bsrc, (lds_bytes *)&tile[stage][kWeightStep * kBytesI + row * kBytesO], 16, from, 0, 0, 0);
-        }
-        if (++step == steps) step = 0, ++plane;
     };
 
     v4f acc[kIi][kOi];
@@ -187,41 +189,70 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave) void weight_grad(G *__rest
     // Transposing read: the 16 lanes of a group point at four rows of 16 columns, 8 bytes each; lane c of them receives column c of the four.
     // A lane's eight values of the sum's index are rows 8 g .. 8 g + 7 for its group g.
     const int trow = fgroup * 8 + frow / 4;
-    auto fragment = [&](const int8_t *base, int row_bytes, int block) {
+    constexpr int kAtI = kIi < kSwapI + 1 ? kIi : kSwapI + 1, kAtO = kOi < kSwapO + 1 ? kOi : kSwapO + 1;
+    int at_i[kAtI], at_o[kAtO];                      // of the first fragments
+#pragma unroll
+    for (int i = 0; i < kAtI; ++i)
+        at_i[i] = trow / kRowsI * kLoadI + trow % kRowsI * kBytesI + ((wi * kIi + i) ^ (trow & kSwapI)) * 32 + frow % 4 * 8;
+#pragma unroll
+    for (int o = 0; o < kAtO; ++o)
+        at_o[o] = kPartI + trow / kRowsO * kLoadO + trow % kRowsO * kBytesO + ((wo * kOi + o) ^ (trow & kSwapO)) * 32 + frow % 4 * 8;
+    auto fragment = [&](const int8_t *low, int four_rows) {
         typedef __attribute__((address_space(3))) v4s lds_v4s;
-        const int low = trow * row_bytes + ((block ^ (frow / 4)) * 32) + frow % 4 * 8;
-        const int high = (trow + 4) * row_bytes + ((block ^ (frow / 4 + 4)) * 32) + frow % 4 * 8;
-        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(base + low));
-        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(base + high));
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)low);
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(low + four_rows));
         return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    auto work_on = [&](int stage) {
-#pragma unroll
-        for (int kk = 0; kk < kWeightStep / 32; ++kk) {
-            const int8_t *ib = &tile[stage][kk * 32 * kBytesI], *ob = &tile[stage][kWeightStep * kBytesI + kk * 32 * kBytesO];
-            v8bf af[kIi], bf[kOi];
-#pragma unroll
-            for (int i = 0; i < kIi; ++i) af[i] = fragment(ib, kBytesI, wi * kIi + i);
-#pragma unroll
-            for (int o = 0; o < kOi; ++o) bf[o] = fragment(ob, kBytesO, wo * kOi + o);
-#pragma unroll
-            for (int o = 0; o < kOi; ++o)
-#pragma unroll
-                for (int i = 0; i < kIi; ++i) {
-                    if constexpr (kInFirst) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[o], af[i], acc[i][o], 0, 0, 0);
-                    else acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[i], bf[o], acc[i][o], 0, 0, 0);
-                }
-        }
+    constexpr int kFourI = 4 * kBytesI + (kLoadI - 1024) * 4 / kRowsI, kFourO = 4 * kBytesO + (kLoadO - 1024) * 4 / kRowsO;
+    struct Frags {
+        v8bf i[kIi], o[kOi];
     };
-
-    if (begin < end) send(0);
-    int stage = 0;
-    for (int c = begin; c < end; ++c, stage ^= 1) {
-        // this stage has arrived, for every wavefront, and nobody reads the other one any more
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (c + 1 < end) send(stage ^ 1);
-        work_on(stage);
+    auto read = [&](Frags &f, int stage) {
+#pragma unroll
+        for (int o = 0; o < kOi; ++o) f.o[o] = fragment(&tile[stage][at_o[o % kAtO] + o / kAtO * kAtO * 32], kFourO);
+#pragma unroll
+        for (int i = 0; i < kIi; ++i) f.i[i] = fragment(&tile[stage][at_i[i % kAtI] + i / kAtI * kAtI * 32], kFourI);
+    };
+    auto multiply = [&](const Frags &f) {
+#pragma unroll
+        for (int i = 0; i < kIi; ++i)
+#pragma unroll
+            for (int o = 0; o < kOi; ++o) {
+                if constexpr (kInFirst) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.o[o], f.i[i], acc[i][o], 0, 0, 0);
+                else acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.i[i], f.o[o], acc[i][o], 0, 0, 0);
+            }
+    };
+    constexpr int kReads = 2 * (kIi + kOi), kPer = kIi * kOi / kReads;
+    auto mixed = [&]() {
+#pragma unroll
+        for (int u = 0; u < kReads; ++u) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);          // a read from LDS
+            __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);       // matrix instructions
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kIi * kOi - kPer * kReads, 0);
+    };
+    constexpr int kLoads = kLoadsI + kLoadsO;
+    auto advance = [&](int u, const Frags &now, Frags &next) {          // a step, as in product8
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+        send((u + 3) % kStages);
+        read(next, (u + 1) % kStages);
+        multiply(now);
+        mixed();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    Frags even, odd;
+    send(0);
+    send(1);
+    send(2);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
+    read(even, 0);
+    for (int c = begin; c < end; c += kStages) {
+        advance(0, even, odd);
+        advance(1, odd, even);
+        advance(2, even, odd);
+        advance(3, odd, even);
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");         // LDS belongs to the next workgroup after this one
 
     G *ot = out + worker * a.worker_stride + piece * a.piece_stride;
     const int64_t across = kInFirst ? a.cols : a.outs, along = kInFirst ? a.outs : a.cols;

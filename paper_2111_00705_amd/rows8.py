@@ -27,6 +27,11 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _sixteens(t, stride):
+    """Whether an int8 or 16-bit array is known to have its rows at multiples of 16 bytes."""
+    return 1 if (t.data_ptr() | stride * t.element_size()) % 16 == 0 and stride < 1 << 22 else 0
+
+
 def _leading(t, rows, what):
     """A dense float32 tensor of one number a row."""
     import torch
@@ -158,7 +163,7 @@ def linear_q8(q, scale, weight, weight_scale, bias=None, dtype=None, out=None):
         out = torch.empty((*q.shape[:-1], outs), dtype=torch.bfloat16 if dtype is None else dtype, device=q.device)
     _need(out.shape == (*q.shape[:-1], outs) and dtype in (None, out.dtype), "out must be [..., outs] of the type asked for")
     kind = _type(out)
-    work, work_ptr, work_bytes = _work("comp_ams_linear_q8_work_bytes", q.device, rows, cols, outs)
+    work, work_ptr, work_bytes = _work("comp_ams_linear_q8_work_bytes", q.device, rows, cols, outs, _sixteens(q, q_stride), _sixteens(weight, w_stride))
     _check(lib().comp_ams_linear_q8(out.data_ptr(), q.data_ptr(), scale.data_ptr(), weight.data_ptr(), weight_scale.data_ptr(), _ptr(bias), rows, cols,
                                     outs, _rows(out, "out")[2], q_stride, w_stride, kind, work_ptr, work_bytes, s))
     return out
@@ -189,6 +194,6 @@ def linear_weight_grad(dy, q, scale, dweight, dbias=None, binary=False):
               "dbias must be [n, outs] with the type and worker stride of dweight")
     s = _stream(dy, q, scale, dweight, dbias)
     work, work_ptr, work_bytes = _work("comp_ams_linear_weight_grad_work_bytes", dy.device, rows, cols, outs, n, 1 if binary else 0, kind,
-                                       1 if dy.data_ptr() % 16 == 0 and dy_stride % 8 == 0 else 0)
+                                       _sixteens(dy, dy_stride))
     _check(lib().comp_ams_linear_weight_grad(dweight.data_ptr(), _ptr(dbias), dy.data_ptr(), q.data_ptr(), scale.data_ptr(), rows, cols, outs, dy_stride,
                                              q_stride, n, stride, 1 if in_first else 0, 1 if binary else 0, kind, _type(dweight), work_ptr, work_bytes, s))

@@ -43,9 +43,9 @@ int main(void)
     EXPECT(comp_ams_linear_q8(buf, bytes8, buf, bytes8, buf, NULL, 2, 4, 3, 3, far, 4, COMP_AMS_F32, NULL, 0, NULL), COMP_AMS_EINVAL);
     EXPECT(comp_ams_linear_q8(buf, bytes8, buf, bytes8, buf, NULL, far, 4, far, 3, 4, 4, COMP_AMS_F32, NULL, 0, NULL), COMP_AMS_EINVAL);
     EXPECT(comp_ams_linear_q8(NULL, NULL, NULL, bytes8, buf, NULL, 0, 4, 3, 3, 4, 4, COMP_AMS_F32, NULL, 0, NULL), COMP_AMS_OK);
-    EXPECT(comp_ams_linear_q8_work_bytes(2147483647, 131071, 2147483647, &bytes), COMP_AMS_EINVAL);
-    EXPECT(comp_ams_linear_q8_work_bytes(0, 0, 0, &bytes), COMP_AMS_OK);
-    EXPECT(comp_ams_linear_q8_work_bytes(100, 131071, 100, &bytes), COMP_AMS_OK);
+    EXPECT(comp_ams_linear_q8_work_bytes(2147483647, 131071, 2147483647, 0, 0, &bytes), COMP_AMS_EINVAL);
+    EXPECT(comp_ams_linear_q8_work_bytes(0, 0, 0, 0, 0, &bytes), COMP_AMS_OK);
+    EXPECT(comp_ams_linear_q8_work_bytes(100, 131071, 100, 0, 1, &bytes), COMP_AMS_OK);
     EXPECT(comp_ams_linear_weight_grad(buf, buf, buf, bytes8, buf, 4, 4, 3, far, 4, 2, 16, 0, 0, COMP_AMS_F32, COMP_AMS_F32, buf, 256, NULL), COMP_AMS_EINVAL);
     EXPECT(comp_ams_linear_weight_grad(buf, buf, buf, bytes8, buf, 4, far, far, 4, 4, 2, 16, 0, 0, COMP_AMS_F32, COMP_AMS_F32, buf, 256, NULL), COMP_AMS_EINVAL);
     EXPECT(comp_ams_linear_weight_grad_work_bytes(0, 0, 0, 1, 0, COMP_AMS_F32, 1, &bytes), COMP_AMS_OK);

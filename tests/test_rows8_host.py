@@ -46,7 +46,7 @@ CALLS = [
     ("linear_q8", LINEAR, [dict(y=None), dict(q=None), dict(scale=None), dict(w=None), dict(w_scale=None), dict(rows=-1), dict(rows=B31), dict(cols=-1),
                            dict(cols=131_072), dict(outs=-1), dict(outs=B31), dict(y_stride=5), dict(q_stride=7), dict(w_stride=7), dict(type=3), dict(y=A + 2),
                            dict(bias=A + 2), dict(scale=A + 1), dict(w_scale=A + 2), dict(rows=B31 - 1, outs=B31 - 1, y_stride=1 << 29),
-                           dict(rows=100, cols=4096, outs=100, q_stride=4096, w_stride=4096, y_stride=100)]),
+                           dict(rows=100, cols=4096, outs=100, q_stride=4096, w_stride=4096, y_stride=100), dict(rows=100, cols=9, q_stride=9, w_stride=9)]),
     ("linear_weight_grad", WEIGHT, [dict(dweight=None), dict(dy=None), dict(q=None), dict(scale=None), dict(rows=-2), dict(rows=5), dict(n=0), dict(n=70_000),
                                     dict(cols=-1), dict(cols=B31), dict(outs=B31), dict(cols=1 << 21, outs=1 << 20), dict(dy_stride=5), dict(q_stride=7),
                                     dict(grad_stride=47), dict(type=3), dict(grad_type=-1), dict(work=None), dict(work_bytes=8), dict(work=A + 8),
@@ -73,8 +73,8 @@ def test_work_bytes():
     L, n = P.lib(), C.c_uint64(99)
     assert L.comp_ams_rms_norm_work_bytes(4096, 768, 8, C.byref(n)) == P.OK and n.value >= 8 * 768 * 4
     assert L.comp_ams_rms_norm_work_bytes(4097, 768, 8, C.byref(n)) == P.EINVAL and L.comp_ams_rms_norm_work_bytes(4096, 768, 8, None) == P.EINVAL
-    assert L.comp_ams_linear_q8_work_bytes(4, 4096, 4096, C.byref(n)) == P.OK and n.value == 0
-    assert L.comp_ams_linear_q8_work_bytes(4, 131_072, 4096, C.byref(n)) == P.EINVAL and L.comp_ams_linear_q8_work_bytes(4, 5, 6, None) == P.EINVAL
+    assert L.comp_ams_linear_q8_work_bytes(4, 4096, 4096, 0, 0, C.byref(n)) == P.OK and n.value == 0
+    assert L.comp_ams_linear_q8_work_bytes(4, 131_072, 4096, 1, 1, C.byref(n)) == P.EINVAL and L.comp_ams_linear_q8_work_bytes(4, 5, 6, 0, 0, None) == P.EINVAL
     assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 8, 1, 1, 1, C.byref(n)) == P.OK
     assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 7, 1, 1, 1, C.byref(n)) == P.EINVAL
     assert L.comp_ams_linear_weight_grad_work_bytes(4096, 768, 768, 8, 1, 7, 1, C.byref(n)) == P.EINVAL
