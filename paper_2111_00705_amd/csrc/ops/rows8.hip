@@ -103,10 +103,27 @@ int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rs
 
 // --- the product -----------------------------------------------------------------------------------------------------
 
+// What a tile costs, for the choice among them: us of a step of `alone` for the first workgroup of a compute unit and of `more` for each
+// that it takes besides.  Fitted to kernels timed over 17 (products) and 15 (weight gradients) sizes from 16 x 4096 x 4096 to 4096 x 4096 x 4096; what is chosen
+// was within 8 % of the best there, where one tile for all would be up to 4 times off.
+struct TileCost {
+    int high, wide;
+    double alone, more;
+    bool splits;             // whether the sum may be cut into pieces
+};
+double tile_cost(const TileCost &t, int64_t tiles, int64_t pieces, int64_t steps, double cells)
+{
+    const double deep = (double)ceil_div(std::max<int64_t>(tiles * pieces, 1), 256);
+    const double join = pieces > 1 ? 4.5 + (double)(pieces + 1) * cells * 4.0 / 3e6 : 0.0;      // a launch, and the pieces' sums back from memory
+    return (t.alone + (deep - 1) * t.more) * (double)steps + join;
+}
+constexpr TileCost kProductTiles[] = {{256, 256, 1.05, 1.05, false}, {256, 128, 0.62, 0.62, false}, {128, 128, 0.40, 0.33, false},
+                                      {64, 128, 0.23, 0.22, false}, {64, 64, 0.155, 0.138, true}};
+
 // Which kernel takes a product, into how many pieces k is cut, and where the work memory holds what.
 struct ProductShape {
     int few;                 // tokens in sixteens for product8_few, or 0
-    int tile;                // tokens and channels of a tile
+    int high, wide;          // tokens and channels of a tile
     int splits, k_split;
     int64_t tiles_m, tiles_n, ld;
     uint64_t x_at, w_at, sums_at, bytes;
@@ -115,19 +132,23 @@ ProductShape product_shape(int64_t rows, int64_t cols, int64_t outs, bool x_alig
 {
     ProductShape s = {};
     s.splits = 1;
-    if (rows <= 64) {
-        s.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    if (rows <= 32) {
+        s.few = rows <= 16 ? 1 : 2;
         s.tiles_m = 1, s.tiles_n = ceil_div(outs, 16);
         return s;
     }
-    for (s.tile = 256;; s.tile /= 2) {
-        s.tiles_m = ceil_div(rows, s.tile), s.tiles_n = ceil_div(outs, s.tile);
-        if (s.tile == 64 || s.tiles_m * s.tiles_n >= 200) break;
-    }
-    const int64_t tiles = s.tiles_m * s.tiles_n, steps = ceil_div(std::max<int64_t>(cols, 1), kProductStep);
-    const int64_t pieces = tiles > 0 && tiles < 128 ? std::max<int64_t>(1, std::min(256 / tiles, steps / 16)) : 1;
-    s.k_split = (int)(ceil_div(steps, pieces) * kProductStep);
-    s.splits = (int)ceil_div(steps * kProductStep, s.k_split);
+    const int64_t steps = ceil_div(std::max<int64_t>(cols, 1), kProductStep);
+    double best = 0;
+    for (const TileCost &t : kProductTiles)
+        for (int64_t pieces = 1; pieces <= (t.splits ? 16 : 1); pieces *= 2) {
+            const int64_t length = ceil_div(steps, pieces), tm = ceil_div(rows, t.high), tn = ceil_div(outs, t.wide);
+            if (pieces > 1 && length < 8) break;
+            const double us = tile_cost(t, tm * tn, ceil_div(steps, length), length, (double)rows * (double)outs);
+            if (best && us >= best) continue;
+            best = us;
+            s.high = t.high, s.wide = t.wide, s.tiles_m = tm, s.tiles_n = tn;
+            s.k_split = (int)(length * kProductStep), s.splits = (int)ceil_div(steps, length);
+        }
     s.ld = ceil_div(cols, 16) * 16;
     if (cols % 16) x_aligned = w_aligned = false;
     s.x_at = 0;
@@ -151,6 +172,8 @@ int product_check(const char *what, int64_t rows, int64_t cols, int64_t outs)
 
 constexpr int64_t kMostChannels = (int64_t)1 << 23;      // a step's rows lie within 31 bits
 
+constexpr TileCost kWeightTiles[] = {{256, 256, 0.83, 0.83, false}, {128, 128, 0.32, 0.24, true}, {64, 64, 0.16, 0.11, true}};
+
 // How a call is cut, and where its work memory holds what.
 struct WeightShape {
     int tile;                // input and output channels of a tile
@@ -168,15 +191,17 @@ WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bo
     WeightShape s = {};
     s.planes = type == COMP_AMS_F32 ? 3 : type == COMP_AMS_BF16 && binary ? 1 : 2;
     s.copied = s.planes > 1 || !dy_aligned || outs % 8 != 0;
-    for (s.tile = 256;; s.tile /= 2) {
-        s.tiles_i = ceil_div(cols, s.tile), s.tiles_o = ceil_div(outs, s.tile);
-        if (s.tile == 64 || s.tiles_i * s.tiles_o * n >= 200) break;
-    }
-    const int64_t tiles = s.tiles_i * s.tiles_o * n, steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.planes);
-    int64_t pieces = 1;
-    if (tiles > 0 && tiles < 200) pieces = std::max<int64_t>(1, std::min(512 / tiles, steps / 16));
-    s.split_steps = ceil_div(steps, pieces);
-    s.splits = ceil_div(steps, s.split_steps);
+    const int64_t steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.planes);
+    double best = 0;
+    for (const TileCost &t : kWeightTiles)
+        for (int64_t pieces = 1; pieces <= (t.splits ? 16 : 1); pieces *= 2) {
+            const int64_t length = ceil_div(steps, pieces), ti = ceil_div(cols, t.high), to = ceil_div(outs, t.wide);
+            if (pieces > 1 && length < 8) break;
+            const double us = tile_cost(t, ti * to * n, ceil_div(steps, length), length, (double)cols * (double)outs * n);
+            if (best && us >= best) continue;
+            best = us;
+            s.tile = t.high, s.tiles_i = ti, s.tiles_o = to, s.split_steps = length, s.splits = ceil_div(steps, length);
+        }
     const int64_t want = std::max<int64_t>(1, 1024 / (n * ceil_div(std::max<int64_t>(outs, 1), kRmsThreads)));
     s.bias_rows = std::max<int64_t>(16, ceil_div(per, want));
     s.bias_chunks = std::max<int64_t>(1, ceil_div(per, s.bias_rows));
@@ -453,8 +478,7 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
                 });
             };
             if (s.few == 1) go(product8_few<Y, 1>);
-            else if (s.few == 2) go(product8_few<Y, 2>);
-            else go(product8_few<Y, 4>);
+            else go(product8_few<Y, 2>);
             return;
         }
         auto go = [&](auto kernel, int threads) {
@@ -471,10 +495,13 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
                 a.first = first;
                 product8_join<Y><<<count, kProductThreads, 0, stream>>>(yt, sums, scale, w_scale, bias, a);
             });
-        } else if (s.tile == 256) {
-            go(product8<Y, 256, 256, 2, 4, false>, 512);
-        } else if (s.tile == 128) {
+        } else if (s.high == 256) {
+            if (s.wide == 256) go(product8<Y, 256, 256, 2, 4, false>, 512);
+            else go(product8<Y, 256, 128, 4, 2, false>, 512);
+        } else if (s.high == 128) {
             go(product8<Y, 128, 128, 2, 2, false>, 256);
+        } else if (s.wide == 128) {
+            go(product8<Y, 64, 128, 2, 2, false>, 256);
         } else {
             go(product8<Y, 64, 64, 2, 2, false>, 256);
         }
