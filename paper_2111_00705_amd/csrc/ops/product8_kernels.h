@@ -18,6 +18,7 @@ struct ProductArgs {
     int tiles_m, tiles_n;
     int splits, k_split;         // pieces of k and their length, a multiple of kProductStep
     unsigned first;
+    bool stream_out;             // y is stored as a stream
 };
 
 constexpr int kProductStep = 64;         // bytes of k in a stage of LDS
@@ -65,6 +66,50 @@ __device__ __forceinline__ v4i load_row16(const int8_t *row, int k, int cols)
         }
     }
     return v;
+}
+
+// Sixteen rows of kFrags fragments each from a wavefront to memory: a lane holds columns 16 f + 4 (lane / 16) + 0..3 of row lane % 16.  Through the
+// wavefront's own piece of LDS, so that a store takes 16 neighbouring bytes a lane and whole lines a row: stored as they are held, in
+// pieces of 8 bytes, the 134 MB of 16384 x 4096 results took 110 us of 330.
+// rows, cols: how many there are from the first on.
+template <typename Y, int kFrags> constexpr int kSixteenLd = kFrags * 16 + 16 / (int)sizeof(Y);       // elements from row to row in LDS
+template <typename Y, int kFrags>
+__device__ __forceinline__ void store_sixteen(Y *lds, const Y (&v)[kFrags][4], Y *to, int64_t stride, int64_t rows, int64_t cols, bool stream)
+{
+    constexpr int E = 16 / (int)sizeof(Y), kLd = kSixteenLd<Y, kFrags>, kLanes = kFrags * 16 / E, kRows = kWave / kLanes;
+    const int lane = threadIdx.x % kWave;
+    Y *mine = lds + (lane & 15) * kLd + (lane >> 4) * 4;
+#pragma unroll
+    for (int f = 0; f < kFrags; ++f) {
+        if constexpr (sizeof(Y) == 4) *reinterpret_cast<v4u *>(mine + f * 16) = v4u{bits1(v[f][0]), bits1(v[f][1]), bits1(v[f][2]), bits1(v[f][3])};
+        else *reinterpret_cast<uint64_t *>(mine + f * 16) = (uint64_t)(bits1(v[f][2]) | (bits1(v[f][3]) << 16)) << 32 | (bits1(v[f][0]) | (bits1(v[f][1]) << 16));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const int col = lane % kLanes * E;
+#pragma unroll
+    for (int r = 0; r < 16; r += kRows) {
+        const int row = r + lane / kLanes;
+        const v4u raw = *reinterpret_cast<const v4u *>(lds + row * kLd + col);
+        if (row >= rows || col >= cols) continue;
+        Y *p = to + row * stride + col;
+        if (col + E <= cols) {
+            store_vec(p, raw, stream);
+        } else {
+#pragma unroll
+            for (int q = 0; q < E; ++q) {
+                const uint32_t bits = sizeof(Y) == 4 ? raw[q * (int)sizeof(Y) / 4] : raw[q / 2] >> (16 * (q & 1));
+                if (col + q < cols) {
+                    if constexpr (sizeof(Y) == 4) reinterpret_cast<uint32_t *>(p)[q] = bits;
+                    else reinterpret_cast<uint16_t *>(p)[q] = (uint16_t)bits;
+                }
+            }
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // Four neighbouring channels from n on of token m.
@@ -244,21 +289,14 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__rest
         step(2, even, odd);
         step(3, odd, even);
     }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");         // LDS belongs to the next workgroup after this one
-
+    if constexpr (kSplit) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");     // LDS belongs to the next workgroup after this one
 #pragma unroll
-    for (int n = 0; n < kNi; ++n) {
-        const int64_t at_n = n0 + (wn * kNi + n) * 16 + fgroup * 4;
-        float ws[4], b[4];
-        if constexpr (!kSplit) {
-            load_channels(ws, w_scale, at_n, a.outs);
-            load_channels(b, bias, at_n, a.outs);
-        }
+        for (int n = 0; n < kNi; ++n)
 #pragma unroll
-        for (int m = 0; m < kMi; ++m) {
-            const int64_t at_m = m0 + (wm * kMi + m) * 16 + frow;
-            if (at_m >= a.rows || at_n >= a.outs) continue;
-            if constexpr (kSplit) {
+            for (int m = 0; m < kMi; ++m) {
+                const int64_t at_n = n0 + (wn * kNi + n) * 16 + fgroup * 4, at_m = m0 + (wm * kMi + m) * 16 + frow;
+                if (at_m >= a.rows || at_n >= a.outs) continue;
                 int *p = work + ((int64_t)piece * a.rows + at_m) * a.outs + at_n;
                 if (at_n + 4 <= a.outs) {
                     *reinterpret_cast<v4u_any *>(p) = __builtin_bit_cast(v4u, acc[n][m]);
@@ -267,9 +305,32 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__rest
                     for (int q = 0; q < 4; ++q)
                         if (at_n + q < a.outs) p[q] = acc[n][m][q];
                 }
-            } else {
-                store_channels<Y>(y, acc[n][m], x_scale[at_m], ws, b, at_m, at_n, a);
             }
+    } else {
+        float ws[kNi][4], b[kNi][4], xs[kMi];
+#pragma unroll
+        for (int n = 0; n < kNi; ++n) {
+            load_channels(ws[n], w_scale, n0 + (wn * kNi + n) * 16 + fgroup * 4, a.outs);
+            load_channels(b[n], bias, n0 + (wn * kNi + n) * 16 + fgroup * 4, a.outs);
+        }
+#pragma unroll
+        for (int m = 0; m < kMi; ++m) {
+            const int64_t at_m = m0 + (wm * kMi + m) * 16 + frow;
+            xs[m] = at_m < a.rows ? x_scale[at_m] : 0.f;
+        }
+        // nothing is on its way to LDS or read from it any more, by any wavefront
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        Y *mine = reinterpret_cast<Y *>(&tile[0][0]) + wave * 16 * kSixteenLd<Y, kNi>;
+        static_assert(kWaves * 16 * kSixteenLd<Y, kNi> * sizeof(Y) <= sizeof tile, "room for the results");
+#pragma unroll
+        for (int m = 0; m < kMi; ++m) {
+            Y out[kNi][4];
+#pragma unroll
+            for (int n = 0; n < kNi; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) out[n][q] = narrow1<Y>((float)acc[n][m][q] * xs[m] * ws[n][q] + b[n][q]);
+            const int64_t at_m = m0 + (wm * kMi + m) * 16, at_n = n0 + wn * kNi * 16;
+            store_sixteen<Y, kNi>(mine, out, y + at_m * a.y_stride + at_n, a.y_stride, a.rows - at_m, a.outs - at_n, a.stream_out);
         }
     }
 }

@@ -448,7 +448,7 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
             (unsigned long long)s.bytes);
     if (rows == 0 || outs == 0) return COMP_AMS_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    ProductArgs a = {rows, outs, q_stride, w_stride, y_stride, (int)cols, (int)s.tiles_m, (int)s.tiles_n, s.splits, s.k_split, 0};
+    ProductArgs a = {rows, outs, q_stride, w_stride, y_stride, (int)cols, (int)s.tiles_m, (int)s.tiles_n, s.splits, s.k_split, 0, streamed_out(rows * outs, type)};
     const int64_t blocks = s.tiles_m * s.tiles_n * s.splits;
     int8_t *memory = static_cast<int8_t *>(work);
     if (!s.few && cols && !(q_aligned && w_aligned)) {
@@ -552,6 +552,7 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
         a.worker_rows = per, a.out_stride = in_first ? outs : cols;
         a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.planes = s.planes;
         a.splits = (int)s.splits, a.split_steps = (int)s.split_steps;
+        a.stream_out = s.splits == 1 && streamed_out(cells * n, grad_type);
         const bf16_t *a_rows = reinterpret_cast<const bf16_t *>(memory + s.a_at);
         const bf16_t *b_rows = s.copied ? reinterpret_cast<const bf16_t *>(memory + s.b_at) : static_cast<const bf16_t *>(dy);
         if (s.splits > 1) {

@@ -111,6 +111,7 @@ struct WeightArgs {
     int tiles_i, tiles_o, n, planes;
     int splits, split_steps;                         // pieces of the sum over planes and steps of rows, and their length
     unsigned first;
+    bool stream_out;                                 // the result is stored as a stream
 };
 
 constexpr int kWeightStep = 32;          // rows in a stage of LDS
@@ -252,30 +253,24 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
         advance(2, even, odd);
         advance(3, odd, even);
     }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");         // LDS belongs to the next workgroup after this one
-
+    // nothing is on its way to LDS or read from it any more, by any wavefront
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     G *ot = out + worker * a.worker_stride + piece * a.piece_stride;
+    constexpr int kAcross = kInFirst ? kIi : kOi, kAlong = kInFirst ? kOi : kIi;     // fragments across the result's rows and along them
     const int64_t across = kInFirst ? a.cols : a.outs, along = kInFirst ? a.outs : a.cols;
+    const int64_t row0 = kInFirst ? i0 + wi * kIi * 16 : o0 + wo * kOi * 16, col0 = kInFirst ? o0 + wo * kOi * 16 : i0 + wi * kIi * 16;
+    G *mine = reinterpret_cast<G *>(&tile[0][0]) + wave * 16 * kSixteenLd<G, kAlong>;
+    static_assert(kWaves * 16 * kSixteenLd<G, kAlong> * sizeof(G) <= sizeof tile, "room for the results");
 #pragma unroll
-    for (int i = 0; i < kIi; ++i)
+    for (int x = 0; x < kAcross; ++x) {
+        G values[kAlong][4];
 #pragma unroll
-        for (int o = 0; o < kOi; ++o) {
-            const int64_t ci = i0 + (wi * kIi + i) * 16, co = o0 + (wo * kOi + o) * 16;
-            const int64_t row = (kInFirst ? ci : co) + frow, col = (kInFirst ? co : ci) + fgroup * 4;
-            if (row >= across || col >= along) continue;
-            G *p = ot + row * a.out_stride + col;
-            G four[4];
+        for (int y = 0; y < kAlong; ++y)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) four[c] = narrow1<G>(acc[i][o][c]);
-            if (col + 4 <= along) {
-                if constexpr (sizeof(G) == 4) *reinterpret_cast<v4u_any *>(p) = v4u{bits1(four[0]), bits1(four[1]), bits1(four[2]), bits1(four[3])};
-                else *reinterpret_cast<v2u_any *>(p) = v2u_any{bits1(four[0]) | (bits1(four[1]) << 16), bits1(four[2]) | (bits1(four[3]) << 16)};
-            } else {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (col + c < along) p[c] = four[c];
-            }
-        }
+            for (int c = 0; c < 4; ++c) values[y][c] = narrow1<G>(kInFirst ? acc[kInFirst ? x : 0][kInFirst ? y : 0][c] : acc[kInFirst ? 0 : y][kInFirst ? 0 : x][c]);
+        const int64_t row = row0 + x * 16;
+        store_sixteen<G, kAlong>(mine, values, ot + row * a.out_stride + col0, a.out_stride, across - row, along - col0, a.stream_out);
+    }
 }
 
 constexpr int kWeightJoinThreads = 256;
