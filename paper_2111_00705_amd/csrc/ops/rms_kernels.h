@@ -14,7 +14,7 @@ namespace cams_ops {
 struct RmsArgs {
     int64_t rows, cols, x_stride, r_stride, h_stride, y_stride;
     float eps, inv_cols;
-    bool binary, stream_out;
+    bool binary, stream_out, stream_h;
 };
 
 constexpr int kRmsThreads = 256;
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void rms_forward(void *y, float 
                 for (int q = 0; q < E; ++q) w[q] += u[q];
                 xraw[v] = narrow<T>(w);
             }
-            if (h) store_slab<T, kTeam>(h + row * a.h_stride, v * kTeam * E, me.lane, cols, xraw[v], v < kVecs - 1, a.stream_out);
+            if (h) store_slab<T, kTeam>(h + row * a.h_stride, v * kTeam * E, me.lane, cols, xraw[v], v < kVecs - 1, a.stream_h);
             widen<T>(xraw[v], d[v]);
 #pragma unroll
             for (int q = 0; q < E; ++q) s = fmaf(d[v][q], d[v][q], s);
@@ -332,20 +332,6 @@ __global__ __launch_bounds__(kRmsThreads) void columns_join(G *__restrict__ grad
 #pragma unroll
     for (int q = 1; q < kColumnsParts; ++q) s += parts[q][lane];
     grad[(int64_t)blockIdx.y * grad_stride + c] = narrow1<G>(s);
-}
-
-// Column sums of rows [chunk's rows] of one worker, for a bias' gradient: a lane takes 256 columns' worth of its own, one column each.
-template <typename T>
-__global__ __launch_bounds__(kRmsThreads) void column_sums(float *__restrict__ work, const T *__restrict__ dy, int64_t cols, int64_t stride,
-                                                           int64_t worker_rows, int64_t chunk_rows)
-{
-    const int64_t c = (int64_t)blockIdx.x * kRmsThreads + threadIdx.x;
-    if (c >= cols) return;
-    const int64_t lo = (int64_t)blockIdx.y * chunk_rows, hi = min(lo + chunk_rows, worker_rows);
-    float s = 0.f;
-#pragma unroll 4
-    for (int64_t q = lo; q < hi; ++q) s += widen1(dy[((int64_t)blockIdx.z * worker_rows + q) * stride + c]);
-    work[((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * cols + c] = s;
 }
 
 }  // namespace cams_ops

@@ -52,8 +52,13 @@ int rms_check(const char *what, int64_t rows, int64_t cols, int32_t type)
     return COMP_AMS_OK;
 }
 
-constexpr int64_t kRmsBlocks = 2048;         // workgroups of the forward pass
-constexpr int64_t kRmsChunkBlocks = 1024;    // workgroups that the rows of all workers are cut into in the backward pass
+// Workgroups of the forward pass, us at 1024 / 2048 / 4096: in 8 bits 16384 x 2048 bf16 47.5 / 45.4 / 43.0; 8192 x 4096 bf16 48.7 / 50.4 / 47.9;
+// 16384 x 768 19.4 / 20.4 / 20.7.
+constexpr int64_t kRmsBlocks = 4096;
+// Workgroups that the rows of all workers are cut into in the backward pass, and the fewest rows of one.  More keep more rows in flight, and write
+// more partial sums.  us with the join, at 512 / 750 / 1024 / 2048: 16384 x 768 bf16, n = 8 22.4 / 23.8 / 21.6 / 24.8; 20000 x 2047 fp32 kept in 8 bits,
+// n = 20 134 / 129 / 117 / 118; 8192 x 4096 bf16, n = 4 67.8 / 66.1 / 67.2 / 73.9.  1024 x 4096 bf16, n = 8 at 4 / 2 / 1 rows 15.6 / 16.5 / 23.2.
+constexpr int64_t kRmsChunkBlocks = 1024, kRmsChunkRows = 4;
 
 // How a worker's rows are cut for the gain's gradients: chunks of rows with one set of column sums each.
 struct RmsChunks {
@@ -62,9 +67,12 @@ struct RmsChunks {
 RmsChunks rms_chunks(int64_t worker_rows, int32_t n)
 {
     const int64_t want = std::max<int64_t>(1, ceil_div(kRmsChunkBlocks, n));
-    const int64_t rows = std::max<int64_t>(16, ceil_div(worker_rows, want));
+    const int64_t rows = std::max<int64_t>(kRmsChunkRows, ceil_div(worker_rows, want));
     return {rows, std::max<int64_t>(1, ceil_div(worker_rows, rows))};
 }
+
+// h is read again by the norm after the next product, when little of it would be left in the caches.
+bool streamed_h(int64_t elements, int32_t type) { return elements > ((int64_t)16 << 20) / (int64_t)type_size(type); }
 
 int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rstd, const void *x, const void *residual, const float *gain,
                      const RmsArgs &a, bool q8, int32_t type, hipStream_t stream)
@@ -202,8 +210,8 @@ WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bo
             best = us;
             s.tile = t.high, s.tiles_i = ti, s.tiles_o = to, s.split_steps = length, s.splits = ceil_div(steps, length);
         }
-    const int64_t want = std::max<int64_t>(1, 1024 / (n * ceil_div(std::max<int64_t>(outs, 1), kRmsThreads)));
-    s.bias_rows = std::max<int64_t>(16, ceil_div(per, want));
+    const int64_t want = std::max<int64_t>(1, 1024 / (n * ceil_div(std::max<int64_t>(outs, 1), kBiasCols)));
+    s.bias_rows = std::max<int64_t>(64, ceil_div(per, want));
     s.bias_chunks = std::max<int64_t>(1, ceil_div(per, s.bias_rows));
     s.a_ld = ceil_div(cols, 8) * 8, s.b_ld = ceil_div(outs, 8) * 8;
     const uint64_t a_bytes = (uint64_t)(rows * s.a_ld) * 2, b_bytes = s.copied ? (uint64_t)(s.planes * rows * s.b_ld) * 2 : 0;
@@ -229,19 +237,30 @@ int weight_check(const char *what, int64_t rows, int64_t cols, int64_t outs, int
     return COMP_AMS_OK;
 }
 
+// Rows in bfloat16 for the product (if there is one), and the sums of dy's columns (if there is a bias).
 void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, const int8_t *q, const float *scale, int64_t rows, int64_t cols,
-                           int64_t outs, int64_t dy_stride, int64_t q_stride, bool binary, int32_t type, hipStream_t stream)
+                           int64_t outs, int64_t dy_stride, int64_t q_stride, int32_t n, bool binary, bool bias, int32_t type, hipStream_t stream)
 {
-    PrepareArgs a = {rows, cols, outs, q_stride, dy_stride, s.a_ld, s.b_ld, rows * s.b_ld, shared_lanes(s.a_ld / 8), shared_lanes(s.b_ld / 8), 0, 0};
-    const int64_t blocks_a = ceil_div(rows, kPrepareThreads / a.lanes_a), blocks_b = s.copied ? ceil_div(rows, kPrepareThreads / a.lanes_b) : 0;
-    a.blocks_a = (unsigned)blocks_a;
+    PrepareArgs a = {};
+    a.rows = rows, a.cols = cols, a.outs = outs, a.q_stride = q_stride, a.dy_stride = dy_stride;
+    a.a_ld = s.a_ld, a.b_ld = s.b_ld, a.b_plane = rows * s.b_ld;
+    a.worker_rows = rows / n, a.bias_rows = s.bias_rows, a.bias_chunks = (unsigned)s.bias_chunks;
+    a.lanes_a = shared_lanes(s.a_ld / 8), a.lanes_b = shared_lanes(s.b_ld / 8);
+    const bool product = rows > 0 && cols > 0;
+    a.blocks_a = product ? (unsigned)ceil_div(rows, kPrepareThreads / a.lanes_a * kPrepareRows) : 0u;
+    a.blocks_b = product && s.copied ? (unsigned)ceil_div(rows, kPrepareThreads / a.lanes_b * kPrepareRows) : 0u;
+    const int64_t blocks = (int64_t)a.blocks_a + a.blocks_b + (bias ? n * s.bias_chunks * ceil_div(outs, kBiasCols) : 0);
     auto go = [&](auto t, auto planes) {
         using T = decltype(t);
-        in_launches(blocks_a + blocks_b, kPrepareThreads, [&](unsigned first, unsigned count) {
-            a.first = first;
-            weight_prepare<T, decltype(planes)::value><<<count, kPrepareThreads, 0, stream>>>(
-                reinterpret_cast<bf16_t *>(work + s.a_at), reinterpret_cast<bf16_t *>(work + s.b_at), static_cast<const T *>(dy), q, scale, a);
-        });
+        auto launch = [&](auto kernel) {
+            in_launches(blocks, kPrepareThreads, [&](unsigned first, unsigned count) {
+                a.first = first;
+                kernel<<<count, kPrepareThreads, 0, stream>>>(reinterpret_cast<bf16_t *>(work + s.a_at), reinterpret_cast<bf16_t *>(work + s.b_at),
+                                                              reinterpret_cast<float *>(work + s.bias_at), static_cast<const T *>(dy), q, scale, a);
+            });
+        };
+        if (bias) launch(weight_prepare<T, decltype(planes)::value, true>);
+        else launch(weight_prepare<T, decltype(planes)::value, false>);
     };
     if (type == COMP_AMS_F32) go(float{}, std::integral_constant<int, 3>{});
     else if (type == COMP_AMS_F16) go(f16_t{}, std::integral_constant<int, 2>{});
@@ -250,13 +269,15 @@ void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, con
 }
 
 template <typename G>
-void weight_launch(G *out, const bf16_t *a_rows, const bf16_t *b_rows, WeightArgs a, int tile, bool in_first, hipStream_t stream)
+void weight_launch(G *out, G *dbias, const bf16_t *a_rows, const bf16_t *b_rows, const float *bias_sums, WeightArgs a, int tile, bool in_first,
+                   hipStream_t stream)
 {
-    const int64_t blocks = (int64_t)a.tiles_i * a.tiles_o * a.n * a.splits;
+    const int64_t tiles = (int64_t)a.tiles_i * a.tiles_o * a.n * a.splits;
+    a.tiles = (unsigned)tiles;
     auto go = [&](auto kernel, int threads) {
-        in_launches(blocks, threads, [&](unsigned first, unsigned count) {
+        in_launches(tiles + (dbias ? a.n * ceil_div(a.outs, threads) : 0), threads, [&](unsigned first, unsigned count) {
             a.first = first;
-            kernel<<<count, threads, 0, stream>>>(out, a_rows, b_rows, a);
+            kernel<<<count, threads, 0, stream>>>(out, dbias, a_rows, b_rows, bias_sums, a);
         });
     };
     if (tile == 256) {
@@ -333,7 +354,7 @@ int comp_ams_rms_norm(void *y, void *h, float *rstd, const void *x, const void *
     REQUIRE_RMS_FORWARD(what);
     REQUIRE_ROWS(what, "y", y, rows, cols, y_stride, type);
     REQUIRE(!h || h != y || rows == 0, "%s: y and h are the same array", what);
-    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, y_stride, eps, (float)(1.0 / (double)cols), false, streamed_out(rows * cols, type)};
+    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, y_stride, eps, (float)(1.0 / (double)cols), false, streamed_out(rows * cols, type), streamed_h(rows * cols, type)};
     return rms_forward_call(what, y, nullptr, h, rstd, x, residual, gain, a, false, type, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -346,7 +367,7 @@ int comp_ams_rms_norm_q8(int8_t *q, float *scale, void *h, float *rstd, const vo
     REQUIRE_BYTE_ROWS(what, "q", q, rows, cols, q_stride);
     REQUIRE(scale || rows == 0, "%s: scale is NULL", what);
     REQUIRE(aligned(scale, 4), "%s: scale must be 4-byte aligned", what);
-    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, q_stride, eps, (float)(1.0 / (double)cols), binary != 0, streamed_out(rows * cols, type)};
+    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, q_stride, eps, (float)(1.0 / (double)cols), binary != 0, false, streamed_h(rows * cols, type)};
     return rms_forward_call(what, q, scale, h, rstd, x, residual, gain, a, true, type, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -541,52 +562,38 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     char *memory = static_cast<char *>(work);
     float *sums = reinterpret_cast<float *>(memory + s.sums_at), *bias_sums = reinterpret_cast<float *>(memory + s.bias_at);
-    const int64_t cells = cols * outs, per = rows / n;
-    if (cells) {
-        if (rows > 0) {
-            weight_prepare_launch(s, memory, dy, q, scale, rows, cols, outs, dy_stride, q_stride, binary != 0, type, stream);
-            if (const int rc = launched(what)) return rc;      // what the product would read has not been written
-        }
-        WeightArgs a = {};
-        a.cols = cols, a.outs = outs, a.a_ld = s.a_ld, a.b_ld = s.copied ? s.b_ld : dy_stride, a.b_plane = rows * s.b_ld;
-        a.worker_rows = per, a.out_stride = in_first ? outs : cols;
-        a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.planes = s.planes;
-        a.splits = (int)s.splits, a.split_steps = (int)s.split_steps;
-        a.stream_out = s.splits == 1 && streamed_out(cells * n, grad_type);
-        const bf16_t *a_rows = reinterpret_cast<const bf16_t *>(memory + s.a_at);
-        const bf16_t *b_rows = s.copied ? reinterpret_cast<const bf16_t *>(memory + s.b_at) : static_cast<const bf16_t *>(dy);
-        if (s.splits > 1) {
-            a.worker_stride = cells, a.piece_stride = cells * n;
-            weight_launch<float>(sums, a_rows, b_rows, a, s.tile, in_first != 0, stream);
-            if (const int rc = launched(what)) return rc;      // what the join would read has not been written
-        } else {
-            a.worker_stride = grad_stride;
-        }
-        with_type(grad_type, [&](auto t) {
-            using G = decltype(t);
-            if (s.splits == 1) {
-                weight_launch<G>(static_cast<G *>(dweight), a_rows, b_rows, a, s.tile, in_first != 0, stream);
-                return;
-            }
-            in_launches(ceil_div(cells, 4 * kWeightJoinThreads), kWeightJoinThreads, [&](unsigned first, unsigned count) {
-                weight_join<G><<<dim3(count, (unsigned)n), kWeightJoinThreads, 0, stream>>>(static_cast<G *>(dweight), sums, cells, (int)s.splits,
-                                                                                          cells * n, grad_stride, first);
-            });
-        });
-        if (const int rc = launched(what)) return rc;
+    const int64_t cells = cols * outs;
+    if (cells == 0 && !dbias) return COMP_AMS_OK;
+    weight_prepare_launch(s, memory, dy, q, scale, rows, cols, outs, dy_stride, q_stride, n, binary != 0, dbias != nullptr, type, stream);
+    if (const int rc = launched(what)) return rc;              // what the product would read has not been written
+    WeightArgs a = {};
+    a.cols = cols, a.outs = outs, a.a_ld = s.a_ld, a.b_ld = s.copied ? s.b_ld : dy_stride, a.b_plane = rows * s.b_ld;
+    a.worker_rows = rows / n, a.out_stride = in_first ? outs : cols;
+    a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.planes = s.planes;
+    a.splits = (int)s.splits, a.split_steps = (int)s.split_steps;
+    a.bias_chunks = (unsigned)s.bias_chunks, a.grad_stride = grad_stride;
+    a.stream_out = s.splits == 1 && streamed_out(cells * n, grad_type);
+    const bf16_t *a_rows = reinterpret_cast<const bf16_t *>(memory + s.a_at);
+    const bf16_t *b_rows = s.copied ? reinterpret_cast<const bf16_t *>(memory + s.b_at) : static_cast<const bf16_t *>(dy);
+    if (s.splits > 1) {
+        a.worker_stride = cells, a.piece_stride = cells * n;
+        weight_launch<float>(sums, nullptr, a_rows, b_rows, nullptr, a, s.tile, in_first != 0, stream);
+        if (const int rc = launched(what)) return rc;          // what the join would read has not been written
+    } else {
+        a.worker_stride = grad_stride;
     }
-    if (!dbias) return COMP_AMS_OK;
-    with_type(type, [&](auto t) {
-        using T = decltype(t);
-        column_sums<T><<<dim3((unsigned)ceil_div(outs, kRmsThreads), (unsigned)s.bias_chunks, (unsigned)n), kRmsThreads, 0, stream>>>(
-            bias_sums, static_cast<const T *>(dy), outs, dy_stride, per, s.bias_rows);
-    });
-    if (const int rc = launched(what)) return rc;
     with_type(grad_type, [&](auto t) {
         using G = decltype(t);
-        in_launches(ceil_div(outs, kColumnsJoin), kRmsThreads, [&](unsigned first, unsigned count) {
-            columns_join<G><<<dim3(count, (unsigned)n), kRmsThreads, 0, stream>>>(static_cast<G *>(dbias), bias_sums, outs, (int)s.bias_chunks, grad_stride,
-                                                                                 first);
+        if (s.splits == 1) {
+            weight_launch<G>(static_cast<G *>(dweight), static_cast<G *>(dbias), a_rows, b_rows, bias_sums, a, s.tile, in_first != 0, stream);
+            return;
+        }
+        const int64_t blocks = ceil_div(cells, 4 * kWeightJoinThreads);
+        a.tiles = (unsigned)blocks;
+        in_launches(blocks + (dbias ? ceil_div(outs, kWeightJoinThreads) : 0), kWeightJoinThreads, [&](unsigned first, unsigned count) {
+            a.first = first;
+            weight_join<G><<<dim3(count, (unsigned)n), kWeightJoinThreads, 0, stream>>>(static_cast<G *>(dweight), static_cast<G *>(dbias), sums, bias_sums,
+                                                                                      cells, (int)s.splits, cells * n, a);
         });
     });
     return launched(what);
