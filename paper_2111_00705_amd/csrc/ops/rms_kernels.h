@@ -14,7 +14,7 @@ namespace cams_ops {
 struct RmsArgs {
     int64_t rows, cols, x_stride, r_stride, h_stride, y_stride;
     float eps, inv_cols;
-    bool binary, stream_out, stream_h;
+    bool binary, stream_in, stream_out, stream_h;      // x and residual, y, h pass the caches by
 };
 
 constexpr int kRmsThreads = 256;
@@ -72,11 +72,11 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void rms_forward(void *y, float 
     v4u xraw[kVecs], rraw[kVecs];
     auto fetch = [&](int64_t at) {
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) xraw[v] = load_slab<T, kTeam>(x + at * a.x_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1);
+        for (int v = 0; v < kVecs; ++v) xraw[v] = load_slab<T, kTeam>(x + at * a.x_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1, a.stream_in);
         if (residual) {
 #pragma unroll
             for (int v = 0; v < kVecs; ++v)
-                rraw[v] = load_slab<T, kTeam>(residual + at * a.r_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1);
+                rraw[v] = load_slab<T, kTeam>(residual + at * a.r_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1, a.stream_in);
         }
     };
     fetch(row);
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void rms_forward(void *y, float 
 struct RmsBackArgs {
     int64_t rows, cols, dx_stride, dy_stride, h_stride, r_stride;
     float inv_cols;
-    bool stream_out;
+    bool stream_in, stream_out;
 };
 
 // The kept row is in the gradients' type, or in 8 bits with a scale.
@@ -218,13 +218,13 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void rms_backward(T *dx, float *
 #pragma unroll
         for (int v = 0; v < kVecs; ++v) {
             if constexpr (k8) h8[v] = load_byte_slab<E, kTeam>(h + at * a.h_stride, v * kTeam * E, me.lane, cols, v < kVecs - 1);
-            else hraw[v] = load_slab<T, kTeam>(h + at * a.h_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1);
-            dyraw[v] = load_slab<T, kTeam>(dy + at * a.dy_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1);
+            else hraw[v] = load_slab<T, kTeam>(h + at * a.h_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1, a.stream_in);
+            dyraw[v] = load_slab<T, kTeam>(dy + at * a.dy_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1, a.stream_in);
         }
         if (dresidual) {
 #pragma unroll
             for (int v = 0; v < kVecs; ++v)
-                rraw[v] = load_slab<T, kTeam>(dresidual + at * a.r_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1);
+                rraw[v] = load_slab<T, kTeam>(dresidual + at * a.r_stride, v * kTeam * E, me.lane, cols, cols, v < kVecs - 1, a.stream_in);
         }
         r = rstd[at];
         if constexpr (k8) hs = h_scale[at];
