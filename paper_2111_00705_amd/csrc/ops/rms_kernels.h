@@ -137,6 +137,9 @@ struct RmsBackArgs {
     int64_t rows, cols, dx_stride, dy_stride, h_stride, r_stride;
     float inv_cols;
     bool stream_in, stream_out;
+    void *dgain;                 // where a worker's rows are one chunk, its sums go there at once, in the gradients' type
+    int64_t grad_stride;
+    int grad_type;               // 0: fp32, 1: bfloat16, 2: half precision
 };
 
 // The kept row is in the gradients' type, or in 8 bits with a scale.
@@ -287,13 +290,24 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void rms_backward(T *dx, float *
             store_slab<T, kTeam>(dx + now * a.dx_stride, v * kTeam * E, me.lane, cols, out[v], v < kVecs - 1, a.stream_out);
     }
     float *to = work + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.cols;
+    const bool only = gridDim.x == 1;
+    auto emit = [&](int c, float sum) {
+        if (!only) {
+            to[c] = sum;
+            return;
+        }
+        const int64_t at = (int64_t)blockIdx.y * a.grad_stride + c;
+        if (a.grad_type == 0) static_cast<float *>(a.dgain)[at] = sum;
+        else if (a.grad_type == 1) static_cast<bf16_t *>(a.dgain)[at] = narrow1<bf16_t>(sum);
+        else static_cast<f16_t *>(a.dgain)[at] = narrow1<f16_t>(sum);
+    };
     if constexpr (kTeams == 1) {
 #pragma unroll
         for (int v = 0; v < kVecs; ++v)
 #pragma unroll
             for (int q = 0; q < E; ++q) {
                 const int c = v * kTeam * E + me.lane * E + q;
-                if (c < cols) to[c] = dg[v][q];
+                if (c < cols) emit(c, dg[v][q]);
             }
     } else {
 #pragma unroll
@@ -305,7 +319,7 @@ __global__ __launch_bounds__(kTeamBlock<kTeam>) void rms_backward(T *dx, float *
             float sum = joined[c];
 #pragma unroll
             for (int t = 1; t < kTeams; ++t) sum += joined[t * kSlots + c];
-            to[c] = sum;
+            emit(c, sum);
         }
     }
 }

@@ -58,7 +58,8 @@ constexpr int64_t kRmsBlocks = 4096;
 // Workgroups that the rows of all workers are cut into in the backward pass, and the fewest rows of one.  More keep more rows in flight, and write
 // more partial sums.  us with the join, at 512 / 750 / 1024 / 2048: 16384 x 768 bf16, n = 8 22.4 / 23.8 / 21.6 / 24.8; 20000 x 2047 fp32 kept in 8 bits,
 // n = 20 134 / 129 / 117 / 118; 8192 x 4096 bf16, n = 4 67.8 / 66.1 / 67.2 / 73.9.  1024 x 4096 bf16, n = 8 at 4 / 2 / 1 rows 15.6 / 16.5 / 23.2.
-constexpr int64_t kRmsChunkBlocks = 1024, kRmsChunkRows = 4;
+// Up to kRmsOnlyRows of a worker are one chunk, which needs no join and no launch for it.
+constexpr int64_t kRmsChunkBlocks = 1024, kRmsChunkRows = 4, kRmsOnlyRows = 16;
 
 // How a worker's rows are cut for the gain's gradients: chunks of rows with one set of column sums each.
 struct RmsChunks {
@@ -66,6 +67,7 @@ struct RmsChunks {
 };
 RmsChunks rms_chunks(int64_t worker_rows, int32_t n)
 {
+    if (worker_rows <= kRmsOnlyRows) return {kRmsOnlyRows, 1};
     const int64_t want = std::max<int64_t>(1, ceil_div(kRmsChunkBlocks, n));
     const int64_t rows = std::max<int64_t>(kRmsChunkRows, ceil_div(worker_rows, want));
     return {rows, std::max<int64_t>(1, ceil_div(worker_rows, rows))};
@@ -408,16 +410,18 @@ int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void
     REQUIRE(work && work_bytes >= need, "%s: needs %llu bytes of work memory", what, (unsigned long long)need);
     REQUIRE(aligned(work, 16), "%s: work must be 16-byte aligned", what);
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const RmsBackArgs a = {rows, cols, dx_stride, dy_stride, h_stride, dresidual_stride, (float)(1.0 / (double)cols), streamed_rows(rows * cols, type), streamed_out(rows * cols, type)};
+    const RmsBackArgs a = {rows, cols, dx_stride, dy_stride, h_stride, dresidual_stride, (float)(1.0 / (double)cols), streamed_rows(rows * cols, type), streamed_out(rows * cols, type),
+                           dgain, grad_stride, grad_type};
     const RmsChunks ch = rms_chunks(rows / n, n);
     float *sums = static_cast<float *>(work);
+    bool held = false;
     with_type(type, [&](auto t) {
         using T = decltype(t);
         auto call = [&](auto kept) {
             using H = decltype(kept);
             const T *dyt = static_cast<const T *>(dy), *rt = static_cast<const T *>(dresidual);
             const H *ht = static_cast<const H *>(h);
-            const bool held = with_team<T>(cols, [&](auto shape) {
+            held = with_team<T>(cols, [&](auto shape) {
                 using S = decltype(shape);
                 rms_backward<T, H, S::threads, S::vecs><<<dim3((unsigned)ch.count, (unsigned)n), kTeamBlock<S::threads>, 0, stream>>>(
                     static_cast<T *>(dx), sums, dyt, ht, h_scale, rstd, gain, rt, a, rows / n, ch.rows);
@@ -434,6 +438,7 @@ int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void
         else call(T{});
     });
     if (const int rc = launched(what)) return rc;              // what the join would read has not been written
+    if (held && ch.count == 1) return COMP_AMS_OK;
     with_type(grad_type, [&](auto t) {
         using G = decltype(t);
         in_launches(ceil_div(cols, kColumnsJoin), kRmsThreads, [&](unsigned first, unsigned count) {

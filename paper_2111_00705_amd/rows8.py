@@ -231,7 +231,11 @@ def rms_norm_backward(dy, h, rstd, gain, dgain, dresidual=None, scale=None, out=
         r_stride = _columns(dresidual, "dresidual")[1]
     rows = _scales(rstd, lead, "rstd")
     _parameter(gain, cols, "gain")
-    stride, n = _param_grad(dgain, (cols,), "dgain"), dgain.shape[0]
+    g_shape, g_strides = dgain.shape, dgain.stride()
+    if len(g_shape) != 2 or g_shape[1] != cols or cols > 1 and g_strides[1] != 1:
+        raise ValueError(f"dgain must be [n, {cols}], dense within a worker's row")
+    n = g_shape[0]
+    stride = g_strides[0] if n > 1 else cols
     s = _stream(dy, h, scale, rstd, gain, dgain, dresidual, out)
     if out is None:
         dx, dx_stride = _new(dy), cols
