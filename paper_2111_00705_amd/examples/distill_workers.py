@@ -6,7 +6,10 @@ grads[n, d], which CompAms.step compresses and averages: norm gains and shifts, 
 operators, matrix parameters by batched products over the workers.  The teacher (random weights) is asked once per batch for its
 best tokens, as a recorded teacher would be.
 
-    python -m paper_2111_00705_amd.examples.distill_workers [--iterations 60] [--workers 8]
+With --eight-bits the student runs and keeps its activations in 8 bits: root-mean-square norms whose results leave in 8 bits, products of 8-bit
+integers, and weight gradients formed from the 8-bit rows that the products read.  Gradients go straight through the roundings.
+
+    python -m paper_2111_00705_amd.examples.distill_workers [--iterations 60] [--workers 8] [--eight-bits]
 """
 from __future__ import annotations
 
@@ -84,7 +87,53 @@ def distill_iteration(P, lay, theta, grads, tokens, lengths, idx, val, bounds):
     return loss.view(n, -1).mean(1)
 
 
-def run(iterations=60, n=8, batch=4, seed=0, report=None):
+def distill_iteration_eight_bits(P, lay, theta, grads, tokens, lengths, idx, val, bounds):
+    """The same for a student with root-mean-square norms (b1 and b2 are not used) whose products take 8 bits.  What is kept for the backward
+    pass of a product is the 8-bit rows that it read."""
+    import torch
+    n, batch, length = tokens.shape
+    rows, dim = n * batch * length, WIDTH // HEADS
+    p = {name: lay.view(theta, name) for name in lay.shape}
+    g = {name: lay.view(grads, name) for name in lay.shape}
+    f32 = theta.dtype
+    weights = {name: P.quantize_rows(p[name].t().contiguous()) for name in ("qkv", "out", "head")}        # [outs, cols], a scale for each channel
+
+    def product(kept, name):
+        return P.linear_q8(*kept, *weights[name], dtype=f32)
+
+    def product_backward(dy, kept, name):
+        P.linear_weight_grad(dy, *kept, g[name].transpose(1, 2), binary=True)
+        return dy @ P.restore_rows(*weights[name], f32)
+
+    x0 = p["embed"][tokens.view(-1)]                                                   # [rows, WIDTH]
+    *kept1, _, rstd1 = P.rms_norm_q8(x0, p["g1"], binary=True)
+    qkv = product(kept1, "qkv").view(n * batch, length, 3, HEADS, dim).permute(2, 0, 3, 1, 4).contiguous()
+    q, k, v = qkv[0], qkv[1], qkv[2]
+    probs = P.rel_bias_softmax(torch.matmul(q, k.transpose(-1, -2).contiguous()), p["bias"], bounds, scale=dim ** -0.5, causal=True, key_lengths=lengths)
+    mixed = P.quantize_rows(torch.matmul(probs, v).transpose(1, 2).reshape(rows, WIDTH), binary=True)
+    *kept2, x1, rstd2 = P.rms_norm_q8(product(mixed, "out"), p["g2"], x0, binary=True)
+    logits = product(kept2, "head")
+
+    weight = torch.full((rows,), 1.0 / (batch * length), device=theta.device)           # each worker's loss is its mean
+    loss, dlogits = P.distill_grad(logits, idx, val, weight, temperature=TEMPERATURE, out=logits)
+
+    dx1 = P.rms_norm_backward(product_backward(dlogits, kept2, "head"), x1, rstd2, p["g2"], g["g2"])
+    dmixed = product_backward(dx1, mixed, "out").view(n * batch, length, HEADS, dim).transpose(1, 2).contiguous()
+    dprobs = torch.matmul(dmixed, v.transpose(-1, -2).contiguous())
+    dv = torch.matmul(probs.transpose(-1, -2).contiguous(), dmixed)
+    dscores = P.rel_bias_softmax_backward(dprobs, probs, bounds, g["bias"], scale=dim ** -0.5, causal=True, key_lengths=lengths, out=dprobs)
+    dq, dk = torch.matmul(dscores, k), torch.matmul(dscores.transpose(-1, -2).contiguous(), q)
+    dqkv = torch.stack([dq, dk, dv]).permute(1, 3, 0, 2, 4).reshape(rows, 3 * WIDTH)
+    dx0 = P.rms_norm_backward(product_backward(dqkv, kept1, "qkv"), x0, rstd1, p["g1"], g["g1"], dresidual=dx1)
+    g["b1"].zero_()
+    g["b2"].zero_()
+    g["embed"].zero_()
+    for w in range(n):
+        g["embed"][w].index_add_(0, tokens[w].view(-1), dx0.view(n, batch * length, -1)[w])
+    return loss.view(n, -1).mean(1)
+
+
+def run(iterations=60, n=8, batch=4, seed=0, report=None, eight_bits=False):
     """Distils; returns (mean loss before each iteration, bits per step and worker, the same without compression)."""
     import torch
 
@@ -105,8 +154,9 @@ def run(iterations=60, n=8, batch=4, seed=0, report=None):
     h = P.CompAms(lay.d, n, P.TOPK, lay.d // 50, 0.9, 0.999, 1e-8, 3e-3)
     h.set_theta(theta)
     losses = []
+    iteration = distill_iteration_eight_bits if eight_bits else distill_iteration
     for t in range(iterations):
-        loss = distill_iteration(P, lay, theta, grads, tokens, lengths, idx, val, bounds)
+        loss = iteration(P, lay, theta, grads, tokens, lengths, idx, val, bounds)
         losses.append(float(loss.mean()))
         if report and t % 10 == 0:
             report(f"{t:9d} {losses[-1]:12.4f}")
@@ -121,11 +171,12 @@ def main() -> int:
     ap = argparse.ArgumentParser()
     ap.add_argument("--iterations", type=int, default=60)
     ap.add_argument("--workers", type=int, default=8)
+    ap.add_argument("--eight-bits", action="store_true")
     args = ap.parse_args()
     import torch
     assert torch.cuda.is_available(), "this example needs a GPU"
     print(f"{args.workers} workers, vocabulary {VOCAB}, the teacher's {TOP} best tokens\niteration    mean loss")
-    losses, bits, dense = run(args.iterations, args.workers, report=print)
+    losses, bits, dense = run(args.iterations, args.workers, report=print, eight_bits=args.eight_bits)
     print(f"{args.iterations:9d} {losses[-1]:12.4f}   bits per step and worker (up + down) {bits}, uncompressed {dense}")
     return 0
 

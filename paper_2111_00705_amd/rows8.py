@@ -312,10 +312,8 @@ def linear_weight_grad(dy, q, scale, dweight, dbias=None, binary=False, *, strea
             _need(strides[2] == outs, "dweight must be dense within a worker's row")
         else:
             _need(strides[1] == cols or outs == 1, "dweight must be dense within a worker's row")
-    elif n > 1:
-        stride = max(stride, outs)                   # nothing of it is written
-    else:
-        stride = outs
+    else:                                            # nothing of it is written
+        stride = outs if dbias is None or n <= 1 or dbias.dim() != 2 else dbias.stride(0)
     if dbias is not None:
         _need(dbias.dtype is dweight.dtype and tuple(dbias.shape) == (n, outs) and (_param_grad(dbias, (outs,), "dbias") == stride or n == 1),
               "dbias must be [n, outs] with the type and worker stride of dweight")

@@ -240,7 +240,9 @@ def test_linear_q8(rows, cols, outs):
             assert R.same_bits(P.linear_q8(q.cuda(), sc, w.cuda(), ws.cuda(), bc, dtype=dtype), first)
 
 
-@pytest.mark.parametrize("rows,cols,outs", [(3600, 80, 3700), (3585, 77, 3599), (4000, 400, 3400)])
+# the tiles of 256 x 256, 256 x 128, 128 x 128 and 64 x 128, and k in pieces, each over sizes that end inside a tile
+@pytest.mark.parametrize("rows,cols,outs", [(3600, 80, 3700), (3585, 77, 3599), (4000, 400, 3400), (2000, 208, 4100), (2040, 131, 4001), (1000, 200, 4090), (500, 333, 4000),
+                                            (100, 8200, 1000), (70, 16_400, 130), (40, 20_000, 65)])
 def test_linear_q8_large_tiles(rows, cols, outs):
     print(f"[case] product {rows}x{cols}x{outs}", flush=True)
     g = gen("large", rows, cols, outs)
@@ -326,7 +328,8 @@ def test_linear_weight_grad(n, per, cols, outs, dtype, binary):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("n,per,cols,outs", [(8, 64, 1300, 1290), (1, 96, 3600, 3700), (4, 70, 2047, 1801)])
+@pytest.mark.parametrize("n,per,cols,outs", [(8, 64, 1300, 1290), (1, 96, 3600, 3700), (4, 70, 2047, 1801), (1, 500, 2040, 2000), (1, 9000, 1000, 1030),
+                                                   (2, 5000, 300, 200), (3, 2000, 70, 520)])
 def test_linear_weight_grad_large_tiles(n, per, cols, outs, dtype):
     print(f"[case] weights {n}x{per} {cols}->{outs} {dtype}", flush=True)
     g = gen("weights large", n, per, cols, outs)
@@ -347,6 +350,8 @@ def test_linear_weight_grad_of_nothing():
     P.linear_weight_grad(z(0, 4), z(0, 3, t=torch.int8), z(0), grads[:, :12].unflatten(1, (4, 3)), grads[:, 12:])
     assert (grads == 0).all()
     P.linear_weight_grad(z(6, 4), z(6, 0, t=torch.int8), z(6), dw[:, :, :0])
+    P.linear_weight_grad(z(6, 4) + 2, z(6, 0, t=torch.int8), z(6), grads[:, :0].unflatten(1, (4, 0)), grads[:, 5:9])       # no weight, a bias all the same
+    assert (grads[:, 5:9] == 6).all() and (grads[:, :5] == 0).all() and (grads[:, 9:] == 0).all()
     P.linear_weight_grad(z(6, 0), z(6, 3, t=torch.int8), z(6), dw[:, :0])
     assert (dw == 5).all()
 
