@@ -117,21 +117,42 @@ int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rs
 // --- the product -----------------------------------------------------------------------------------------------------
 
 // What a tile costs, for the choice among them: us of a step of `alone` for the first workgroup of a compute unit and of `more` for each
-// that it takes besides.  Fitted to kernels timed over 17 (products) and 15 (weight gradients) sizes from 16 x 4096 x 4096 to 4096 x 4096 x 4096; what is chosen
-// was within 8 % of the best there, where one tile for all would be up to 4 times off.
+// that it takes besides, kTileStart steps for its start and end.  Fitted to kernels timed over 25 (products; their weights from memory, as a model's layers in turn find
+// them) and 15 (weight gradients) sizes from 16 x 4096 x 4096 to 4096 x 4096 x 4096.  There the choice was within 15 % of the best, where one
+// tile for all would be up to 4 times off.
 struct TileCost {
     int high, wide;
     double alone, more;
     bool splits;             // whether the sum may be cut into pieces
 };
-double tile_cost(const TileCost &t, int64_t tiles, int64_t pieces, int64_t steps, double cells)
+constexpr int64_t kTileStart = 6, kLeastPiece = 16;
+// tiles of `pieces` pieces of `steps` steps; cells: of the result; bytes: of the operands.  Pieces have to gain a sixth: they cost another launch.
+double tile_cost(const TileCost &t, int64_t tiles, int64_t pieces, int64_t steps, double cells, double bytes)
 {
     const double deep = (double)ceil_div(std::max<int64_t>(tiles * pieces, 1), 256);
-    const double join = pieces > 1 ? 4.5 + (double)(pieces + 1) * cells * 4.0 / 3e6 : 0.0;      // a launch, and the pieces' sums back from memory
-    return (t.alone + (deep - 1) * t.more) * (double)steps + join;
+    const double us = std::max((t.alone + (deep - 1) * t.more) * (double)(steps + kTileStart), bytes / 5e6);
+    return pieces > 1 ? 1.15 * (us + 4.5 + (double)(pieces + 1) * cells * 4.0 / 3e6) : us;
 }
-constexpr TileCost kProductTiles[] = {{256, 256, 1.05, 1.05, false}, {256, 128, 0.62, 0.62, false}, {128, 128, 0.40, 0.33, false},
-                                      {64, 128, 0.23, 0.22, false}, {64, 64, 0.155, 0.138, true}};
+// The least of them: f(tile, pieces, steps of a piece) for each that is cheaper than those before.
+template <int kTiles, typename F>
+void choose_tile(const TileCost (&costs)[kTiles], int64_t steps, double cells, double bytes, int64_t high, int64_t wide, int64_t sets, F &&f)
+{
+    double best = -1;
+    for (const TileCost &t : costs)
+        for (int64_t pieces = 1; pieces <= (t.splits ? 16 : 1); pieces *= 2) {
+            const int64_t length = ceil_div(steps, pieces);
+            if (pieces > 1 && length < kLeastPiece) break;
+            const double us = tile_cost(t, ceil_div(high, t.high) * ceil_div(wide, t.wide) * sets, ceil_div(steps, length), length, cells, bytes);
+            if (best >= 0 && us >= best) continue;
+            best = us;
+            f(t, ceil_div(steps, length), length);
+        }
+}
+constexpr TileCost kProductTiles[] = {{256, 256, 1.05, 1.05, false}, {256, 128, 0.65, 0.63, false}, {128, 128, 0.42, 0.32, true},
+                                      {64, 128, 0.37, 0.20, false}, {64, 64, 0.33, 0.12, true}};
+// Tokens up to which a product goes to product8_few, and with up to how many weights twice as many do: 32 x 4096 x 4096 9.4 us against 12.0 by tiles,
+// 32 x 8192 x 8192 28.9 against 20.3.
+constexpr int64_t kFewRows = 16, kFewWeights = (int64_t)1 << 25;
 
 // Which kernel takes a product, into how many pieces k is cut, and where the work memory holds what.
 struct ProductShape {
@@ -145,23 +166,16 @@ ProductShape product_shape(int64_t rows, int64_t cols, int64_t outs, bool x_alig
 {
     ProductShape s = {};
     s.splits = 1;
-    if (rows <= 32) {
-        s.few = rows <= 16 ? 1 : 2;
+    if (rows <= kFewRows || (rows <= 2 * kFewRows && outs * cols <= kFewWeights)) {
+        s.few = rows <= kFewRows ? 1 : 2;
         s.tiles_m = 1, s.tiles_n = ceil_div(outs, 16);
         return s;
     }
-    const int64_t steps = ceil_div(std::max<int64_t>(cols, 1), kProductStep);
-    double best = 0;
-    for (const TileCost &t : kProductTiles)
-        for (int64_t pieces = 1; pieces <= (t.splits ? 16 : 1); pieces *= 2) {
-            const int64_t length = ceil_div(steps, pieces), tm = ceil_div(rows, t.high), tn = ceil_div(outs, t.wide);
-            if (pieces > 1 && length < 8) break;
-            const double us = tile_cost(t, tm * tn, ceil_div(steps, length), length, (double)rows * (double)outs);
-            if (best && us >= best) continue;
-            best = us;
-            s.high = t.high, s.wide = t.wide, s.tiles_m = tm, s.tiles_n = tn;
-            s.k_split = (int)(length * kProductStep), s.splits = (int)ceil_div(steps, length);
-        }
+    choose_tile(kProductTiles, ceil_div(std::max<int64_t>(cols, 1), kProductStep), (double)rows * (double)outs, (double)cols * (double)(rows + outs), rows, outs, 1,
+                [&](const TileCost &t, int64_t pieces, int64_t length) {
+                    s.high = t.high, s.wide = t.wide, s.tiles_m = ceil_div(rows, t.high), s.tiles_n = ceil_div(outs, t.wide);
+                    s.k_split = (int)(length * kProductStep), s.splits = (int)pieces;
+                });
     s.ld = ceil_div(cols, 16) * 16;
     if (cols % 16) x_aligned = w_aligned = false;
     s.x_at = 0;
@@ -205,16 +219,10 @@ WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bo
     s.planes = type == COMP_AMS_F32 ? 3 : type == COMP_AMS_BF16 && binary ? 1 : 2;
     s.copied = s.planes > 1 || !dy_aligned || outs % 8 != 0;
     const int64_t steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.planes);
-    double best = 0;
-    for (const TileCost &t : kWeightTiles)
-        for (int64_t pieces = 1; pieces <= (t.splits ? 16 : 1); pieces *= 2) {
-            const int64_t length = ceil_div(steps, pieces), ti = ceil_div(cols, t.high), to = ceil_div(outs, t.wide);
-            if (pieces > 1 && length < 8) break;
-            const double us = tile_cost(t, ti * to * n, ceil_div(steps, length), length, (double)cols * (double)outs * n);
-            if (best && us >= best) continue;
-            best = us;
-            s.tile = t.high, s.tiles_i = ti, s.tiles_o = to, s.split_steps = length, s.splits = ceil_div(steps, length);
-        }
+    choose_tile(kWeightTiles, steps, (double)cols * (double)outs * n, 0.0, cols, outs, n, [&](const TileCost &t, int64_t pieces, int64_t length) {
+        s.tile = t.high, s.tiles_i = ceil_div(cols, t.high), s.tiles_o = ceil_div(outs, t.wide);
+        s.split_steps = length, s.splits = pieces;
+    });
     const int64_t want = std::max<int64_t>(1, 1024 / (n * ceil_div(std::max<int64_t>(outs, 1), kBiasCols)));
     s.bias_rows = std::max<int64_t>(64, ceil_div(per, want));
     s.bias_chunks = std::max<int64_t>(1, ceil_div(per, s.bias_rows));
@@ -517,7 +525,8 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
             });
         };
         if (s.splits > 1) {
-            go(product8<Y, 64, 64, 2, 2, true>, 256);
+            if (s.high == 128) go(product8<Y, 128, 128, 2, 2, true>, 256);
+            else go(product8<Y, 64, 64, 2, 2, true>, 256);
             rc = launched(what);                               // unless it is good, what the join would read has not been written
             if (rc) return;
             in_launches(ceil_div(ceil_div(outs, 4) * rows, kProductThreads), kProductThreads, [&](unsigned first, unsigned count) {
