@@ -89,7 +89,7 @@ int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, int3
  * half precision with scales that are powers of two).  binary != 0 promises that all scales are powers of two, as binary quantising
  * gives them; dy in bfloat16 then takes one product in place of two, and where the promise does not hold q scale is rounded to bfloat16.
  * An infinity or a NaN in dy or a scale reaches the worker's gradients that it belongs to, as an infinity or a NaN.
- * rows >= 0 a multiple of n and below 2^35, a worker's below 2^29; 0 <= cols, outs <= 2^23.  With rows = 0 the gradients are zero.
+ * rows >= 0 a multiple of n and below 2^32, a worker's below 2^29; 0 <= cols, outs <= 2^23.  With rows = 0 the gradients are zero.
  * work: comp_ams_linear_weight_grad_work_bytes() bytes, 16-byte aligned, not kept from one call to the next: q in bfloat16, and dy too
  * unless it is bfloat16 with binary != 0, outs is a multiple of 8 and, as dy_aligned != 0 promises, dy and its stride are multiples of 16 bytes.
  */

@@ -175,9 +175,9 @@ __global__ __launch_bounds__(kRmsThreads) void rms_backward_any(T *dx, const T *
 template <typename T, typename H>
 __global__ __launch_bounds__(kRmsThreads) void rms_param_any(float *__restrict__ work, const T *__restrict__ dy, const H *__restrict__ h,
                                                              const float *__restrict__ h_scale, const float *__restrict__ rstd,
-                                                             RmsBackArgs a, int64_t worker_rows, int64_t chunk_rows)
+                                                             RmsBackArgs a, int64_t worker_rows, int64_t chunk_rows, unsigned first)
 {
-    const int64_t c = (int64_t)blockIdx.x * kRmsThreads + threadIdx.x;
+    const int64_t c = (int64_t)(first + blockIdx.x) * kRmsThreads + threadIdx.x;
     const int64_t lo = (int64_t)blockIdx.y * chunk_rows, hi = min(lo + chunk_rows, worker_rows);
     if (c >= a.cols) return;
     float dg = 0.f;

@@ -241,7 +241,7 @@ int weight_check(const char *what, int64_t rows, int64_t cols, int64_t outs, int
 {
     REQUIRE(known_type(type), "%s: unknown type %d", what, type);
     REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
-    REQUIRE(rows >= 0 && rows < (int64_t)1 << 35 && rows / n < kLimit31 / 4, "%s: rows=%lld are too many", what, (long long)rows);
+    REQUIRE(rows >= 0 && rows < (int64_t)1 << 32 && rows / n < kLimit31 / 4, "%s: rows=%lld are too many", what, (long long)rows);
     REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
     REQUIRE(cols >= 0 && cols <= kMostChannels && outs >= 0 && outs <= kMostChannels, "%s: cols=%lld or outs=%lld is out of range", what,
             (long long)cols, (long long)outs);
@@ -436,8 +436,11 @@ int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void
             });
             if (held) return;
             // the gain's gradients first: dx may replace dy or h
-            rms_param_any<T, H><<<dim3((unsigned)ceil_div(cols, kRmsThreads), (unsigned)ch.count, (unsigned)n), kRmsThreads, 0, stream>>>(
-                sums, dyt, ht, h_scale, rstd, a, rows / n, ch.rows);
+            // every launch of fewer than 2^32 threads
+            in_launches(ceil_div(cols, kRmsThreads), kRmsThreads * (int)ch.count * n, [&](unsigned first, unsigned count) {
+                rms_param_any<T, H><<<dim3(count, (unsigned)ch.count, (unsigned)n), kRmsThreads, 0, stream>>>(sums, dyt, ht, h_scale, rstd, a, rows / n, ch.rows,
+                                                                                                             first);
+            });
             if (rows > 0)
                 rms_backward_any<T, H><<<(unsigned)std::min(rows, most_blocks(kRmsThreads)), kRmsThreads, 0, stream>>>(static_cast<T *>(dx), dyt, ht,
                                                                                                                       h_scale, rstd, gain, rt, a);
@@ -449,7 +452,7 @@ int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void
     if (held && ch.count == 1) return COMP_AMS_OK;
     with_type(grad_type, [&](auto t) {
         using G = decltype(t);
-        in_launches(ceil_div(cols, kColumnsJoin), kRmsThreads, [&](unsigned first, unsigned count) {
+        in_launches(ceil_div(cols, kColumnsJoin), kRmsThreads * n, [&](unsigned first, unsigned count) {
             columns_join<G><<<dim3(count, (unsigned)n), kRmsThreads, 0, stream>>>(static_cast<G *>(dgain), sums, cols, (int)ch.count, grad_stride, first);
         });
     });
