@@ -24,12 +24,40 @@ namespace {
 constexpr int64_t kLimit31 = (int64_t)1 << 31;
 constexpr int64_t kMostStride = kLimit31 / 512;      // bytes between rows, of which a tile has 256
 
+// Whether a product's result is stored past the caches: only rows that begin at multiples of 128 bytes.  Lines that two tiles share have to meet in a
+// cache: weight gradients of 4 workers' 128 rows, 4096 x 4096, past the caches / through them, at such rows 47 / 51 us, 20 bytes further 86 / 53.
+bool streamed_result(const void *p, int64_t elements, int64_t row_stride, int64_t set_stride, int32_t type)
+{
+    const int64_t size = (int64_t)type_size(type);
+    return streamed_out(elements, type) && aligned(p, 128) && row_stride * size % 128 == 0 && set_stride * size % 128 == 0;
+}
+
 // Lanes of a workgroup of 256 that share a row of `chunks`, when it is written anew.
 int shared_lanes(int64_t chunks)
 {
     int lanes = 8;
     while (lanes < 256 && lanes < chunks) lanes *= 2;
     return lanes;
+}
+
+// f(Shape) as with_team, and rows of up to `most` vectors by a workgroup of 1024, three or four vectors a lane.  us of the forms that read a row several
+// times / of these, 5000 x 12000 fp32: norm 393 / 167, in 8 bits 456 / 164, its backward pass 425 / 191, a checkpoint written and read 249 / 95.
+template <typename T, int kMost, typename F>
+bool with_rows(int64_t len, F &&f)
+{
+    if (with_team<T>(len, f)) return true;
+    const int64_t vecs = ceil_div(len, kVec<T>);
+    if constexpr (kMost > 2048) {
+        if (vecs > 2048 && vecs <= 3072) {
+            f(Shape<1024, 3>{});
+            return true;
+        }
+        if (vecs > 3072 && vecs <= 4096) {
+            f(Shape<1024, 4>{});
+            return true;
+        }
+    }
+    return false;
 }
 
 int rows8_check(const char *what, int64_t rows, int64_t cols, const float *scale, int32_t type)
@@ -87,7 +115,7 @@ int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rs
         using T = decltype(t);
         auto call = [&](auto eight) {
             constexpr bool k8 = decltype(eight)::value;
-            const bool held = with_team<T>(a.cols, [&](auto shape) {
+            const bool held = with_rows<T, 4096>(a.cols, [&](auto shape) {
                 using S = decltype(shape);
                 const int64_t teams = kTeamBlock<S::threads> / S::threads;
                 rms_forward<T, S::threads, S::vecs, k8><<<(unsigned)std::min<int64_t>(ceil_div(a.rows, teams), kRmsBlocks), kTeamBlock<S::threads>, 0, stream>>>(
@@ -117,20 +145,21 @@ int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rs
 // --- the product -----------------------------------------------------------------------------------------------------
 
 // What a tile costs, for the choice among them: us of a step of `alone` for the first workgroup of a compute unit and of `more` for each
-// that it takes besides, kTileStart steps for its start and end.  Fitted to kernels timed over 25 (products; their weights from memory, as a model's layers in turn find
+// that it takes besides, and `start` steps for its start and end (results of large tiles leave while nothing else runs on the unit).  Fitted to kernels timed over 25 (products; their weights from memory, as a model's layers in turn find
 // them) and 15 (weight gradients) sizes from 16 x 4096 x 4096 to 4096 x 4096 x 4096.  There the choice was within 15 % of the best, where one
 // tile for all would be up to 4 times off.
 struct TileCost {
     int high, wide;
     double alone, more;
+    int start;
     bool splits;             // whether the sum may be cut into pieces
 };
-constexpr int64_t kTileStart = 6, kLeastPiece = 16;
+constexpr int64_t kLeastPiece = 16;
 // tiles of `pieces` pieces of `steps` steps; cells: of the result; bytes: of the operands.  Pieces have to gain a sixth: they cost another launch.
 double tile_cost(const TileCost &t, int64_t tiles, int64_t pieces, int64_t steps, double cells, double bytes)
 {
     const double deep = (double)ceil_div(std::max<int64_t>(tiles * pieces, 1), 256);
-    const double us = std::max((t.alone + (deep - 1) * t.more) * (double)(steps + kTileStart), bytes / 5e6);
+    const double us = std::max((t.alone + (deep - 1) * t.more) * (double)(steps + t.start), bytes / 5e6);
     return pieces > 1 ? 1.15 * (us + 4.5 + (double)(pieces + 1) * cells * 4.0 / 3e6) : us;
 }
 // The least of them: f(tile, pieces, steps of a piece) for each that is cheaper than those before.
@@ -148,8 +177,8 @@ void choose_tile(const TileCost (&costs)[kTiles], int64_t steps, double cells, d
             f(t, ceil_div(steps, length), length);
         }
 }
-constexpr TileCost kProductTiles[] = {{256, 256, 1.05, 1.05, false}, {256, 128, 0.65, 0.63, false}, {128, 128, 0.42, 0.32, true},
-                                      {64, 128, 0.37, 0.20, false}, {64, 64, 0.33, 0.12, true}};
+constexpr TileCost kProductTiles[] = {{256, 256, 1.05, 1.05, 8, false}, {256, 128, 0.65, 0.63, 7, false}, {128, 128, 0.42, 0.32, 6, true},
+                                      {64, 128, 0.37, 0.20, 6, false}, {64, 64, 0.33, 0.12, 6, true}};
 // Tokens up to which a product goes to product8_few, and with up to how many weights twice as many do: 32 x 4096 x 4096 9.4 us against 12.0 by tiles,
 // 32 x 8192 x 8192 28.9 against 20.3.
 constexpr int64_t kFewRows = 16, kFewWeights = (int64_t)1 << 25;
@@ -199,7 +228,7 @@ int product_check(const char *what, int64_t rows, int64_t cols, int64_t outs)
 
 constexpr int64_t kMostChannels = (int64_t)1 << 23;      // a step's rows lie within 31 bits
 
-constexpr TileCost kWeightTiles[] = {{256, 256, 0.83, 0.83, false}, {128, 128, 0.32, 0.24, true}, {64, 64, 0.16, 0.11, true}};
+constexpr TileCost kWeightTiles[] = {{256, 256, 0.83, 0.83, 16, false}, {128, 128, 0.32, 0.24, 6, true}, {64, 64, 0.16, 0.11, 6, true}};
 
 // How a call is cut, and where its work memory holds what.
 struct WeightShape {
@@ -321,7 +350,7 @@ int comp_ams_quantize_rows(int8_t *q, float *scale, const void *x, int64_t rows,
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        const bool held = with_team<T>(cols, [&](auto shape) {
+        const bool held = with_rows<T, 4096>(cols, [&](auto shape) {
             using S = decltype(shape);
             in_launches(ceil_div(rows, kTeamBlock<S::threads> / S::threads), kTeamBlock<S::threads>, [&](unsigned first, unsigned count) {
                 a.first = first;
@@ -346,7 +375,7 @@ int comp_ams_restore_rows(void *x, const int8_t *q, const float *scale, int64_t 
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        const bool held = with_team<T>(cols, [&](auto shape) {
+        const bool held = with_rows<T, 4096>(cols, [&](auto shape) {
             using S = decltype(shape);
             in_launches(ceil_div(rows, kTeamBlock<S::threads> / S::threads), kTeamBlock<S::threads>, [&](unsigned first, unsigned count) {
                 a.first = first;
@@ -429,7 +458,7 @@ int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void
             using H = decltype(kept);
             const T *dyt = static_cast<const T *>(dy), *rt = static_cast<const T *>(dresidual);
             const H *ht = static_cast<const H *>(h);
-            held = with_team<T>(cols, [&](auto shape) {
+            held = with_rows<T, sizeof(T) == 4 ? 4096 : 2048>(cols, [&](auto shape) {
                 using S = decltype(shape);
                 rms_backward<T, H, S::threads, S::vecs><<<dim3((unsigned)ch.count, (unsigned)n), kTeamBlock<S::threads>, 0, stream>>>(
                     static_cast<T *>(dx), sums, dyt, ht, h_scale, rstd, gain, rt, a, rows / n, ch.rows);
@@ -488,7 +517,7 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
             (unsigned long long)s.bytes);
     if (rows == 0 || outs == 0) return COMP_AMS_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    ProductArgs a = {rows, outs, q_stride, w_stride, y_stride, (int)cols, (int)s.tiles_m, (int)s.tiles_n, s.splits, s.k_split, 0, streamed_out(rows * outs, type)};
+    ProductArgs a = {rows, outs, q_stride, w_stride, y_stride, (int)cols, (int)s.tiles_m, (int)s.tiles_n, s.splits, s.k_split, 0, streamed_result(y, rows * outs, y_stride, 0, type)};
     const int64_t blocks = s.tiles_m * s.tiles_n * s.splits;
     int8_t *memory = static_cast<int8_t *>(work);
     if (!s.few && cols && !(q_aligned && w_aligned)) {
@@ -592,7 +621,7 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
     a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.planes = s.planes;
     a.splits = (int)s.splits, a.split_steps = (int)s.split_steps;
     a.bias_chunks = (unsigned)s.bias_chunks, a.grad_stride = grad_stride;
-    a.stream_out = s.splits == 1 && streamed_out(cells * n, grad_type);
+    a.stream_out = s.splits == 1 && streamed_result(dweight, cells * n, a.out_stride, n > 1 ? grad_stride : 0, grad_type);
     const bf16_t *a_rows = reinterpret_cast<const bf16_t *>(memory + s.a_at);
     const bf16_t *b_rows = s.copied ? reinterpret_cast<const bf16_t *>(memory + s.b_at) : static_cast<const bf16_t *>(dy);
     if (s.splits > 1) {
