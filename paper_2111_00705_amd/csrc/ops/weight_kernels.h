@@ -206,9 +206,10 @@ constexpr int kWeightStep = 32;          // rows in a stage of LDS
 
 // A tile of kI input channels x kO output channels by kWavesI x kWavesO wavefronts.  kInFirst: the result is [i][o], otherwise [o][i].
 //
-// A transposing read takes 32 bytes, the 16 columns of a fragment, from each of four rows at a time, and these are to lie in different banks: a
-// row's 32-byte blocks stand at place block ^ (row & 3); where a load's 1024 bytes are two rows only, at block ^ (row & 1), and loads stand 64
-// bytes further apart.  All fragments of a lane then lie at a few addresses and constant distances from them.  Four stages as in product8.
+// A transposing read takes 32 bytes, the 16 columns of a fragment, from rows 0..3 and 8..11 at a time, then from 16..19 and 24..27, and these are to lie in
+// different banks: a row's 32-byte blocks stand at place block ^ (row & 3); where a load's 1024 bytes are two rows only, at block ^ (row & 1), and
+// loads stand 64 bytes further apart; every eight rows another 128.  All fragments of a lane then lie at a few addresses and constant
+// distances from them.  Four stages as in product8.
 template <typename G, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
 __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__restrict__ out, G *__restrict__ dbias,
                                                                           const bf16_t *__restrict__ a_rows, const bf16_t *__restrict__ b_rows,
@@ -228,7 +229,9 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
     static_assert(kLoadsI * kRowsI * kWaves == kWeightStep && kLoadsO * kRowsO * kWaves == kWeightStep, "whole loads");
     constexpr int kSwapI = kRowsI == 2 ? 1 : 3, kSwapO = kRowsO == 2 ? 1 : 3;
     constexpr int kLoadI = kRowsI == 2 ? 1088 : 1024, kLoadO = kRowsO == 2 ? 1088 : 1024;      // bytes from load to load in LDS
-    constexpr int kPartI = kWeightStep / kRowsI * kLoadI, kPartO = kWeightStep / kRowsO * kLoadO, kStages = 4;
+    constexpr int kEight = 128;                                                                // and besides from eight rows to the next
+    constexpr int kPartI = kWeightStep / kRowsI * kLoadI + kWeightStep / 8 * kEight, kPartO = kWeightStep / kRowsO * kLoadO + kWeightStep / 8 * kEight;
+    constexpr int kStages = 4;
     __shared__ __attribute__((aligned(1024))) int8_t tile[kStages][kPartI + kPartO];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -263,9 +266,9 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
         const v4u asrc = raw_buffer(a_next, (uint32_t)left * (uint32_t)a.a_ld * 2u);
         const v4u bsrc = raw_buffer(b_next, (uint32_t)left * (uint32_t)a.b_ld * 2u);
 #pragma unroll
-        for (int j = 0; j < kLoadsI; ++j) to_lds(asrc, off_i[j], &tile[stage][(j * kWaves + wave) * kLoadI]);
+        for (int j = 0; j < kLoadsI; ++j) to_lds(asrc, off_i[j], &tile[stage][(j * kWaves + wave) * kLoadI + (j * kWaves + wave) * kRowsI / 8 * kEight]);
 #pragma unroll
-        for (int j = 0; j < kLoadsO; ++j) to_lds(bsrc, off_o[j], &tile[stage][kPartI + (j * kWaves + wave) * kLoadO]);
+        for (int j = 0; j < kLoadsO; ++j) to_lds(bsrc, off_o[j], &tile[stage][kPartI + (j * kWaves + wave) * kLoadO + (j * kWaves + wave) * kRowsO / 8 * kEight]);
         a_next += kWeightStep * a.a_ld;
         b_next += kWeightStep * a.b_ld;
         if (++step == steps) {                       // the next plane
@@ -289,10 +292,10 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
     int at_i[kAtI], at_o[kAtO];                      // of the first fragments
 #pragma unroll
     for (int i = 0; i < kAtI; ++i)
-        at_i[i] = trow / kRowsI * kLoadI + trow % kRowsI * kBytesI + ((wi * kIi + i) ^ (trow & kSwapI)) * 32 + frow % 4 * 8;
+        at_i[i] = trow / kRowsI * kLoadI + fgroup * kEight + trow % kRowsI * kBytesI + ((wi * kIi + i) ^ (trow & kSwapI)) * 32 + frow % 4 * 8;
 #pragma unroll
     for (int o = 0; o < kAtO; ++o)
-        at_o[o] = kPartI + trow / kRowsO * kLoadO + trow % kRowsO * kBytesO + ((wo * kOi + o) ^ (trow & kSwapO)) * 32 + frow % 4 * 8;
+        at_o[o] = kPartI + trow / kRowsO * kLoadO + fgroup * kEight + trow % kRowsO * kBytesO + ((wo * kOi + o) ^ (trow & kSwapO)) * 32 + frow % 4 * 8;
     auto fragment = [&](const int8_t *low, int four_rows) {
         typedef __attribute__((address_space(3))) v4s lds_v4s;
         const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)low);
