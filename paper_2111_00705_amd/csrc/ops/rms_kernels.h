@@ -6,6 +6,9 @@
 //
 // HBM-bound: a row is read once and kept in registers, where it is added, normed and rounded; the next row is on its way meanwhile.  A
 // lane keeps its columns' gradient sums in registers over all rows of its chunk, as in norm_kernels.h.
+// Measured alone, with TB/s of what has to move: forward in 8 bits 16384 x 2048 bf16 with residual 39.6 us (235 MB, 5.9); backward 16384 x 768
+// bf16, n = 8 18.4 (101 MB, 5.5) and 4.0 for the join of its chunks; 20000 x 2047 fp32 kept in 8 bits, n = 20 87 to 107 (533 MB, 5.0 to 6.1: rows of
+// odd length, one in flight a workgroup beside the one worked on).  A copy reaches 6.1 TB/s.
 #pragma once
 #include "rows8.h"
 

@@ -5,6 +5,10 @@
 // A row's values are read, reduced to their largest magnitude and rounded while they stand in registers.  Scales that are powers of two
 // make every product q scale a number of 7 bits: restored values are exact in any of the types, and so are the products of a backward
 // pass that reads the row (weight_kernels.h); the price is up to one bit, half a bit on average.
+//
+// HBM-bound: a row is read once and written once.  16384 x 4096 bf16: to 8 bits 29.6 us (201 MB, 6.8 TB/s), back 28.8 (7.0; the 8 bits come from the
+// memory-side cache).  Teams of 16 lanes to a workgroup of 1024 hold a row in registers between its maximum and its rounding, so that no second
+// read is needed up to 32768 elements of 16 bits, 16384 of 32.
 #pragma once
 #include "op_common.h"
 

@@ -11,6 +11,10 @@
 // each number is widened once and not once for every tile that it meets.  The sum runs over planes and rows.  Both operands lie across it (their rows are the sum's
 // index): a step's rows go from memory to LDS as they lie, without registers, and the transposing LDS reads hand every lane its column's
 // values.
+//
+// 16384 rows, 4096 x 4096, four workers, bfloat16: 439 us with the first kernel, which takes 33 of them (HBM-bound, 6.1 TB/s); 1350 TFLOP/s for the
+// product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  16384 rows, 768 x 2304, eight workers:
+// 70 us, 216 tiles for 256 compute units.
 #pragma once
 #include "product8_kernels.h"
 
