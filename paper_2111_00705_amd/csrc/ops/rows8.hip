@@ -83,21 +83,25 @@ int rms_check(const char *what, int64_t rows, int64_t cols, int32_t type)
 // Workgroups of the forward pass, us at 1024 / 2048 / 4096: in 8 bits 16384 x 2048 bf16 47.5 / 45.4 / 43.0; 8192 x 4096 bf16 48.7 / 50.4 / 47.9;
 // 16384 x 768 19.4 / 20.4 / 20.7.
 constexpr int64_t kRmsBlocks = 4096;
-// Workgroups that the rows of all workers are cut into in the backward pass, and the fewest rows of one.  More keep more rows in flight, and write
+// Workgroups that the rows of all workers are cut into in the backward pass.  More keep more rows in flight, and write
 // more partial sums.  us with the join, at 512 / 750 / 1024 / 2048: 16384 x 768 bf16, n = 8 22.4 / 23.8 / 21.6 / 24.8; 20000 x 2047 fp32 kept in 8 bits,
-// n = 20 134 / 129 / 117 / 118; 8192 x 4096 bf16, n = 4 67.8 / 66.1 / 67.2 / 73.9.  1024 x 4096 bf16, n = 8 at 4 / 2 / 1 rows 15.6 / 16.5 / 23.2.
-// Up to kRmsOnlyRows of a worker are one chunk, which needs no join and no launch for it.
-constexpr int64_t kRmsChunkBlocks = 1024, kRmsChunkRows = 4, kRmsOnlyRows = 16;
+// n = 20 134 / 129 / 117 / 118; 8192 x 4096 bf16, n = 4 67.8 / 66.1 / 67.2 / 73.9.
+constexpr int64_t kRmsChunkBlocks = 1024;
 
 // How a worker's rows are cut for the gain's gradients: chunks of rows with one set of column sums each.
 struct RmsChunks {
     int64_t rows, count;     // rows of a chunk; chunks of a worker
 };
-RmsChunks rms_chunks(int64_t worker_rows, int32_t n)
+// A workgroup takes as many rows at a time as it has teams (of fp32 rows; half as many columns for the same team in 16 bits), one such turn where rows
+// are few, four at least where they fill the chip: 1024 x 4096 bf16, n = 8 at 4 / 2 / 1 turns 15.6 / 16.5 / 23.2 us, 64 x 8192, n = 2 at 4 / 1 turns 17.2 / 12.3.  Up to two turns of
+// a worker's rows are one chunk, which needs no join and no launch for it.
+RmsChunks rms_chunks(int64_t worker_rows, int64_t cols, int32_t n)
 {
-    if (worker_rows <= kRmsOnlyRows) return {kRmsOnlyRows, 1};
+    const int64_t teams = cols <= 128 ? 16 : cols <= 1024 ? 4 : 1;
+    if (worker_rows <= 2 * teams) return {2 * teams, 1};
+    const int64_t turns = std::min<int64_t>(4, ceil_div(worker_rows * n, 256 * teams));
     const int64_t want = std::max<int64_t>(1, ceil_div(kRmsChunkBlocks, n));
-    const int64_t rows = std::max<int64_t>(kRmsChunkRows, ceil_div(worker_rows, want));
+    const int64_t rows = std::max<int64_t>(turns * teams, ceil_div(worker_rows, want));
     return {rows, std::max<int64_t>(1, ceil_div(worker_rows, rows))};
 }
 
@@ -420,7 +424,7 @@ int comp_ams_rms_norm_work_bytes(int64_t rows, int64_t cols, int32_t n, uint64_t
     REQUIRE(n >= 1 && n <= 65535, "%s: n=%d must be in [1, 65535]", what, n);
     REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
     REQUIRE(bytes, "%s: bytes is NULL", what);
-    *bytes = (uint64_t)rms_chunks(rows / n, n).count * (uint64_t)n * (uint64_t)cols * sizeof(float);
+    *bytes = (uint64_t)rms_chunks(rows / n, cols, n).count * (uint64_t)n * (uint64_t)cols * sizeof(float);
     return COMP_AMS_OK;
 }
 
@@ -449,7 +453,7 @@ int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const RmsBackArgs a = {rows, cols, dx_stride, dy_stride, h_stride, dresidual_stride, (float)(1.0 / (double)cols), streamed_rows(rows * cols, type), streamed_out(rows * cols, type),
                            dgain, grad_stride, grad_type};
-    const RmsChunks ch = rms_chunks(rows / n, n);
+    const RmsChunks ch = rms_chunks(rows / n, cols, n);
     float *sums = static_cast<float *>(work);
     bool held = false;
     with_type(type, [&](auto t) {
