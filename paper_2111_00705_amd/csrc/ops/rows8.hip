@@ -92,9 +92,9 @@ constexpr int64_t kRmsChunkBlocks = 1024;
 struct RmsChunks {
     int64_t rows, count;     // rows of a chunk; chunks of a worker
 };
-// A workgroup takes as many rows at a time as it has teams (of fp32 rows; half as many columns for the same team in 16 bits), one such turn where rows
-// are few, four at least where they fill the chip: 1024 x 4096 bf16, n = 8 at 4 / 2 / 1 turns 15.6 / 16.5 / 23.2 us, 64 x 8192, n = 2 at 4 / 1 turns 17.2 / 12.3.  Up to two turns of
-// a worker's rows are one chunk, which needs no join and no launch for it.
+// A workgroup takes as many rows at a time as it has teams (of fp32 rows; 16-bit rows have a team for twice the columns): one such turn where rows
+// are few, four at least where they fill the chip.  us at 4 / 2 / 1 turns: 1024 x 4096 bf16, n = 8 15.6 / 16.5 / 23.2; 64 x 8192, n = 2 17.2 / - / 12.3.
+// Up to two turns of a worker's rows are one chunk, which needs no join and no launch for it.
 RmsChunks rms_chunks(int64_t worker_rows, int64_t cols, int32_t n)
 {
     const int64_t teams = cols <= 128 ? 16 : cols <= 1024 ? 4 : 1;
@@ -149,9 +149,9 @@ int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rs
 // --- the product -----------------------------------------------------------------------------------------------------
 
 // What a tile costs, for the choice among them: us of a step of `alone` for the first workgroup of a compute unit and of `more` for each
-// that it takes besides, and `start` steps for its start and end (results of large tiles leave while nothing else runs on the unit).  Fitted to kernels timed over 25 (products; their weights from memory, as a model's layers in turn find
-// them) and 15 (weight gradients) sizes from 16 x 4096 x 4096 to 4096 x 4096 x 4096.  There the choice was within 15 % of the best, where one
-// tile for all would be up to 4 times off.
+// that it takes besides, and `start` steps for its start and end (results of large tiles leave while nothing else runs on the unit).  Fitted to
+// kernels timed over 25 sizes of products (their weights from memory, as a model's layers in turn find them) and 15 of weight gradients, from
+// 16 x 4096 x 4096 to 4096 x 4096 x 4096.  There the choice was within 15 % of the best, where one tile for all would be up to 4 times off.
 struct TileCost {
     int high, wide;
     double alone, more;

@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 DTYPES = [F32, BF16, F16]
 SIZES = [(1, 1), (3, 2), (5, 7), (4, 16), (9, 33), (2, 64), (7, 130), (3, 255), (3, 256), (6, 257), (5, 511), (5, 512), (4, 768), (3, 1023), (3, 1025),
-         (2, 2047), (2, 2049), (2, 4099), (2, 8192), (2, 8193), (1, 16_385), (1, 33_001), (2, 70_001), (3000, 24), (2500, 1000)]
+         (2, 2047), (2, 2049), (2, 4099), (2, 8192), (2, 8193), (3, 12_001), (2, 16_001), (1, 16_385), (2, 24_001), (1, 30_003), (1, 33_001), (2, 70_001), (3000, 24), (2500, 1000)]
 
 
 def gen(*key):
@@ -151,7 +151,8 @@ def test_rms_norm_of_nothing_but_zeros():
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n,per,cols", [(1, 1, 1), (3, 2, 7), (2, 5, 33), (1, 40, 64), (4, 33, 130), (2, 3, 256), (5, 7, 511), (8, 20, 768), (2, 2, 1025), (3, 9, 2047),
-                                        (2, 3, 4099), (1, 4, 8193), (2, 1, 33_001), (20, 100, 96), (1, 3000, 48)])
+                                        (2, 3, 4099), (1, 4, 8193), (2, 1, 33_001), (20, 100, 96), (1, 3000, 48), (2, 3, 12_001), (1, 5, 16_003), (3, 9, 1000), (1, 33, 100), (2, 2, 9001),
+                                        (1, 700, 1030)])
 def test_rms_norm_backward(n, per, cols, dtype):
     print(f"[case] rms backward {n}x{per}x{cols} {dtype}", flush=True)
     g = gen("rmsb", n, per, cols)
