@@ -185,11 +185,14 @@ static __global__ __launch_bounds__(kPackThreads) void product8_pack(int8_t *__r
     for (int k = threadIdx.x % a.lanes * 16; k < a.cols; k += a.lanes * 16) *reinterpret_cast<v4i *>(to + k) = load_row16(from, k, a.cols);
 }
 
+template <int kM, int kN> constexpr int kProductStages = kM + kN <= 128 ? 8 : 4;
+
 // A tile of kM tokens x kN channels by kWavesM x kWavesN wavefronts.  Rows, strides and addresses are multiples of 16 bytes: memory goes to LDS
 // without registers.  kSplit: a piece of k; the sums go to work[piece][rows][outs].
 //
-// A step is 64 bytes of k.  Of four stages in LDS two are on their way from memory, one has arrived and is read into registers while the matrix
-// instructions work on what was read before: one barrier a step, and nothing waits for memory or LDS within it.  A step's row is four
+// A step is 64 bytes of k.  Of the stages in LDS one has arrived and is read into registers while the matrix instructions work on what was read
+// before, and the others but one are on their way from memory: one barrier a step, and nothing waits for memory or LDS within it.  Four stages fill the
+// LDS for tiles of 256 x 256; those of 64 x 64, whose steps are shorter than memory takes for three, have eight.  A step's row is four
 // 16-byte chunks; chunk c of row r stands at place c ^ (r / 2 & 3), so that eight rows at one chunk lie in different banks.
 template <typename Y, int kM, int kN, int kWavesM, int kWavesN, bool kSplit>
 __global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__restrict__ y, int *__restrict__ work, const int8_t *__restrict__ x,
@@ -197,7 +200,7 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__rest
                                                                     const float *__restrict__ w_scale, const float *__restrict__ bias,
                                                                     ProductArgs a)
 {
-    constexpr int kWaves = kWavesM * kWavesN, kRows = kM + kN, kStep = kProductStep, kStages = 4;
+    constexpr int kWaves = kWavesM * kWavesN, kRows = kM + kN, kStep = kProductStep, kStages = kProductStages<kM, kN>;
     constexpr int kMi = kM / kWavesM / 16, kNi = kN / kWavesN / 16;
     constexpr int kLoads = kRows / 16 / kWaves, kLoadsX = kM / 16 / kWaves;     // wavefront-wide loads of 16 rows each
     static_assert(kM % (16 * kWaves) == 0 && kN % (16 * kWaves) == 0, "whole loads");
@@ -273,27 +276,28 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__rest
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kMi * kNi - kPer * (kMi + kNi), 0);
     };
-    // One step: the next stage has arrived, for every wavefront (of three that were sent the youngest may still be on its way), and nobody
-    // reads the one before any more, which the step after the next but one takes.  Steps past the end read zeros.
+    // One step: the next stage has arrived, for every wavefront (those sent after it may still be on their way), and nobody reads the one before
+    // any more, which the youngest step takes.  Steps past the end read zeros.
     auto step = [&](int u, const Frags &now, Frags &next) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
-        send((u + 3) % kStages);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 3) * kLoads) : "memory");
+        send((u + kStages - 1) % kStages);
         read(next, (u + 1) % kStages);
         multiply(now);
         mixed();
     };
     Frags even, odd;
     const int steps = (k_end - k_begin + kStep - 1) / kStep;
-    send(0);
-    send(1);
-    send(2);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
+#pragma unroll
+    for (int u = 0; u < kStages - 1; ++u) send(u);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
     read(even, 0);
     for (int s = 0; s < steps; s += kStages) {
-        step(0, even, odd);
-        step(1, odd, even);
-        step(2, even, odd);
-        step(3, odd, even);
+#pragma unroll
+        for (int u = 0; u < kStages; u += 2) {
+            if (kStages > 4 && s + u >= steps) break;
+            step(u, even, odd);
+            step(u + 1, odd, even);
+        }
     }
     if constexpr (kSplit) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");     // LDS belongs to the next workgroup after this one

@@ -213,7 +213,7 @@ constexpr int kWeightStep = 32;          // rows in a stage of LDS
 // A transposing read takes 32 bytes, the 16 columns of a fragment, from rows 0..3 and 8..11 at a time, then from 16..19 and 24..27, and these are to lie in
 // different banks: a row's 32-byte blocks stand at place block ^ (row & 3); where a load's 1024 bytes are two rows only, at block ^ (row & 1), and
 // loads stand 64 bytes further apart; every eight rows another 128.  All fragments of a lane then lie at a few addresses and constant
-// distances from them.  Four stages as in product8.
+// distances from them.  Stages as in product8.
 template <typename G, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
 __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__restrict__ out, G *__restrict__ dbias,
                                                                           const bf16_t *__restrict__ a_rows, const bf16_t *__restrict__ b_rows,
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
     constexpr int kLoadI = kRowsI == 2 ? 1088 : 1024, kLoadO = kRowsO == 2 ? 1088 : 1024;      // bytes from load to load in LDS
     constexpr int kEight = 128;                                                                // and besides from eight rows to the next
     constexpr int kPartI = kWeightStep / kRowsI * kLoadI + kWeightStep / 8 * kEight, kPartO = kWeightStep / kRowsO * kLoadO + kWeightStep / 8 * kEight;
-    constexpr int kStages = 4;
+    constexpr int kStages = kI + kO <= 128 ? 8 : 4;
     __shared__ __attribute__((aligned(1024))) int8_t tile[kStages][kPartI + kPartO];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -336,24 +336,25 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
     };
     constexpr int kLoads = kLoadsI + kLoadsO;
     auto advance = [&](int u, const Frags &now, Frags &next) {          // a step, as in product8
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
-        send((u + 3) % kStages);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 3) * kLoads) : "memory");
+        send((u + kStages - 1) % kStages);
         read(next, (u + 1) % kStages);
         multiply(now);
         mixed();
         __builtin_amdgcn_sched_barrier(0);
     };
     Frags even, odd;
-    send(0);
-    send(1);
-    send(2);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
+#pragma unroll
+    for (int u = 0; u < kStages - 1; ++u) send(u);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
     read(even, 0);
     for (int c = begin; c < end; c += kStages) {
-        advance(0, even, odd);
-        advance(1, odd, even);
-        advance(2, even, odd);
-        advance(3, odd, even);
+#pragma unroll
+        for (int u = 0; u < kStages; u += 2) {
+            if (kStages > 4 && c + u >= end) break;
+            advance(u, even, odd);
+            advance(u + 1, odd, even);
+        }
     }
     // nothing is on its way to LDS or read from it any more, by any wavefront
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
