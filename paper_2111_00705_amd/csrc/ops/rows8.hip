@@ -151,7 +151,7 @@ int rms_forward_call(const char *what, void *y, float *scale, void *h, float *rs
 // What a tile costs, for the choice among them: us of a step of `alone` for the first workgroup of a compute unit and of `more` for each
 // that it takes besides, and `start` steps for its start and end (results of large tiles leave while nothing else runs on the unit).  Fitted to
 // kernels timed over 25 sizes of products (their weights from memory, as a model's layers in turn find them) and 15 of weight gradients, from
-// 16 x 4096 x 4096 to 4096 x 4096 x 4096.  There the choice was within 15 % of the best, where one tile for all would be up to 4 times off.
+// 16 x 4096 x 4096 to 4096 x 4096 x 4096.  There the choice was within 20 % of the best, where one tile for all would be up to 4 times off.
 struct TileCost {
     int high, wide;
     double alone, more;
@@ -159,12 +159,13 @@ struct TileCost {
     bool splits;             // whether the sum may be cut into pieces
 };
 constexpr int64_t kLeastPiece = 16;
-// tiles of `pieces` pieces of `steps` steps; cells: of the result; bytes: of the operands.  Pieces have to gain a sixth: they cost another launch.
+// tiles of `pieces` pieces of `steps` steps; cells: of the result; bytes: of the operands.  Pieces have to gain a twentieth: the host
+// pays for another launch.
 double tile_cost(const TileCost &t, int64_t tiles, int64_t pieces, int64_t steps, double cells, double bytes)
 {
     const double deep = (double)ceil_div(std::max<int64_t>(tiles * pieces, 1), 256);
     const double us = std::max((t.alone + (deep - 1) * t.more) * (double)(steps + t.start), bytes / 5e6);
-    return pieces > 1 ? 1.15 * (us + 4.5 + (double)(pieces + 1) * cells * 4.0 / 3e6) : us;
+    return pieces > 1 ? 1.05 * (us + 4.5 + (double)(pieces + 1) * cells * 4.0 / 3e6) : us;
 }
 // The least of them: f(tile, pieces, steps of a piece) for each that is cheaper than those before.
 template <int kTiles, typename F>
@@ -182,7 +183,7 @@ void choose_tile(const TileCost (&costs)[kTiles], int64_t steps, double cells, d
         }
 }
 constexpr TileCost kProductTiles[] = {{256, 256, 1.05, 1.05, 8, false}, {256, 128, 0.65, 0.63, 7, false}, {128, 128, 0.42, 0.32, 6, true},
-                                      {64, 128, 0.37, 0.20, 6, false}, {64, 64, 0.33, 0.12, 6, true}};
+                                      {64, 128, 0.37, 0.20, 6, false}, {64, 64, 0.22, 0.15, 6, true}};
 // Tokens up to which a product goes to product8_few, and with up to how many weights twice as many do: 32 x 4096 x 4096 9.4 us against 12.0 by tiles,
 // 32 x 8192 x 8192 28.9 against 20.3.
 constexpr int64_t kFewRows = 16, kFewWeights = (int64_t)1 << 25;
@@ -400,7 +401,8 @@ int comp_ams_rms_norm(void *y, void *h, float *rstd, const void *x, const void *
     REQUIRE_RMS_FORWARD(what);
     REQUIRE_ROWS(what, "y", y, rows, cols, y_stride, type);
     REQUIRE(!h || h != y || rows == 0, "%s: y and h are the same array", what);
-    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, y_stride, eps, (float)(1.0 / (double)cols), false, streamed_rows(rows * cols, type), streamed_out(rows * cols, type), streamed_h(rows * cols, type)};
+    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, y_stride, eps, (float)(1.0 / (double)cols), false,
+                       streamed_rows(rows * cols, type), streamed_out(rows * cols, type), streamed_h(rows * cols, type)};
     return rms_forward_call(what, y, nullptr, h, rstd, x, residual, gain, a, false, type, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -413,7 +415,8 @@ int comp_ams_rms_norm_q8(int8_t *q, float *scale, void *h, float *rstd, const vo
     REQUIRE_BYTE_ROWS(what, "q", q, rows, cols, q_stride);
     REQUIRE(scale || rows == 0, "%s: scale is NULL", what);
     REQUIRE(aligned(scale, 4), "%s: scale must be 4-byte aligned", what);
-    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, q_stride, eps, (float)(1.0 / (double)cols), binary != 0, streamed_rows(rows * cols, type), false, streamed_h(rows * cols, type)};
+    const RmsArgs a = {rows, cols, x_stride, residual_stride, h_stride, q_stride, eps, (float)(1.0 / (double)cols), binary != 0,
+                       streamed_rows(rows * cols, type), false, streamed_h(rows * cols, type)};
     return rms_forward_call(what, q, scale, h, rstd, x, residual, gain, a, true, type, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -451,7 +454,8 @@ int comp_ams_rms_norm_backward(void *dx, void *dgain, const void *dy, const void
     REQUIRE(work && work_bytes >= need, "%s: needs %llu bytes of work memory", what, (unsigned long long)need);
     REQUIRE(aligned(work, 16), "%s: work must be 16-byte aligned", what);
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const RmsBackArgs a = {rows, cols, dx_stride, dy_stride, h_stride, dresidual_stride, (float)(1.0 / (double)cols), streamed_rows(rows * cols, type), streamed_out(rows * cols, type),
+    const RmsBackArgs a = {rows, cols, dx_stride, dy_stride, h_stride, dresidual_stride, (float)(1.0 / (double)cols),
+                           streamed_rows(rows * cols, type), streamed_out(rows * cols, type),
                            dgain, grad_stride, grad_type};
     const RmsChunks ch = rms_chunks(rows / n, cols, n);
     float *sums = static_cast<float *>(work);
@@ -521,7 +525,8 @@ int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_
             (unsigned long long)s.bytes);
     if (rows == 0 || outs == 0) return COMP_AMS_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    ProductArgs a = {rows, outs, q_stride, w_stride, y_stride, (int)cols, (int)s.tiles_m, (int)s.tiles_n, s.splits, s.k_split, 0, streamed_result(y, rows * outs, y_stride, 0, type)};
+    ProductArgs a = {rows, outs, q_stride, w_stride, y_stride, (int)cols, (int)s.tiles_m, (int)s.tiles_n, s.splits, s.k_split, 0,
+                     streamed_result(y, rows * outs, y_stride, 0, type)};
     const int64_t blocks = s.tiles_m * s.tiles_n * s.splits;
     int8_t *memory = static_cast<int8_t *>(work);
     if (!s.few && cols && !(q_aligned && w_aligned)) {
