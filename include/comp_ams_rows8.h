@@ -85,13 +85,16 @@ int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, int3
  *   dweight[w][o][i] = sum dy[r][o] q[r][i] scale[r],  dbias[w][o] = sum dy[r][o]        over the rows r of worker w
  * Workers as for comp_ams_layer_norm_backward.  dweight points at the weight's place in worker 0's row, dense, [outs][cols], or [cols][outs]
  * with in_first != 0; dbias (may be NULL) at the bias'; the next worker's are grad_stride elements further.
- * Sums are fp32.  Before the product dy[r][o] scale[r] is rounded to fp32 and then, for dy in 16 bits, to 16 bits of mantissa (nothing is lost of
- * half precision with scales that are powers of two).  binary != 0 promises that all scales are powers of two, as binary quantising
- * gives them; dy in bfloat16 then takes one product in place of two, and where the promise does not hold q scale is rounded to bfloat16.
+ * Sums are fp32.  Before the product dy[r][o] scale[r] is rounded to fp32 and then, for dy in 16 bits, to 16 bits of mantissa; of bfloat16 it may
+ * be q[r][i] scale[r] in its place.  binary != 0 promises that all scales are powers of two, as binary quantising gives them; dy in 16 bits then takes
+ * one product in place of two and nothing is lost, and where the promise does not hold q scale is rounded to dy's type.
+ * Of half precision with binary != 0, rows whose q scale is out of its range (not a multiple of 2^-24, or beyond 65504) are added
+ * apart, at a far lower rate: rows of numbers in half precision have none.  Its numbers below 2^-14, in dy or q scale, are as the matrix unit
+ * takes them: their products are exact to 2^-24 of what they would be with 2^-14 in their place.
  * An infinity or a NaN in dy or a scale reaches the worker's gradients that it belongs to, as an infinity or a NaN.
  * rows >= 0 a multiple of n and below 2^32, a worker's below 2^29; 0 <= cols, outs <= 2^23.  With rows = 0 the gradients are zero.
- * work: comp_ams_linear_weight_grad_work_bytes() bytes, 16-byte aligned, not kept from one call to the next: q in bfloat16, and dy too
- * unless it is bfloat16 with binary != 0, outs is a multiple of 8 and, as dy_aligned != 0 promises, dy and its stride are multiples of 16 bytes.
+ * work: comp_ams_linear_weight_grad_work_bytes() bytes, 16-byte aligned, not kept from one call to the next: q in 16 bits, and dy too
+ * unless one product takes it, outs is a multiple of 8 and, as dy_aligned != 0 promises, dy and its stride are multiples of 16 bytes.
  */
 int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, const int8_t *q, const float *scale, int64_t rows,
                                 int64_t cols, int64_t outs, int64_t dy_stride, int64_t q_stride, int32_t n, int64_t grad_stride,

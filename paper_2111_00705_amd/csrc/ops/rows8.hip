@@ -238,21 +238,28 @@ constexpr TileCost kWeightTiles[] = {{256, 256, 0.83, 0.83, 16, false}, {128, 12
 // How a call is cut, and where its work memory holds what.
 struct WeightShape {
     int tile;                // input and output channels of a tile
-    int planes;              // of dy
+    int q_planes, dy_planes; // one of them is 1
     bool copied;             // dy is written anew
+    bool half;               // in half precision
     int64_t tiles_i, tiles_o;
     int64_t splits, split_steps;         // pieces of the sum over planes and steps of rows, steps of a piece
     int64_t bias_chunks, bias_rows;      // pieces of a worker's rows for the bias, rows of a piece
     int64_t a_ld, b_ld;
-    uint64_t a_at, b_at, sums_at, bias_at, bytes;
+    int64_t lost_ld;
+    uint64_t a_at, b_at, sums_at, bias_at, lost_at, bytes;
 };
 WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bool binary, int32_t type, bool dy_aligned)
 {
     const int64_t per = rows / n;
     WeightShape s = {};
-    s.planes = type == COMP_AMS_F32 ? 3 : type == COMP_AMS_BF16 && binary ? 1 : 2;
-    s.copied = s.planes > 1 || !dy_aligned || outs % 8 != 0;
-    const int64_t steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.planes);
+    const bool as_it_lies = dy_aligned && outs % 8 == 0;
+    s.q_planes = 1;
+    s.dy_planes = type == COMP_AMS_F32 ? 3 : binary ? 1 : 2;
+    // bytes written: two planes of q scale, and dy if it is not read as it lies; or q and two planes of dy scale
+    if (type == COMP_AMS_BF16 && !binary && cols + (as_it_lies ? 0 : outs) <= 2 * outs) s.q_planes = 2, s.dy_planes = 1;
+    s.copied = s.dy_planes > 1 || !as_it_lies;
+    s.half = type == COMP_AMS_F16 && s.dy_planes == 1;
+    const int64_t steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.q_planes * s.dy_planes);
     choose_tile(kWeightTiles, steps, (double)cols * (double)outs * n, 0.0, cols, outs, n, [&](const TileCost &t, int64_t pieces, int64_t length) {
         s.tile = t.high, s.tiles_i = ceil_div(cols, t.high), s.tiles_o = ceil_div(outs, t.wide);
         s.split_steps = length, s.splits = pieces;
@@ -261,13 +268,15 @@ WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bo
     s.bias_rows = std::max<int64_t>(64, ceil_div(per, want));
     s.bias_chunks = std::max<int64_t>(1, ceil_div(per, s.bias_rows));
     s.a_ld = ceil_div(cols, 8) * 8, s.b_ld = ceil_div(outs, 8) * 8;
-    const uint64_t a_bytes = (uint64_t)(rows * s.a_ld) * 2, b_bytes = s.copied ? (uint64_t)(s.planes * rows * s.b_ld) * 2 : 0;
+    s.lost_ld = s.half ? ceil_div(per, 16) * 16 : 0;
+    const uint64_t a_bytes = (uint64_t)(s.q_planes * rows * s.a_ld) * 2, b_bytes = s.copied ? (uint64_t)(s.dy_planes * rows * s.b_ld) * 2 : 0;
     const uint64_t sums = s.splits > 1 ? (uint64_t)(s.splits * n) * (uint64_t)(cols * outs) * sizeof(float) : 0;
     s.a_at = 0;
     s.b_at = s.a_at + a_bytes;
     s.sums_at = s.b_at + b_bytes;
     s.bias_at = s.sums_at + (sums + 15) / 16 * 16;
-    s.bytes = s.bias_at + (uint64_t)(s.bias_chunks * n * outs) * sizeof(float);
+    s.lost_at = s.bias_at + ((uint64_t)(s.bias_chunks * n * outs) * sizeof(float) + 15) / 16 * 16;
+    s.bytes = s.lost_at + (uint64_t)(n * s.lost_ld);
     return s;
 }
 
@@ -290,15 +299,17 @@ void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, con
 {
     PrepareArgs a = {};
     a.rows = rows, a.cols = cols, a.outs = outs, a.q_stride = q_stride, a.dy_stride = dy_stride;
-    a.a_ld = s.a_ld, a.b_ld = s.b_ld, a.b_plane = rows * s.b_ld;
+    a.a_ld = s.a_ld, a.b_ld = s.b_ld, a.a_plane = rows * s.a_ld, a.b_plane = rows * s.b_ld;
+    a.lost = reinterpret_cast<uint8_t *>(work + s.lost_at), a.lost_ld = s.lost_ld;
     a.worker_rows = rows / n, a.bias_rows = s.bias_rows, a.bias_chunks = (unsigned)s.bias_chunks;
     a.lanes_a = shared_lanes(s.a_ld / 8), a.lanes_b = shared_lanes(s.b_ld / 8);
     const bool product = rows > 0 && cols > 0;
     a.blocks_a = product ? (unsigned)ceil_div(rows, kPrepareThreads / a.lanes_a * kPrepareRows) : 0u;
     a.blocks_b = product && s.copied ? (unsigned)ceil_div(rows, kPrepareThreads / a.lanes_b * kPrepareRows) : 0u;
     const int64_t blocks = (int64_t)a.blocks_a + a.blocks_b + (bias ? n * s.bias_chunks * ceil_div(outs, kBiasCols) : 0);
-    auto go = [&](auto t, auto planes) {
+    auto go = [&](auto t, auto q_planes, auto dy_planes) {
         using T = decltype(t);
+        constexpr int kQ = decltype(q_planes)::value, kD = decltype(dy_planes)::value;
         auto launch = [&](auto kernel) {
             in_launches(blocks, kPrepareThreads, [&](unsigned first, unsigned count) {
                 a.first = first;
@@ -306,13 +317,17 @@ void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, con
                                                               reinterpret_cast<float *>(work + s.bias_at), static_cast<const T *>(dy), q, scale, a);
             });
         };
-        if (bias) launch(weight_prepare<T, decltype(planes)::value, true>);
-        else launch(weight_prepare<T, decltype(planes)::value, false>);
+        if (bias) launch(weight_prepare<T, kQ, kD, true>);
+        else launch(weight_prepare<T, kQ, kD, false>);
     };
-    if (type == COMP_AMS_F32) go(float{}, std::integral_constant<int, 3>{});
-    else if (type == COMP_AMS_F16) go(f16_t{}, std::integral_constant<int, 2>{});
-    else if (binary) go(bf16_t{}, std::integral_constant<int, 1>{});
-    else go(bf16_t{}, std::integral_constant<int, 2>{});
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 2> two{};
+    if (type == COMP_AMS_F32) go(float{}, one, std::integral_constant<int, 3>{});
+    else if (type == COMP_AMS_F16 && s.half) go(f16_t{}, one, one);
+    else if (type == COMP_AMS_F16) go(f16_t{}, one, two);
+    else if (s.q_planes == 2) go(bf16_t{}, two, one);
+    else if (s.dy_planes == 2) go(bf16_t{}, one, two);
+    else go(bf16_t{}, one, one);
 }
 
 template <typename G>
@@ -327,16 +342,16 @@ void weight_launch(G *out, G *dbias, const bf16_t *a_rows, const bf16_t *b_rows,
             kernel<<<count, threads, 0, stream>>>(out, dbias, a_rows, b_rows, bias_sums, a);
         });
     };
-    if (tile == 256) {
-        if (in_first) go(weight_grad<G, true, 256, 256, 2, 4>, 512);
-        else go(weight_grad<G, false, 256, 256, 2, 4>, 512);
-    } else if (tile == 128) {
-        if (in_first) go(weight_grad<G, true, 128, 128, 2, 2>, 256);
-        else go(weight_grad<G, false, 128, 128, 2, 2>, 256);
-    } else {
-        if (in_first) go(weight_grad<G, true, 64, 64, 2, 2>, 256);
-        else go(weight_grad<G, false, 64, 64, 2, 2>, 256);
-    }
+    auto form = [&](auto half, auto first) {
+        constexpr bool kHalf = decltype(half)::value, kFirst = decltype(first)::value;
+        if (tile == 256) go(weight_grad<G, kHalf, kFirst, 256, 256, 2, 4>, 512);
+        else if (tile == 128) go(weight_grad<G, kHalf, kFirst, 128, 128, 2, 2>, 256);
+        else go(weight_grad<G, kHalf, kFirst, 64, 64, 2, 2>, 256);
+    };
+    if (a.lost && in_first) form(std::true_type{}, std::true_type{});
+    else if (a.lost) form(std::true_type{}, std::false_type{});
+    else if (in_first) form(std::false_type{}, std::true_type{});
+    else form(std::false_type{}, std::false_type{});
 }
 
 }  // namespace
@@ -625,9 +640,14 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
     weight_prepare_launch(s, memory, dy, q, scale, rows, cols, outs, dy_stride, q_stride, n, binary != 0, dbias != nullptr, type, stream);
     if (const int rc = launched(what)) return rc;              // what the product would read has not been written
     WeightArgs a = {};
-    a.cols = cols, a.outs = outs, a.a_ld = s.a_ld, a.b_ld = s.copied ? s.b_ld : dy_stride, a.b_plane = rows * s.b_ld;
+    a.cols = cols, a.outs = outs, a.a_ld = s.a_ld, a.b_ld = s.copied ? s.b_ld : dy_stride;
+    a.a_plane = s.q_planes > 1 ? rows * s.a_ld : 0, a.b_plane = s.dy_planes > 1 ? rows * s.b_ld : 0;
+    if (s.half) {
+        a.lost = reinterpret_cast<uint8_t *>(memory + s.lost_at), a.lost_ld = s.lost_ld;
+        a.q = q, a.scale = scale, a.dy = static_cast<const f16_t *>(dy), a.q_stride = q_stride, a.dy_stride = dy_stride;
+    }
     a.worker_rows = rows / n, a.out_stride = in_first ? outs : cols;
-    a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.planes = s.planes;
+    a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.planes = s.q_planes * s.dy_planes;
     a.splits = (int)s.splits, a.split_steps = (int)s.split_steps;
     a.bias_chunks = (unsigned)s.bias_chunks, a.grad_stride = grad_stride;
     a.stream_out = s.splits == 1 && streamed_result(dweight, cells * n, a.out_stride, n > 1 ? grad_stride : 0, grad_type);

@@ -4,18 +4,24 @@
 //
 // The matrix instruction takes bfloat16, which holds q exactly (7 bits); what it cannot hold goes in several planes whose products are added up:
 //   dy in bfloat16, scales powers of two     q scale and dy, both exact: one plane
-//   dy in bfloat16, any scale; in float16    fl32(dy scale) in two planes of 8 bits: 2^-17 of each product is lost, nothing where the
-//                                            scale is a power of two and dy half precision
-//   dy in float32                            the same in three planes: all 24 bits
+//   dy in float16, scales powers of two      the same in half precision; what of q scale is out of its range is added at the end
+//   dy in bfloat16, any scale                fl32(q scale) or fl32(dy scale), whichever makes less to write, in two planes of 8 bits: 2^-17 of
+//                                            each product is lost, nothing where the scale is a power of two
+//   dy in float16, any scale                 fl32(dy scale) in two planes, the same
+//   dy in float32                            fl32(dy scale) in three planes: all 24 bits
 // A first kernel writes q and the planes of dy as rows of bfloat16 (dy itself is read where one plane does and its rows are aligned), so that
 // each number is widened once and not once for every tile that it meets.  The sum runs over planes and rows.  Both operands lie across it (their rows are the sum's
 // index): a step's rows go from memory to LDS as they lie, without registers, and the transposing LDS reads hand every lane its column's
 // values.
 //
 // 16384 rows, 4096 x 4096, four workers, bfloat16: 439 us with the first kernel, which takes 33 of them (HBM-bound, 6.1 TB/s); 1350 TFLOP/s for the
-// product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  16384 rows, 768 x 2304, eight workers:
+// product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  Half precision with scales of powers
+// of two, one worker: 414 us, in two planes of bfloat16 806 (13698 rows, 192 x 3914, two workers: 78 and 148, most of it the planes' bytes).  bfloat16 with
+// any scales, 6168 rows, 183 x 4697, four workers: 80 us with the planes on q's side, 90 on dy's.  16384 rows, 768 x 2304, eight workers:
 // 70 us, 216 tiles for 256 compute units.
 #pragma once
+#include <type_traits>
+
 #include "product8_kernels.h"
 
 namespace cams_ops {
@@ -23,9 +29,6 @@ namespace cams_ops {
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
-
-template <typename T, bool kBinary> constexpr int kPlanes = sizeof(T) == 4 ? 3 : 2;
-template <> constexpr int kPlanes<bf16_t, true> = 1;
 
 // x = hi + rest with 8 bits in hi.  Of an infinity nothing is left.
 __device__ __forceinline__ float take_plane(float &x)
@@ -35,11 +38,20 @@ __device__ __forceinline__ float take_plane(float &x)
     return hi;
 }
 
+// x in half precision, the nearest finite number (of a NaN, a NaN).  Rows of q with a power of two that was made for half precision fit: their
+// numbers are multiples of 2^-24 and at most 65504; others may not.
+__device__ __forceinline__ float half_of(float x)
+{
+    return widen1(narrow1<f16_t>(fabsf(x) > 65504.f ? copysignf(65504.f, x) : x));
+}
+
 constexpr int kPrepareThreads = 256;
 
 struct PrepareArgs {
     int64_t rows, cols, outs, q_stride, dy_stride;
-    int64_t a_ld, b_ld, b_plane;                     // rows of the results, elements apart, and planes of dy
+    int64_t a_ld, b_ld, a_plane, b_plane;            // rows of the results, elements apart, and planes of them
+    uint8_t *lost;                                   // rows of q scale that half precision does not hold: 1, the others 0
+    int64_t lost_ld;                                 // from worker to worker
     int64_t worker_rows, bias_rows;                  // rows of a worker, and of one of its pieces for the bias
     int lanes_a, lanes_b;                            // lanes that share a row, powers of two up to 256
     unsigned blocks_a, blocks_b;                     // workgroups for q and for dy; the others are for the bias
@@ -116,11 +128,11 @@ __device__ __forceinline__ void bias_join(G *__restrict__ dbias, const float *__
     dbias[worker * grad_stride + col] = narrow1<G>(sum);
 }
 
-// Rows of bfloat16 whose length is a multiple of eight (zeros behind the row): q scale (one plane) or q; the planes of dy scale, or dy itself.
-// kBias: further workgroups sum dy's columns.  Lanes that share a row take kPrepareRows rows, whose loads are on their way together: one after the
-// other 16384 rows of 768 took 8.2 us in place of 7.4.
+// Rows in 16 bits whose length is a multiple of eight (zeros behind the row): kQ planes of q scale where dy stays as it is (kD = 1), q otherwise; kD
+// planes of dy scale, or dy itself.  In half precision where dy is and stays so.  kBias: further workgroups sum dy's columns.  Lanes that share a
+// row take kPrepareRows rows, whose loads are on their way together: one after the other 16384 rows of 768 took 8.2 us in place of 7.4.
 constexpr int kPrepareRows = 4;
-template <typename T, int kP, bool kBias>
+template <typename T, int kQ, int kD, bool kBias>
 __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__restrict__ a_out, bf16_t *__restrict__ b_out, float *__restrict__ sums,
                                                                   const T *__restrict__ dy, const int8_t *__restrict__ q,
                                                                   const float *__restrict__ scale, PrepareArgs a)
@@ -132,6 +144,8 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
             return;
         }
     }
+    constexpr bool kHalf = kD == 1 && std::is_same<T, f16_t>::value;
+    typedef typename std::conditional<kHalf, f16_t, bf16_t>::type H;
     const bool of_q = block < a.blocks_a;
     if (!of_q) block -= a.blocks_a;
     const int lanes = of_q ? a.lanes_a : a.lanes_b, beside = kPrepareThreads / lanes;     // rows that a workgroup takes at a time
@@ -145,6 +159,12 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
         s[u] = scale[row[u]];
     }
     if (of_q) {
+        __shared__ int lost[kHalf ? kPrepareThreads * kPrepareRows : 1];
+        if constexpr (kHalf) {
+#pragma unroll
+            for (int u = 0; u < kPrepareRows; ++u) lost[u * kPrepareThreads + threadIdx.x] = 0;
+            __syncthreads();
+        }
         for (int64_t c = lane * 8; c < a.cols; c += lanes * 8) {
             uint64_t raw[kPrepareRows];
             if (a.cols >= 8) {
@@ -163,11 +183,43 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
             for (int u = 0; u < kPrepareRows; ++u) {
                 float x[8];
                 from_bytes<8>(raw[u], x);
-                if constexpr (kP == 1) {
+                if constexpr (kD == 1) {
 #pragma unroll
                     for (int v = 0; v < 8; ++v) x[v] *= s[u];
                 }
-                *reinterpret_cast<v4u *>(a_out + row[u] * a.a_ld + c) = narrow<bf16_t>(x);
+                if constexpr (kHalf) {
+                    bool less = false;
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) {
+                        const float y = half_of(x[v]);
+                        less |= (y < x[v] || y > x[v]) && (fabsf(x[v]) < 0x1p-14f || fabsf(x[v]) > 65504.f);    // of others eleven bits are kept
+                        x[v] = y;
+                    }
+                    if (less) lost[u * kPrepareThreads + threadIdx.x / lanes] = 1;
+                }
+#pragma unroll
+                for (int p = 0; p < kQ; ++p) {
+                    float plane[8];
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) {
+                        plane[v] = x[v];
+                        if (p < kQ - 1) {
+                            plane[v] = take_plane(x[v]);
+                            if (x[v] == 0.f) x[v] = plane[v] * 0x1p-60f;         // an infinite dy meets no zero that was none
+                        }
+                    }
+                    *reinterpret_cast<v4u *>(a_out + p * a.a_plane + row[u] * a.a_ld + c) = narrow<H>(plane);
+                }
+            }
+        }
+        if constexpr (kHalf) {
+            __syncthreads();
+            if (lane == 0) {
+#pragma unroll
+                for (int u = 0; u < kPrepareRows; ++u) {
+                    const uint32_t at = (uint32_t)row[u], worker = at / (uint32_t)a.worker_rows;
+                    a.lost[worker * a.lost_ld + (at - worker * (uint32_t)a.worker_rows)] = (uint8_t)lost[u * kPrepareThreads + threadIdx.x / lanes];
+                }
             }
         }
         return;
@@ -178,23 +230,23 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
         for (int u = 0; u < kPrepareRows; ++u) load_eight(x[u], dy + row[u] * a.dy_stride, (int)c, (int)a.outs);
 #pragma unroll
         for (int u = 0; u < kPrepareRows; ++u) {
-            if constexpr (kP > 1) {
+            if constexpr (kD > 1) {
 #pragma unroll
                 for (int v = 0; v < 8; ++v) x[u][v] *= s[u];
             }
 #pragma unroll
-            for (int p = 0; p < kP; ++p) {
+            for (int p = 0; p < kD; ++p) {
                 float plane[8];
 #pragma unroll
-                for (int v = 0; v < 8; ++v) plane[v] = p < kP - 1 ? take_plane(x[u][v]) : x[u][v];
-                *reinterpret_cast<v4u *>(b_out + p * a.b_plane + row[u] * a.b_ld + c) = narrow<bf16_t>(plane);
+                for (int v = 0; v < 8; ++v) plane[v] = p < kD - 1 ? take_plane(x[u][v]) : x[u][v];
+                *reinterpret_cast<v4u *>(b_out + p * a.b_plane + row[u] * a.b_ld + c) = narrow<H>(plane);
             }
         }
     }
 }
 
 struct WeightArgs {
-    int64_t cols, outs, a_ld, b_ld, b_plane;
+    int64_t cols, outs, a_ld, b_ld, a_plane, b_plane;
     int64_t worker_rows;
     int64_t out_stride, worker_stride, piece_stride; // of the result, in elements: its rows', the workers', the pieces'
     int tiles_i, tiles_o, n, planes;
@@ -204,9 +256,66 @@ struct WeightArgs {
     unsigned tiles;                                  // workgroups for tiles; the others join the bias' sums
     unsigned bias_chunks;
     int64_t grad_stride;
+    // in half precision: rows that are not all there, and q, scale and dy as they lie
+    const uint8_t *lost;
+    int64_t lost_ld;
+    const int8_t *q;
+    const float *scale;
+    const f16_t *dy;
+    int64_t q_stride, dy_stride;
 };
 
 constexpr int kWeightStep = 32;          // rows in a stage of LDS
+
+template <bool kHalf> __device__ __forceinline__ v4f matrix_step(v8bf x, v8bf y, v4f sum)
+{
+    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+    if constexpr (kHalf) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, y), sum, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, sum, 0, 0, 0);
+}
+
+// The rows of a worker in [lo, hi) that half precision does not hold: 4096 are looked at at a time, and f(row) is called for each (there are few
+// or none).  lo and the workers' places are multiples of 16; what stands behind a worker's rows is not asked for by f.
+template <typename F> __device__ __forceinline__ void each_lost(const uint8_t *lost, int lo, int hi, F &&f)
+{
+    const int lane = threadIdx.x % kWave;
+    for (int base = lo; base < hi; base += kWave * 64) {
+        v4u some = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int u = 0; u < 64; u += 16)
+            if (base + lane * 64 + u < hi) some |= *reinterpret_cast<const v4u *>(lost + base + lane * 64 + u);
+        for (uint64_t lanes = __ballot((some[0] | some[1] | some[2] | some[3]) != 0u); lanes; lanes &= lanes - 1) {
+            const int first = base + __builtin_ctzll(lanes) * 64;
+            for (int row = first; row < min(first + 64, hi); ++row)
+                if (lost[row]) f(row);
+        }
+    }
+}
+
+// What half precision leaves out of sixteen rows of a result: the sums of (q scale - half_of(q scale)) dy over those rows of the worker, for the channel
+// `across` of a lane and the fragments from channel `along` on.  Infinities of dy are left to the product (which gives NaN for them where
+// half_of(q scale) is zero).
+template <bool kInFirst, int kAlong>
+__device__ __forceinline__ void lost_sums(float (&sum)[kAlong][4], const WeightArgs &a, int worker, int lo, int hi, int64_t across, int64_t along)
+{
+    each_lost(a.lost + worker * a.lost_ld, lo, hi, [&](int row) {
+        const int64_t r = worker * a.worker_rows + row;
+        const float s = a.scale[r];
+        auto left = [&](int64_t col) {
+            const float x = col < a.cols ? (float)a.q[r * a.q_stride + col] * s : 0.f;
+            return x - half_of(x);
+        };
+        auto grad = [&](int64_t col) {
+            const float d = col < a.outs ? widen1(a.dy[r * a.dy_stride + col]) : 0.f;
+            return fabsf(d) == INFINITY ? 0.f : d;
+        };
+        const float mine = kInFirst ? left(across) : grad(across);
+#pragma unroll
+        for (int y = 0; y < kAlong; ++y)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum[y][c] = __builtin_fmaf(mine, kInFirst ? grad(along + y * 16 + c) : left(along + y * 16 + c), sum[y][c]);
+    });
+}
 
 // A tile of kI input channels x kO output channels by kWavesI x kWavesO wavefronts.  kInFirst: the result is [i][o], otherwise [o][i].
 //
@@ -214,7 +323,7 @@ constexpr int kWeightStep = 32;          // rows in a stage of LDS
 // different banks: a row's 32-byte blocks stand at place block ^ (row & 3); where a load's 1024 bytes are two rows only, at block ^ (row & 1), and
 // loads stand 64 bytes further apart; every eight rows another 128.  All fragments of a lane then lie at a few addresses and constant
 // distances from them.  Stages as in product8.
-template <typename G, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
+template <typename G, bool kHalf, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
 __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__restrict__ out, G *__restrict__ dbias,
                                                                           const bf16_t *__restrict__ a_rows, const bf16_t *__restrict__ b_rows,
                                                                           const float *__restrict__ bias_sums, WeightArgs a)
@@ -260,9 +369,9 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
 #pragma unroll
     for (int j = 0; j < kLoadsO; ++j) off_o[j] = offset((j * kWaves + wave) * kRowsO, kBytesO, kSwapO, a.outs - o0, a.b_ld);
     int step = begin % max(steps, 1), unsent = end - begin;
-    const bf16_t *a_next = at + (int64_t)step * kWeightStep * a.a_ld;
+    const bf16_t *a_next = at + begin / max(steps, 1) * a.a_plane + (int64_t)step * kWeightStep * a.a_ld;
     const bf16_t *b_next = bt + begin / max(steps, 1) * a.b_plane + (int64_t)step * kWeightStep * a.b_ld;
-    const int64_t a_back = (int64_t)steps * kWeightStep * a.a_ld, b_back = (int64_t)steps * kWeightStep * a.b_ld - a.b_plane;
+    const int64_t a_back = (int64_t)steps * kWeightStep * a.a_ld - a.a_plane, b_back = (int64_t)steps * kWeightStep * a.b_ld - a.b_plane;
     auto send = [&](int stage) {                     // the next step's rows, memory to LDS, asynchronous; zeros after the last one
         // buffers that end with the worker's last row
         const int left = unsent > 0 ? min(rows - step * kWeightStep, kWeightStep) : 0;
@@ -321,8 +430,8 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
         for (int i = 0; i < kIi; ++i)
 #pragma unroll
             for (int o = 0; o < kOi; ++o) {
-                if constexpr (kInFirst) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.o[o], f.i[i], acc[i][o], 0, 0, 0);
-                else acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.i[i], f.o[o], acc[i][o], 0, 0, 0);
+                if constexpr (kInFirst) acc[i][o] = matrix_step<kHalf>(f.o[o], f.i[i], acc[i][o]);
+                else acc[i][o] = matrix_step<kHalf>(f.i[i], f.o[o], acc[i][o]);
             }
     };
     constexpr int kReads = 2 * (kIi + kOi), kPer = kIi * kOi / kReads;
@@ -346,6 +455,8 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
     Frags even, odd;
 #pragma unroll
     for (int u = 0; u < kStages - 1; ++u) send(u);
+    bool lost = false;                               // asked for here, while the first rows are on their way
+    if constexpr (kHalf) each_lost(a.lost + worker * a.lost_ld, begin * kWeightStep, min(end * kWeightStep, rows), [&](int) { lost = true; });
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
     read(even, 0);
     for (int c = begin; c < end; c += kStages) {
@@ -366,12 +477,19 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
     static_assert(kWaves * 16 * kSixteenLd<G, kAlong> * sizeof(G) <= sizeof tile, "room for the results");
 #pragma unroll
     for (int x = 0; x < kAcross; ++x) {
+        const int64_t row = row0 + x * 16;
+        float more[kAlong][4] = {};
+        if constexpr (kHalf) {
+            if (lost) lost_sums<kInFirst, kAlong>(more, a, worker, begin * kWeightStep, min(end * kWeightStep, rows), row + frow, col0 + fgroup * 4);
+        }
         G values[kAlong][4];
 #pragma unroll
         for (int y = 0; y < kAlong; ++y)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) values[y][c] = narrow1<G>(kInFirst ? acc[kInFirst ? x : 0][kInFirst ? y : 0][c] : acc[kInFirst ? 0 : y][kInFirst ? 0 : x][c]);
-        const int64_t row = row0 + x * 16;
+            for (int c = 0; c < 4; ++c) {
+                const float sum = kInFirst ? acc[kInFirst ? x : 0][kInFirst ? y : 0][c] : acc[kInFirst ? 0 : y][kInFirst ? 0 : x][c];
+                values[y][c] = narrow1<G>(kHalf ? sum + more[y][c] : sum);
+            }
         store_sixteen<G, kAlong>(mine, values, ot + row * a.out_stride + col0, a.out_stride, across - row, along - col0, a.stream_out);
     }
 }

@@ -357,6 +357,66 @@ def test_linear_weight_grad_of_nothing():
     assert (dw == 5).all()
 
 
+@pytest.mark.parametrize("n,per,cols,outs", [(2, 1, 1, 1), (2, 5, 9, 4), (2, 70, 33, 130), (2, 300, 129, 127), (2, 33, 2100, 2080), (2, 4200, 64, 72)])
+def test_linear_weight_grad_rows_that_half_precision_does_not_hold(n, per, cols, outs):
+    """Scales of 2^-126 to 2^100 beside common ones, a worker with nothing but small ones.
+
+    The sums' tolerance is that of other rows, (per + 64) roundings of 2^-24 of the sum of the products' sizes, but for numbers below half precision's
+    least normal one, 2^-14: the matrix unit lines products up by their operands' exponents, which for those is the least normal number's, and cuts them
+    24 bits below the largest.  Such a factor counts as 2^-14 in the products' sizes.  An x of up to 2^-25 rounds to zero: it is added apart, in 32 bits."""
+    print(f"[case] weights out of half {n}x{per} {cols}->{outs}", flush=True)
+    g = gen("weights half", n, per, cols, outs)
+    q = whole(g, n * per, cols)
+    power = torch.randint(-6, 3, (n * per,), generator=g)
+    power[:per] = torch.randint(-60, -24 if per % 2 else -32, (per,), generator=g)         # some and nothing of which rounds to more than zero
+    power[0] = -126
+    power[-1] = 10
+    if per > 30:
+        power[per + 7], power[per + 29], power[-2] = 100, -25, -40
+    scale = torch.ldexp(torch.ones(n * per), power)
+    dy = randn(g, n * per, outs, std=0.1).to(F16)
+    dw, db, _, s_db = Q.weight_grad(dy, q, scale, n, True)
+    x, d = (q.double() * scale.double()[:, None]).abs().view(n, per, cols), dy.double().abs().view(n, per, outs)
+    x = torch.where(x > 2.0 ** -25, x.clamp(min=2.0 ** -14), x)
+    s_dw = (d.clamp(min=2.0 ** -14).transpose(1, 2).contiguous() @ x) * ((per + 64) * Q.E32) + 2.0 ** -120
+    for pad, lead in ((0, 0), (5, 3)):
+        qv, dyv = strided(q, pad, lead)[0], strided(dy, pad, lead, float("nan"))[0]
+        for grad in (F32, BF16):
+            for turned in (False, True):
+                buf = torch.full((n, outs * cols + outs), 7.0, dtype=grad, device="cuda")
+                w = buf[:, :outs * cols]
+                w = w.unflatten(1, (cols, outs)).transpose(1, 2) if turned else w.unflatten(1, (outs, cols))
+                b = buf[:, outs * cols:]
+                P.linear_weight_grad(dyv, qv, scale.cuda(), w, b, binary=True)
+                R.close(w, dw, s_dw, f"dweight {grad} {turned}")
+                R.close(b, db, s_db, "dbias")
+
+
+def test_linear_weight_grad_half_precision_with_scales_that_are_no_numbers():
+    g = gen("weights half nan")
+    q, dy = whole(g, 90, 40), randn(g, 90, 48).to(F16)
+    scale = torch.ones(90)
+    scale[50], scale[20] = float("nan"), 2.0 ** -120
+    dw = torch.zeros(3, 48, 40, device="cuda")
+    P.linear_weight_grad(dy.cuda(), q.cuda(), scale.cuda(), dw, binary=True)
+    assert torch.isnan(dw[1]).all() and torch.isfinite(dw[0]).all() and torch.isfinite(dw[2]).all()
+
+
+def test_linear_weight_grad_infinities_beside_planes_of_the_input():
+    """bfloat16, any scales, more outputs than inputs: the second plane of an input that the first one holds is no zero."""
+    g = gen("weights inf planes")
+    q, scale = Q.quantized(randn(g, 80, 24), True)
+    q[q == 0] = 1
+    dy = randn(g, 80, 56).to(BF16)
+    dy[13, 4], dy[70, 9] = float("inf"), float("-inf")
+    dw = torch.zeros(2, 56, 24, device="cuda")
+    P.linear_weight_grad(dy.cuda(), q.cuda(), scale.cuda(), dw)
+    want = torch.einsum("wro,wri->woi", dy.double().view(2, 40, 56), (q.double() * scale.double()[:, None]).view(2, 40, 24))
+    got = dw.cpu().double()
+    assert not torch.isnan(got).any() and torch.equal(torch.isinf(got), torch.isinf(want))
+    assert torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_linear_weight_grad_infinities_stay_with_their_worker_and_channel(dtype):
     g = gen("weights inf")
