@@ -40,24 +40,22 @@ int shared_lanes(int64_t chunks)
     return lanes;
 }
 
-// f(Shape) as with_team, and rows of up to `most` vectors by a workgroup of 1024, three or four vectors a lane.  us of the forms that read a row several
-// times / of these, 5000 x 12000 fp32: norm 393 / 167, in 8 bits 456 / 164, its backward pass 425 / 191, a checkpoint written and read 249 / 95.
+// f(Shape) for the team and the vectors a lane that hold a row of `len` elements, if one does: up to kMost vectors.  Two workgroups of 512 share a
+// compute unit where one of 1024 has it for itself: us by two vectors of 1024 lanes / by three or four of 512: norm 3262 x 9728 f16 45 / 29, 4000 x 16000
+// bf16 with residual 104 / 86, in 8 bits and back 5853 x 8704 121 / 88, its backward pass 5000 x 10240 111 / 105.  Longer rows: the forms that read a
+// row several times / three or four vectors of 1024 lanes, 5000 x 12000 fp32: norm 393 / 167, in 8 bits 456 / 164, its backward pass 425 / 191, a
+// checkpoint written and read 249 / 95.
 template <typename T, int kMost, typename F>
 bool with_rows(int64_t len, F &&f)
 {
-    if (with_team<T>(len, f)) return true;
     const int64_t vecs = ceil_div(len, kVec<T>);
-    if constexpr (kMost > 2048) {
-        if (vecs > 2048 && vecs <= 3072) {
-            f(Shape<1024, 3>{});
-            return true;
-        }
-        if (vecs > 3072 && vecs <= 4096) {
-            f(Shape<1024, 4>{});
-            return true;
-        }
-    }
-    return false;
+    if (len < kVec<T> || vecs > kMost) return false;
+    if (vecs <= 32) with_vecs<16, 1, 2>((int)ceil_div(vecs, 16), f);
+    else if (vecs <= 256) with_vecs<64, 1, 4>((int)ceil_div(vecs, 64), f);
+    else if (vecs <= 1024) with_vecs<256, 2, 4>((int)ceil_div(vecs, 256), f);
+    else if (vecs <= 2048) with_vecs<512, 3, 4>((int)ceil_div(vecs, 512), f);
+    else if constexpr (kMost > 2048) with_vecs<1024, 3, 4>((int)ceil_div(vecs, 1024), f);
+    return true;
 }
 
 int rows8_check(const char *what, int64_t rows, int64_t cols, const float *scale, int32_t type)
