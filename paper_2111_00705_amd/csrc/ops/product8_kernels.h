@@ -44,6 +44,13 @@ __device__ __forceinline__ void to_lds(const v4u &buffer, uint32_t offset, const
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer) : "memory");
 }
 
+// The same of 64 numbers of 32 bits.
+__device__ __forceinline__ void words_to_lds(const v4u &buffer, uint32_t offset, const float *to)
+{
+    const uint32_t lds = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) float *)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer) : "memory");
+}
+
 // 16 bytes of a row of `cols`, from k on; zero past the row.  Any alignment.
 __device__ __forceinline__ v4i load_row16(const int8_t *row, int k, int cols)
 {
@@ -78,6 +85,8 @@ __device__ __forceinline__ v4i load_row16(const int8_t *row, int k, int cols)
 // wavefront's own piece of LDS, so that a store takes 16 neighbouring bytes a lane and whole lines a row: stored as they are held, in
 // pieces of 8 bytes, the 134 MB of 16384 x 4096 results took 110 us of 330.
 // rows, cols: how many there are from the first on.
+typedef float v4f __attribute__((ext_vector_type(4)));
+
 template <typename Y, int kFrags> constexpr int kSixteenLd = kFrags * 16 + 16 / (int)sizeof(Y);       // elements from row to row in LDS
 template <typename Y, int kFrags>
 __device__ __forceinline__ void store_sixteen(Y *lds, const Y (&v)[kFrags][4], Y *to, int64_t stride, int64_t rows, int64_t cols, bool stream)
@@ -205,6 +214,7 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__rest
     constexpr int kLoads = kRows / 16 / kWaves, kLoadsX = kM / 16 / kWaves;     // wavefront-wide loads of 16 rows each
     static_assert(kM % (16 * kWaves) == 0 && kN % (16 * kWaves) == 0, "whole loads");
     __shared__ __attribute__((aligned(1024))) int8_t tile[kStages][kRows * kStep];
+    __shared__ __attribute__((aligned(16))) float factors[kSplit ? 1 : kM + 2 * kN];        // scales of the tokens, of the channels, and the bias
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const unsigned block = a.first + blockIdx.x;
@@ -287,17 +297,33 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__rest
     };
     Frags even, odd;
     const int steps = (k_end - k_begin + kStep - 1) / kStep;
+    if constexpr (!kSplit) {                         // before all others, and so there before any of them: at the end nothing waits for memory
+        const v4u from[3] = {raw_buffer(x_scale + m0, (uint32_t)rows_m * 4u), raw_buffer(w_scale + n0, (uint32_t)rows_n * 4u),
+                             raw_buffer(bias ? bias + n0 : bias, bias ? (uint32_t)rows_n * 4u : 0u)};
+        constexpr int kOfX = kM / kWave, kOfN = kN / kWave;
+#pragma unroll
+        for (int j = 0; j < kOfX + 2 * kOfN; ++j) {
+            const int which = j < kOfX ? 0 : j < kOfX + kOfN ? 1 : 2, part = j - (which == 0 ? 0 : which == 1 ? kOfX : kOfX + kOfN);
+            if (wave == j % kWaves) words_to_lds(from[which], (uint32_t)(part * kWave + lane) * 4u, &factors[j * kWave]);
+        }
+    }
 #pragma unroll
     for (int u = 0; u < kStages - 1; ++u) send(u);
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
     read(even, 0);
-    for (int s = 0; s < steps; s += kStages) {
+    int s = 0;
+    for (; s + kStages <= steps; s += kStages) {
 #pragma unroll
         for (int u = 0; u < kStages; u += 2) {
-            if (kStages > 4 && s + u >= steps) break;
             step(u, even, odd);
             step(u + 1, odd, even);
         }
+    }
+#pragma unroll
+    for (int u = 0; u < kStages; u += 2) {           // the last ones, in pairs
+        if (s + u >= steps) break;
+        step(u, even, odd);
+        step(u + 1, odd, even);
     }
     if constexpr (kSplit) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");     // LDS belongs to the next workgroup after this one
@@ -317,19 +343,17 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave, 2) void product8(Y *__rest
                 }
             }
     } else {
+        // nothing is on its way to LDS or read from it any more, by any wavefront
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         float ws[kNi][4], b[kNi][4], xs[kMi];
 #pragma unroll
         for (int n = 0; n < kNi; ++n) {
-            load_channels(ws[n], w_scale, n0 + (wn * kNi + n) * 16 + fgroup * 4, a.outs);
-            load_channels(b[n], bias, n0 + (wn * kNi + n) * 16 + fgroup * 4, a.outs);
+            const float *at = &factors[kM + (wn * kNi + n) * 16 + fgroup * 4];
+            *reinterpret_cast<v4f *>(ws[n]) = *reinterpret_cast<const v4f *>(at);
+            *reinterpret_cast<v4f *>(b[n]) = *reinterpret_cast<const v4f *>(at + kN);
         }
 #pragma unroll
-        for (int m = 0; m < kMi; ++m) {
-            const int64_t at_m = m0 + (wm * kMi + m) * 16 + frow;
-            xs[m] = at_m < a.rows ? x_scale[at_m] : 0.f;
-        }
-        // nothing is on its way to LDS or read from it any more, by any wavefront
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        for (int m = 0; m < kMi; ++m) xs[m] = factors[(wm * kMi + m) * 16 + frow];
         Y *mine = reinterpret_cast<Y *>(&tile[0][0]) + wave * 16 * kSixteenLd<Y, kNi>;
         static_assert(kWaves * 16 * kSixteenLd<Y, kNi> * sizeof(Y) <= sizeof tile, "room for the results");
 #pragma unroll

@@ -27,7 +27,6 @@
 namespace cams_ops {
 
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef float v4f __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
 // x = hi + rest with 8 bits in hi.  Of an infinity nothing is left.
