@@ -246,15 +246,17 @@ struct WeightShape {
     int64_t lost_ld;
     uint64_t a_at, b_at, sums_at, bias_at, lost_at, bytes;
 };
-WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bool binary, int32_t type, bool dy_aligned)
+// wide: the gradients are fp32
+WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bool binary, int32_t type, bool dy_aligned, bool wide)
 {
     const int64_t per = rows / n;
     WeightShape s = {};
     const bool as_it_lies = dy_aligned && outs % 8 == 0;
     s.q_planes = 1;
-    s.dy_planes = type == COMP_AMS_F32 ? 3 : binary ? 1 : 2;
-    // bytes written: two planes of q scale, and dy if it is not read as it lies; or q and two planes of dy scale
-    if (type == COMP_AMS_BF16 && !binary && cols + (as_it_lies ? 0 : outs) <= 2 * outs) s.q_planes = 2, s.dy_planes = 1;
+    const int planes = type == COMP_AMS_F32 ? 3 : binary ? 1 : wide ? 3 : 2;
+    s.dy_planes = planes;
+    // bytes written: planes of q scale, and dy if it is not read as it lies; or q and planes of dy scale
+    if (type == COMP_AMS_BF16 && !binary && planes * cols + (as_it_lies ? 0 : outs) <= cols + planes * outs) s.q_planes = planes, s.dy_planes = 1;
     s.copied = s.dy_planes > 1 || !as_it_lies;
     s.half = type == COMP_AMS_F16 && s.dy_planes == 1;
     const int64_t steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.q_planes * s.dy_planes);
@@ -286,8 +288,10 @@ int weight_check(const char *what, int64_t rows, int64_t cols, int64_t outs, int
     REQUIRE(rows % n == 0, "%s: rows=%lld must be a multiple of n=%d", what, (long long)rows, n);
     REQUIRE(cols >= 0 && cols <= kMostChannels && outs >= 0 && outs <= kMostChannels, "%s: cols=%lld or outs=%lld is out of range", what,
             (long long)cols, (long long)outs);
-    const WeightShape s = weight_shape(rows, cols, outs, n, binary != 0, type, true);
-    REQUIRE(s.tiles_i * s.tiles_o <= kMaxBlocks / n / s.splits, "%s: cols, outs and n are too many for one call", what);
+    for (bool wide : {false, true}) {
+        const WeightShape s = weight_shape(rows, cols, outs, n, binary != 0, type, true, wide);
+        REQUIRE(s.tiles_i * s.tiles_o <= kMaxBlocks / n / s.splits, "%s: cols, outs and n are too many for one call", what);
+    }
     return COMP_AMS_OK;
 }
 
@@ -320,10 +324,14 @@ void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, con
     };
     constexpr std::integral_constant<int, 1> one{};
     constexpr std::integral_constant<int, 2> two{};
-    if (type == COMP_AMS_F32) go(float{}, one, std::integral_constant<int, 3>{});
+    constexpr std::integral_constant<int, 3> three{};
+    if (type == COMP_AMS_F32) go(float{}, one, three);
     else if (type == COMP_AMS_F16 && s.half) go(f16_t{}, one, one);
+    else if (type == COMP_AMS_F16 && s.dy_planes == 3) go(f16_t{}, one, three);
     else if (type == COMP_AMS_F16) go(f16_t{}, one, two);
+    else if (s.q_planes == 3) go(bf16_t{}, three, one);
     else if (s.q_planes == 2) go(bf16_t{}, two, one);
+    else if (s.dy_planes == 3) go(bf16_t{}, one, three);
     else if (s.dy_planes == 2) go(bf16_t{}, one, two);
     else go(bf16_t{}, one, one);
 }
@@ -607,7 +615,8 @@ int comp_ams_linear_weight_grad_work_bytes(int64_t rows, int64_t cols, int64_t o
     const char *what = "linear_weight_grad_work_bytes";
     if (const int rc = weight_check(what, rows, cols, outs, n, binary, type)) return rc;
     REQUIRE(bytes, "%s: bytes is NULL", what);
-    *bytes = weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned != 0).bytes;
+    *bytes = std::max(weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned != 0, false).bytes,
+                      weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned != 0, true).bytes);
     return COMP_AMS_OK;
 }
 
@@ -626,7 +635,7 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
     REQUIRE(scale || rows == 0, "%s: scale is NULL", what);
     REQUIRE(aligned(scale, 4), "%s: scale must be 4-byte aligned", what);
     const bool dy_aligned = aligned(dy, 16) && (rows <= 1 || (dy_stride % 8 == 0 && dy_stride <= kMostChannels));
-    const WeightShape s = weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned);
+    const WeightShape s = weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned, grad_type == COMP_AMS_F32);
     REQUIRE(s.bytes == 0 || (work && work_bytes >= s.bytes && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
             (unsigned long long)s.bytes);
     if (outs == 0) return COMP_AMS_OK;

@@ -5,10 +5,11 @@
 // The matrix instruction takes bfloat16, which holds q exactly (7 bits); what it cannot hold goes in several planes whose products are added up:
 //   dy in bfloat16, scales powers of two     q scale and dy, both exact: one plane
 //   dy in float16, scales powers of two      the same in half precision; what of q scale is out of its range is added at the end
-//   dy in bfloat16, any scale                fl32(q scale) or fl32(dy scale), whichever makes less to write, in two planes of 8 bits: 2^-17 of
-//                                            each product is lost, nothing where the scale is a power of two
-//   dy in float16, any scale                 fl32(dy scale) in two planes, the same
-//   dy in float32                            fl32(dy scale) in three planes: all 24 bits
+//   dy in bfloat16, any scale                fl32(q scale) or fl32(dy scale), whichever makes less to write, in planes of 8 bits: three, all 24 bits, for
+//                                            gradients in fp32; for gradients in 16 bits, whose own rounding is 2^-9 or 2^-12, two: 2^-17 of
+//                                            each product is lost
+//   dy in float16, any scale                 fl32(dy scale), the same
+//   dy in float32                            fl32(dy scale) in three planes
 // A first kernel writes q and the planes of dy as rows of bfloat16 (dy itself is read where one plane does and its rows are aligned), so that
 // each number is widened once and not once for every tile that it meets.  The sum runs over planes and rows.  Both operands lie across it (their rows are the sum's
 // index): a step's rows go from memory to LDS as they lie, without registers, and the transposing LDS reads hand every lane its column's
@@ -17,7 +18,7 @@
 // 16384 rows, 4096 x 4096, four workers, bfloat16: 439 us with the first kernel, which takes 33 of them (HBM-bound, 6.1 TB/s); 1350 TFLOP/s for the
 // product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  Half precision with scales of powers
 // of two, one worker: 414 us, in two planes of bfloat16 806 (13698 rows, 192 x 3914, two workers: 78 and 148, most of it the planes' bytes).  bfloat16 with
-// any scales, 6168 rows, 183 x 4697, four workers: 80 us with the planes on q's side, 90 on dy's.  16384 rows, 768 x 2304, eight workers:
+// any scales, 6168 rows, 183 x 4697, four workers: 80 us with two planes on q's side, 90 on dy's.  16384 rows, 768 x 2304, eight workers:
 // 70 us, 216 tiles for 256 compute units.
 #pragma once
 #include <type_traits>
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
                         plane[v] = x[v];
                         if (p < kQ - 1) {
                             plane[v] = take_plane(x[v]);
-                            if (x[v] == 0.f) x[v] = plane[v] * 0x1p-60f;         // an infinite dy meets no zero that was none
+                            if (x[v] == 0.f) x[v] = plane[v] * 0x1p-40f;         // an infinite dy meets no zero that was none
                         }
                     }
                     *reinterpret_cast<v4u *>(a_out + p * a.a_plane + row[u] * a.a_ld + c) = narrow<H>(plane);

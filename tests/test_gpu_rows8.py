@@ -357,6 +357,20 @@ def test_linear_weight_grad_of_nothing():
     assert (dw == 5).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols,outs", [(40, 300), (300, 40), (64, 48), (129, 8)])
+def test_linear_weight_grad_keeps_24_bits_for_fp32(cols, outs, dtype):
+    """Workers of one row: a gradient is one product.  Its factor is rounded to fp32 (2^-24) and cut into planes whose three products are exact; their
+    sum is off by at most 2^-23 for each addition, also where it is cut.  Two planes would be off by up to 2^-17."""
+    g = gen("weights bits", cols, outs)
+    q, scale = Q.quantized(randn(g, 5, cols), False)
+    dy = randn(g, 5, outs, std=0.1).to(dtype)
+    dw = torch.zeros(5, outs, cols, device="cuda")
+    P.linear_weight_grad(dy.cuda(), q.cuda(), scale.cuda(), dw)
+    want = dy.double()[:, :, None] * (q.double() * scale.double()[:, None])[:, None, :]
+    assert ((dw.cpu().double() - want).abs() <= (1 + 2 * 3) * Q.E32 * want.abs() + 2.0 ** -120).all()
+
+
 @pytest.mark.parametrize("n,per,cols,outs", [(2, 1, 1, 1), (2, 5, 9, 4), (2, 70, 33, 130), (2, 300, 129, 127), (2, 33, 2100, 2080), (2, 4200, 64, 72)])
 def test_linear_weight_grad_rows_that_half_precision_does_not_hold(n, per, cols, outs):
     """Scales of 2^-126 to 2^100 beside common ones, a worker with nothing but small ones.
