@@ -19,7 +19,7 @@
 // product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  Half precision with scales of powers
 // of two, one worker: 414 us, in two planes of bfloat16 806 (13698 rows, 192 x 3914, two workers: 78 and 148, most of it the planes' bytes).  bfloat16 with
 // any scales, 6168 rows, 183 x 4697, four workers: 80 us with two planes on q's side, 90 on dy's.  16384 rows, 768 x 2304, eight workers:
-// 70 us, 216 tiles for 256 compute units.
+// 66 us, 216 tiles for 256 compute units.
 #pragma once
 #include <type_traits>
 
