@@ -634,7 +634,8 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
     if (dbias) REQUIRE_ROWS(what, "dbias", dbias, (int64_t)n, outs, grad_stride, grad_type);
     REQUIRE(scale || rows == 0, "%s: scale is NULL", what);
     REQUIRE(aligned(scale, 4), "%s: scale must be 4-byte aligned", what);
-    const bool dy_aligned = aligned(dy, 16) && (rows <= 1 || (dy_stride % 8 == 0 && dy_stride <= kMostChannels));
+    if (rows <= 1) dy_stride = outs;       // any is allowed there, and the product takes the end of dy from it
+    const bool dy_aligned = aligned(dy, 16) && dy_stride % 8 == 0 && dy_stride <= kMostChannels;
     const WeightShape s = weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned, grad_type == COMP_AMS_F32);
     REQUIRE(s.bytes == 0 || (work && work_bytes >= s.bytes && aligned(work, 16)), "%s: needs %llu bytes of 16-byte aligned work memory", what,
             (unsigned long long)s.bytes);

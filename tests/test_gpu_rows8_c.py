@@ -1,0 +1,51 @@
+"""The operators of include/comp_ams_rows8.h through the C functions: what the header allows and the Python entry points never pass."""
+import ctypes as C
+import zlib
+
+import pytest
+import torch
+
+import operators_util as R
+import paper_2111_00705_amd as P
+import rows8_util as Q
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+CODE = {F32: 0, BF16: 1, F16: 2}
+
+
+def gen(*key):
+    return torch.Generator().manual_seed(zlib.crc32(repr(key).encode()))
+
+
+def call(name, *args):
+    stream = torch.cuda.current_stream().cuda_stream
+    rc = getattr(P.lib(), "comp_ams_" + name)(*(a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args), stream)
+    assert rc == P.OK, P.lib().comp_ams_operators_last_error().decode()
+
+
+def work_memory(name, *args):
+    need = C.c_uint64(0)
+    assert getattr(P.lib(), f"comp_ams_{name}_work_bytes")(*args, C.byref(need)) == P.OK
+    return torch.empty(max(need.value, 16), dtype=torch.uint8, device="cuda"), need.value
+
+
+@pytest.mark.parametrize("binary", [1, 0])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("cols,outs", [(40, 64), (300, 256), (24, 600), (9, 17)])
+def test_linear_weight_grad_of_one_row_with_any_stride(cols, outs, dtype, binary):
+    """One row has no next one: its stride, of dy and of q, says nothing."""
+    print(f"[case] one row {cols}->{outs} {dtype} {binary}", flush=True)
+    g = gen("one row", cols, outs)
+    q, scale = Q.quantized(torch.randn(1, cols, generator=g), True)
+    dy = (torch.randn(1, outs, generator=g) * 0.1).to(dtype)
+    dw, db, s_dw, s_db = Q.weight_grad(dy, q, scale, 1, binary)
+    work, size = work_memory("linear_weight_grad", 1, cols, outs, 1, binary, CODE[dtype], 1 if outs % 8 == 0 else 0)
+    qc, sc, dyc = q.cuda(), scale.cuda(), dy.cuda()
+    for dy_stride, q_stride in ((outs, cols), (0, 0), (8, 1), (outs - 1, cols), (outs + 3, 1 << 40), (1 << 31, cols), (3 << 29, cols), (1 << 59, 1 << 59)):
+        for in_first in (0, 1):
+            w, b = torch.full((outs * cols,), 7.0, device="cuda"), torch.full((outs,), 7.0, device="cuda")
+            call("linear_weight_grad", w, b, dyc, qc, sc, 1, cols, outs, dy_stride, q_stride, 1, 0, in_first, binary, CODE[dtype], 0, work, size)
+            got = w.view(cols, outs).t() if in_first else w.view(outs, cols)
+            R.close(got, dw[0], s_dw[0], f"dweight, stride {dy_stride}")
+            R.close(b, db[0], s_db[0], f"dbias, stride {dy_stride}")
