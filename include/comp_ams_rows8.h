@@ -86,11 +86,9 @@ int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, int3
  * Workers as for comp_ams_layer_norm_backward.  dweight points at the weight's place in worker 0's row, dense, [outs][cols], or [cols][outs]
  * with in_first != 0; dbias (may be NULL) at the bias'; the next worker's are grad_stride elements further.
  * Sums are fp32.  Before the product dy[r][o] scale[r] is rounded to fp32 and then, for dy and gradients in 16 bits, to 16 bits of mantissa; of bfloat16 it may
- * be q[r][i] scale[r] in its place.  binary != 0 promises that all scales are powers of two, as binary quantising gives them; dy in 16 bits then takes
- * one product in place of two (of three for fp32 gradients) and nothing is lost, and where the promise does not hold q scale is rounded to dy's type.
- * Of half precision with binary != 0, rows whose q scale is out of its range (not a multiple of 2^-24, or beyond 65504) are added
- * apart, at a far lower rate: rows of numbers in half precision have none.  Its numbers below 2^-14, in dy or q scale, are as the matrix unit
- * takes them: their products are exact to 2^-24 of what they would be with 2^-14 in their place.
+ * be q[r][i] scale[r] in its place.  binary != 0 promises that all scales are powers of two, as binary quantising gives them: of dy in 16 bits nothing is
+ * lost then (but of numbers below 2^-126), and bfloat16 takes one product, half precision two, in place of two or, for fp32 gradients, three.
+ * Where the promise does not hold, q scale is rounded to bfloat16, of half precision dy scale to 16 bits of mantissa.
  * An infinity or a NaN in dy or a scale reaches the worker's gradients that it belongs to, as an infinity or a NaN.
  * rows >= 0 a multiple of n and below 2^32, a worker's below 2^29; 0 <= cols, outs <= 2^23.  With rows = 0 the gradients are zero.
  * work: comp_ams_linear_weight_grad_work_bytes() bytes, 16-byte aligned, not kept from one call to the next: q in 16 bits, and dy too

@@ -238,27 +238,24 @@ struct WeightShape {
     int tile;                // input and output channels of a tile
     int q_planes, dy_planes; // one of them is 1
     bool copied;             // dy is written anew
-    bool half;               // in half precision
     int64_t tiles_i, tiles_o;
     int64_t splits, split_steps;         // pieces of the sum over planes and steps of rows, steps of a piece
     int64_t bias_chunks, bias_rows;      // pieces of a worker's rows for the bias, rows of a piece
     int64_t a_ld, b_ld;
-    int64_t lost_ld;
-    uint64_t a_at, b_at, sums_at, bias_at, lost_at, bytes;
+    uint64_t a_at, b_at, sums_at, bias_at, bytes;
 };
-// wide: the gradients are fp32
+// wide: the gradients are fp32.  Scales of powers of two leave dy its bits: 8, or 11 in two planes.
 WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bool binary, int32_t type, bool dy_aligned, bool wide)
 {
     const int64_t per = rows / n;
     WeightShape s = {};
     const bool as_it_lies = dy_aligned && outs % 8 == 0;
     s.q_planes = 1;
-    const int planes = type == COMP_AMS_F32 ? 3 : binary ? 1 : wide ? 3 : 2;
+    const int planes = type == COMP_AMS_F32 ? 3 : binary ? (type == COMP_AMS_F16 ? 2 : 1) : wide ? 3 : 2;
     s.dy_planes = planes;
     // bytes written: planes of q scale, and dy if it is not read as it lies; or q and planes of dy scale
     if (type == COMP_AMS_BF16 && !binary && planes * cols + (as_it_lies ? 0 : outs) <= cols + planes * outs) s.q_planes = planes, s.dy_planes = 1;
     s.copied = s.dy_planes > 1 || !as_it_lies;
-    s.half = type == COMP_AMS_F16 && s.dy_planes == 1;
     const int64_t steps = std::max<int64_t>(1, ceil_div(per, kWeightStep) * s.q_planes * s.dy_planes);
     choose_tile(kWeightTiles, steps, (double)cols * (double)outs * n, 0.0, cols, outs, n, [&](const TileCost &t, int64_t pieces, int64_t length) {
         s.tile = t.high, s.tiles_i = ceil_div(cols, t.high), s.tiles_o = ceil_div(outs, t.wide);
@@ -268,15 +265,13 @@ WeightShape weight_shape(int64_t rows, int64_t cols, int64_t outs, int32_t n, bo
     s.bias_rows = std::max<int64_t>(64, ceil_div(per, want));
     s.bias_chunks = std::max<int64_t>(1, ceil_div(per, s.bias_rows));
     s.a_ld = ceil_div(cols, 8) * 8, s.b_ld = ceil_div(outs, 8) * 8;
-    s.lost_ld = s.half ? ceil_div(per, 16) * 16 : 0;
     const uint64_t a_bytes = (uint64_t)(s.q_planes * rows * s.a_ld) * 2, b_bytes = s.copied ? (uint64_t)(s.dy_planes * rows * s.b_ld) * 2 : 0;
     const uint64_t sums = s.splits > 1 ? (uint64_t)(s.splits * n) * (uint64_t)(cols * outs) * sizeof(float) : 0;
     s.a_at = 0;
     s.b_at = s.a_at + a_bytes;
     s.sums_at = s.b_at + b_bytes;
     s.bias_at = s.sums_at + (sums + 15) / 16 * 16;
-    s.lost_at = s.bias_at + ((uint64_t)(s.bias_chunks * n * outs) * sizeof(float) + 15) / 16 * 16;
-    s.bytes = s.lost_at + (uint64_t)(n * s.lost_ld);
+    s.bytes = s.bias_at + (uint64_t)(s.bias_chunks * n * outs) * sizeof(float);
     return s;
 }
 
@@ -302,7 +297,6 @@ void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, con
     PrepareArgs a = {};
     a.rows = rows, a.cols = cols, a.outs = outs, a.q_stride = q_stride, a.dy_stride = dy_stride;
     a.a_ld = s.a_ld, a.b_ld = s.b_ld, a.a_plane = rows * s.a_ld, a.b_plane = rows * s.b_ld;
-    a.lost = reinterpret_cast<uint8_t *>(work + s.lost_at), a.lost_ld = s.lost_ld;
     a.worker_rows = rows / n, a.bias_rows = s.bias_rows, a.bias_chunks = (unsigned)s.bias_chunks;
     a.lanes_a = shared_lanes(s.a_ld / 8), a.lanes_b = shared_lanes(s.b_ld / 8);
     const bool product = rows > 0 && cols > 0;
@@ -326,7 +320,6 @@ void weight_prepare_launch(const WeightShape &s, char *work, const void *dy, con
     constexpr std::integral_constant<int, 2> two{};
     constexpr std::integral_constant<int, 3> three{};
     if (type == COMP_AMS_F32) go(float{}, one, three);
-    else if (type == COMP_AMS_F16 && s.half) go(f16_t{}, one, one);
     else if (type == COMP_AMS_F16 && s.dy_planes == 3) go(f16_t{}, one, three);
     else if (type == COMP_AMS_F16) go(f16_t{}, one, two);
     else if (s.q_planes == 3) go(bf16_t{}, three, one);
@@ -348,16 +341,14 @@ void weight_launch(G *out, G *dbias, const bf16_t *a_rows, const bf16_t *b_rows,
             kernel<<<count, threads, 0, stream>>>(out, dbias, a_rows, b_rows, bias_sums, a);
         });
     };
-    auto form = [&](auto half, auto first) {
-        constexpr bool kHalf = decltype(half)::value, kFirst = decltype(first)::value;
-        if (tile == 256) go(weight_grad<G, kHalf, kFirst, 256, 256, 2, 4>, 512);
-        else if (tile == 128) go(weight_grad<G, kHalf, kFirst, 128, 128, 2, 2>, 256);
-        else go(weight_grad<G, kHalf, kFirst, 64, 64, 2, 2>, 256);
+    auto form = [&](auto first) {
+        constexpr bool kFirst = decltype(first)::value;
+        if (tile == 256) go(weight_grad<G, kFirst, 256, 256, 2, 4>, 512);
+        else if (tile == 128) go(weight_grad<G, kFirst, 128, 128, 2, 2>, 256);
+        else go(weight_grad<G, kFirst, 64, 64, 2, 2>, 256);
     };
-    if (a.lost && in_first) form(std::true_type{}, std::true_type{});
-    else if (a.lost) form(std::true_type{}, std::false_type{});
-    else if (in_first) form(std::false_type{}, std::true_type{});
-    else form(std::false_type{}, std::false_type{});
+    if (in_first) form(std::true_type{});
+    else form(std::false_type{});
 }
 
 }  // namespace
@@ -650,10 +641,6 @@ int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, cons
     WeightArgs a = {};
     a.cols = cols, a.outs = outs, a.a_ld = s.a_ld, a.b_ld = s.copied ? s.b_ld : dy_stride;
     a.a_plane = s.q_planes > 1 ? rows * s.a_ld : 0, a.b_plane = s.dy_planes > 1 ? rows * s.b_ld : 0;
-    if (s.half) {
-        a.lost = reinterpret_cast<uint8_t *>(memory + s.lost_at), a.lost_ld = s.lost_ld;
-        a.q = q, a.scale = scale, a.dy = static_cast<const f16_t *>(dy), a.q_stride = q_stride, a.dy_stride = dy_stride;
-    }
     a.worker_rows = rows / n, a.out_stride = in_first ? outs : cols;
     a.tiles_i = (int)s.tiles_i, a.tiles_o = (int)s.tiles_o, a.n = n, a.planes = s.q_planes * s.dy_planes;
     a.splits = (int)s.splits, a.split_steps = (int)s.split_steps;

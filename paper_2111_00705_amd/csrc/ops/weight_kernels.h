@@ -4,7 +4,9 @@
 //
 // The matrix instruction takes bfloat16, which holds q exactly (7 bits); what it cannot hold goes in several planes whose products are added up:
 //   dy in bfloat16, scales powers of two     q scale and dy, both exact: one plane
-//   dy in float16, scales powers of two      the same in half precision; what of q scale is out of its range is added at the end
+//   dy in float16, scales powers of two      dy scale in two planes: its 11 bits are 8 and 3, so nothing is lost.  (The matrix instruction of half precision
+//                                            would take both as they are, but it lines products up as if factors below 2^-14 were 2^-14 and cuts
+//                                            them 24 bits below the largest: gradients of 2^-20 were off by 2^-18 and more.)
 //   dy in bfloat16, any scale                fl32(q scale) or fl32(dy scale), whichever makes less to write, in planes of 8 bits: three, all 24 bits, for
 //                                            gradients in fp32; for gradients in 16 bits, whose own rounding is 2^-9 or 2^-12, two: 2^-17 of
 //                                            each product is lost
@@ -16,13 +18,10 @@
 // values.
 //
 // 16384 rows, 4096 x 4096, four workers, bfloat16: 439 us with the first kernel, which takes 33 of them (HBM-bound, 6.1 TB/s); 1350 TFLOP/s for the
-// product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  Half precision with scales of powers
-// of two, one worker: 414 us, in two planes of bfloat16 806 (13698 rows, 192 x 3914, two workers: 78 and 148, most of it the planes' bytes).  bfloat16 with
-// any scales, 6168 rows, 183 x 4697, four workers: 80 us with two planes on q's side, 90 on dy's.  16384 rows, 768 x 2304, eight workers:
+// product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  Half precision, one worker, in two
+// planes: 806 us (13698 rows, 192 x 3914, two workers: 148, most of it the planes' bytes).  bfloat16 with any scales, 6168 rows, 183 x 4697, four workers: 80 us with two planes on q's side, 90 on dy's.  16384 rows, 768 x 2304, eight workers:
 // 66 us, 216 tiles for 256 compute units.
 #pragma once
-#include <type_traits>
-
 #include "product8_kernels.h"
 
 namespace cams_ops {
@@ -38,20 +37,11 @@ __device__ __forceinline__ float take_plane(float &x)
     return hi;
 }
 
-// x in half precision, the nearest finite number (of a NaN, a NaN).  Rows of q with a power of two that was made for half precision fit: their
-// numbers are multiples of 2^-24 and at most 65504; others may not.
-__device__ __forceinline__ float half_of(float x)
-{
-    return widen1(narrow1<f16_t>(fabsf(x) > 65504.f ? copysignf(65504.f, x) : x));
-}
-
 constexpr int kPrepareThreads = 256;
 
 struct PrepareArgs {
     int64_t rows, cols, outs, q_stride, dy_stride;
     int64_t a_ld, b_ld, a_plane, b_plane;            // rows of the results, elements apart, and planes of them
-    uint8_t *lost;                                   // rows of q scale that half precision does not hold: 1, the others 0
-    int64_t lost_ld;                                 // from worker to worker
     int64_t worker_rows, bias_rows;                  // rows of a worker, and of one of its pieces for the bias
     int lanes_a, lanes_b;                            // lanes that share a row, powers of two up to 256
     unsigned blocks_a, blocks_b;                     // workgroups for q and for dy; the others are for the bias
@@ -129,8 +119,7 @@ __device__ __forceinline__ void bias_join(G *__restrict__ dbias, const float *__
 }
 
 // Rows in 16 bits whose length is a multiple of eight (zeros behind the row): kQ planes of q scale where dy stays as it is (kD = 1), q otherwise; kD
-// planes of dy scale, or dy itself.  In half precision where dy is and stays so.  kBias: further workgroups sum dy's columns.  Lanes that share a
-// row take kPrepareRows rows, whose loads are on their way together: one after the other 16384 rows of 768 took 8.2 us in place of 7.4.
+// planes of dy scale, or dy itself.  kBias: further workgroups sum dy's columns.  Lanes that share a row take kPrepareRows rows, whose loads are on their way together: one after the other 16384 rows of 768 took 8.2 us in place of 7.4.
 constexpr int kPrepareRows = 4;
 template <typename T, int kQ, int kD, bool kBias>
 __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__restrict__ a_out, bf16_t *__restrict__ b_out, float *__restrict__ sums,
@@ -144,8 +133,6 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
             return;
         }
     }
-    constexpr bool kHalf = kD == 1 && std::is_same<T, f16_t>::value;
-    typedef typename std::conditional<kHalf, f16_t, bf16_t>::type H;
     const bool of_q = block < a.blocks_a;
     if (!of_q) block -= a.blocks_a;
     const int lanes = of_q ? a.lanes_a : a.lanes_b, beside = kPrepareThreads / lanes;     // rows that a workgroup takes at a time
@@ -159,12 +146,6 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
         s[u] = scale[row[u]];
     }
     if (of_q) {
-        __shared__ int lost[kHalf ? kPrepareThreads * kPrepareRows : 1];
-        if constexpr (kHalf) {
-#pragma unroll
-            for (int u = 0; u < kPrepareRows; ++u) lost[u * kPrepareThreads + threadIdx.x] = 0;
-            __syncthreads();
-        }
         for (int64_t c = lane * 8; c < a.cols; c += lanes * 8) {
             uint64_t raw[kPrepareRows];
             if (a.cols >= 8) {
@@ -187,16 +168,6 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
 #pragma unroll
                     for (int v = 0; v < 8; ++v) x[v] *= s[u];
                 }
-                if constexpr (kHalf) {
-                    bool less = false;
-#pragma unroll
-                    for (int v = 0; v < 8; ++v) {
-                        const float y = half_of(x[v]);
-                        less |= (y < x[v] || y > x[v]) && (fabsf(x[v]) < 0x1p-14f || fabsf(x[v]) > 65504.f);    // of others eleven bits are kept
-                        x[v] = y;
-                    }
-                    if (less) lost[u * kPrepareThreads + threadIdx.x / lanes] = 1;
-                }
 #pragma unroll
                 for (int p = 0; p < kQ; ++p) {
                     float plane[8];
@@ -208,17 +179,7 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
                             if (x[v] == 0.f) x[v] = plane[v] * 0x1p-40f;         // an infinite dy meets no zero that was none
                         }
                     }
-                    *reinterpret_cast<v4u *>(a_out + p * a.a_plane + row[u] * a.a_ld + c) = narrow<H>(plane);
-                }
-            }
-        }
-        if constexpr (kHalf) {
-            __syncthreads();
-            if (lane == 0) {
-#pragma unroll
-                for (int u = 0; u < kPrepareRows; ++u) {
-                    const uint32_t at = (uint32_t)row[u], worker = at / (uint32_t)a.worker_rows;
-                    a.lost[worker * a.lost_ld + (at - worker * (uint32_t)a.worker_rows)] = (uint8_t)lost[u * kPrepareThreads + threadIdx.x / lanes];
+                    *reinterpret_cast<v4u *>(a_out + p * a.a_plane + row[u] * a.a_ld + c) = narrow<bf16_t>(plane);
                 }
             }
         }
@@ -239,7 +200,7 @@ __global__ __launch_bounds__(kPrepareThreads) void weight_prepare(bf16_t *__rest
                 float plane[8];
 #pragma unroll
                 for (int v = 0; v < 8; ++v) plane[v] = p < kD - 1 ? take_plane(x[u][v]) : x[u][v];
-                *reinterpret_cast<v4u *>(b_out + p * a.b_plane + row[u] * a.b_ld + c) = narrow<H>(plane);
+                *reinterpret_cast<v4u *>(b_out + p * a.b_plane + row[u] * a.b_ld + c) = narrow<bf16_t>(plane);
             }
         }
     }
@@ -256,66 +217,9 @@ struct WeightArgs {
     unsigned tiles;                                  // workgroups for tiles; the others join the bias' sums
     unsigned bias_chunks;
     int64_t grad_stride;
-    // in half precision: rows that are not all there, and q, scale and dy as they lie
-    const uint8_t *lost;
-    int64_t lost_ld;
-    const int8_t *q;
-    const float *scale;
-    const f16_t *dy;
-    int64_t q_stride, dy_stride;
 };
 
 constexpr int kWeightStep = 32;          // rows in a stage of LDS
-
-template <bool kHalf> __device__ __forceinline__ v4f matrix_step(v8bf x, v8bf y, v4f sum)
-{
-    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-    if constexpr (kHalf) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, y), sum, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, sum, 0, 0, 0);
-}
-
-// The rows of a worker in [lo, hi) that half precision does not hold: 4096 are looked at at a time, and f(row) is called for each (there are few
-// or none).  lo and the workers' places are multiples of 16; what stands behind a worker's rows is not asked for by f.
-template <typename F> __device__ __forceinline__ void each_lost(const uint8_t *lost, int lo, int hi, F &&f)
-{
-    const int lane = threadIdx.x % kWave;
-    for (int base = lo; base < hi; base += kWave * 64) {
-        v4u some = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int u = 0; u < 64; u += 16)
-            if (base + lane * 64 + u < hi) some |= *reinterpret_cast<const v4u *>(lost + base + lane * 64 + u);
-        for (uint64_t lanes = __ballot((some[0] | some[1] | some[2] | some[3]) != 0u); lanes; lanes &= lanes - 1) {
-            const int first = base + __builtin_ctzll(lanes) * 64;
-            for (int row = first; row < min(first + 64, hi); ++row)
-                if (lost[row]) f(row);
-        }
-    }
-}
-
-// What half precision leaves out of sixteen rows of a result: the sums of (q scale - half_of(q scale)) dy over those rows of the worker, for the channel
-// `across` of a lane and the fragments from channel `along` on.  Infinities of dy are left to the product (which gives NaN for them where
-// half_of(q scale) is zero).
-template <bool kInFirst, int kAlong>
-__device__ __forceinline__ void lost_sums(float (&sum)[kAlong][4], const WeightArgs &a, int worker, int lo, int hi, int64_t across, int64_t along)
-{
-    each_lost(a.lost + worker * a.lost_ld, lo, hi, [&](int row) {
-        const int64_t r = worker * a.worker_rows + row;
-        const float s = a.scale[r];
-        auto left = [&](int64_t col) {
-            const float x = col < a.cols ? (float)a.q[r * a.q_stride + col] * s : 0.f;
-            return x - half_of(x);
-        };
-        auto grad = [&](int64_t col) {
-            const float d = col < a.outs ? widen1(a.dy[r * a.dy_stride + col]) : 0.f;
-            return fabsf(d) == INFINITY ? 0.f : d;
-        };
-        const float mine = kInFirst ? left(across) : grad(across);
-#pragma unroll
-        for (int y = 0; y < kAlong; ++y)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) sum[y][c] = __builtin_fmaf(mine, kInFirst ? grad(along + y * 16 + c) : left(along + y * 16 + c), sum[y][c]);
-    });
-}
 
 // A tile of kI input channels x kO output channels by kWavesI x kWavesO wavefronts.  kInFirst: the result is [i][o], otherwise [o][i].
 //
@@ -323,7 +227,7 @@ __device__ __forceinline__ void lost_sums(float (&sum)[kAlong][4], const WeightA
 // different banks: a row's 32-byte blocks stand at place block ^ (row & 3); where a load's 1024 bytes are two rows only, at block ^ (row & 1), and
 // loads stand 64 bytes further apart; every eight rows another 128.  All fragments of a lane then lie at a few addresses and constant
 // distances from them.  Stages as in product8.
-template <typename G, bool kHalf, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
+template <typename G, bool kInFirst, int kI, int kO, int kWavesI, int kWavesO>
 __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__restrict__ out, G *__restrict__ dbias,
                                                                           const bf16_t *__restrict__ a_rows, const bf16_t *__restrict__ b_rows,
                                                                           const float *__restrict__ bias_sums, WeightArgs a)
@@ -430,8 +334,8 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
         for (int i = 0; i < kIi; ++i)
 #pragma unroll
             for (int o = 0; o < kOi; ++o) {
-                if constexpr (kInFirst) acc[i][o] = matrix_step<kHalf>(f.o[o], f.i[i], acc[i][o]);
-                else acc[i][o] = matrix_step<kHalf>(f.i[i], f.o[o], acc[i][o]);
+                if constexpr (kInFirst) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.o[o], f.i[i], acc[i][o], 0, 0, 0);
+                else acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.i[i], f.o[o], acc[i][o], 0, 0, 0);
             }
     };
     constexpr int kReads = 2 * (kIi + kOi), kPer = kIi * kOi / kReads;
@@ -455,8 +359,6 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
     Frags even, odd;
 #pragma unroll
     for (int u = 0; u < kStages - 1; ++u) send(u);
-    bool lost = false;                               // asked for here, while the first rows are on their way
-    if constexpr (kHalf) each_lost(a.lost + worker * a.lost_ld, begin * kWeightStep, min(end * kWeightStep, rows), [&](int) { lost = true; });
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kStages - 2) * kLoads) : "memory");
     read(even, 0);
     for (int c = begin; c < end; c += kStages) {
@@ -478,17 +380,13 @@ __global__ __launch_bounds__(kWavesI *kWavesO *kWave, 2) void weight_grad(G *__r
 #pragma unroll
     for (int x = 0; x < kAcross; ++x) {
         const int64_t row = row0 + x * 16;
-        float more[kAlong][4] = {};
-        if constexpr (kHalf) {
-            if (lost) lost_sums<kInFirst, kAlong>(more, a, worker, begin * kWeightStep, min(end * kWeightStep, rows), row + frow, col0 + fgroup * 4);
-        }
         G values[kAlong][4];
 #pragma unroll
         for (int y = 0; y < kAlong; ++y)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const float sum = kInFirst ? acc[kInFirst ? x : 0][kInFirst ? y : 0][c] : acc[kInFirst ? 0 : y][kInFirst ? 0 : x][c];
-                values[y][c] = narrow1<G>(kHalf ? sum + more[y][c] : sum);
+                values[y][c] = narrow1<G>(sum);
             }
         store_sixteen<G, kAlong>(mine, values, ot + row * a.out_stride + col0, a.out_stride, across - row, along - col0, a.stream_out);
     }

@@ -288,7 +288,8 @@ def linear_weight_grad(dy, q, scale, dweight, dbias=None, binary=False, *, strea
     """Weight gradients of y = x @ weight.T + bias from its input in 8 bits: q int8 [..., cols] with scale, dy [..., outs].  Writes
     dweight [n, outs, cols] (or a transposed view of one that is dense as [n, cols, outs]) and dbias [n, outs], views of the optimiser's gradient
     buffer, of its type; worker w's from the w-th of n equal parts of the rows.  binary: all scales are powers of two, as
-    quantize_rows(..., binary=True) gives them: dy in 16 bits then takes one product in place of two, or of three where the gradients are fp32."""
+    quantize_rows(..., binary=True) gives them: of dy in 16 bits nothing is lost then, and it takes one product (bfloat16) or two (float16) in place of
+    two, or of three where the gradients are fp32."""
     if _torch is None:
         _load()
     if stream is not None:
