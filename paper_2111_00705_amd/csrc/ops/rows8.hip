@@ -606,8 +606,10 @@ int comp_ams_linear_weight_grad_work_bytes(int64_t rows, int64_t cols, int64_t o
     const char *what = "linear_weight_grad_work_bytes";
     if (const int rc = weight_check(what, rows, cols, outs, n, binary, type)) return rc;
     REQUIRE(bytes, "%s: bytes is NULL", what);
-    *bytes = std::max(weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned != 0, false).bytes,
-                      weight_shape(rows, cols, outs, n, binary != 0, type, dy_aligned != 0, true).bytes);
+    // for gradients of either width; and without a promise dy may be aligned all the same, where planes of q may take more than a copy of dy
+    *bytes = 0;
+    for (bool wide : {false, true})
+        for (bool lies : {true, dy_aligned != 0}) *bytes = std::max(*bytes, weight_shape(rows, cols, outs, n, binary != 0, type, lies, wide).bytes);
     return COMP_AMS_OK;
 }
 

@@ -49,3 +49,23 @@ def test_linear_weight_grad_of_one_row_with_any_stride(cols, outs, dtype, binary
             got = w.view(cols, outs).t() if in_first else w.view(outs, cols)
             R.close(got, dw[0], s_dw[0], f"dweight, stride {dy_stride}")
             R.close(b, db[0], s_db[0], f"dbias, stride {dy_stride}")
+
+
+@pytest.mark.parametrize("cols,outs", [(12, 8), (33, 24), (300, 200)])
+def test_linear_weight_grad_of_aligned_rows_that_nobody_promised(cols, outs):
+    """bfloat16 and scales of any value: of aligned dy the input may take the planes, for which there has to be room."""
+    print(f"[case] no promise {cols}->{outs}", flush=True)
+    g = gen("no promise", cols, outs)
+    rows, n = 128, 2
+    q, scale = Q.quantized(torch.randn(rows, cols, generator=g), False)
+    dy = (torch.randn(rows, outs, generator=g) * 0.1).to(BF16)
+    dw, _, s_dw, _ = Q.weight_grad(dy, q, scale, n, False)
+    work, size = work_memory("linear_weight_grad", rows, cols, outs, n, 0, 1, 0)
+    w = torch.zeros(n, outs, cols, device="cuda")
+    call("linear_weight_grad", w, None, dy.cuda(), q.cuda(), scale.cuda(), rows, cols, outs, outs, cols, n, outs * cols, 0, 0, 1, 0, work, size)
+    R.close(w, dw, s_dw, "dweight")
+    far = torch.zeros(rows, 1 << 22, dtype=BF16, device="cuda")[:, :outs]                  # aligned rows further apart than the binding promises
+    far.copy_(dy)
+    again = torch.zeros_like(w)
+    P.linear_weight_grad(far, q.cuda(), scale.cuda(), again)
+    assert R.same_bits(again, w)
