@@ -34,7 +34,8 @@ constexpr int kXcds = 8;
 
 // Memory to LDS without registers, asynchronous: a lane's 16 bytes at `offset` of a buffer (base, size in bytes; zeros from its end on) go to `to` +
 // 16 lane, `to` and the buffer being the wavefront's.  vmcnt counts it.  In assembly, because the compiler takes every read of LDS for one of
-// what is still on its way and waits for memory before it; there is no output that it could take for written.
+// what is still on its way and waits for memory before it; there is no output that it could take for written.  The place in LDS is m0, which the
+// compiler sets.
 __device__ __forceinline__ v4u raw_buffer(const void *base, uint32_t bytes)
 {
     const uint64_t at = reinterpret_cast<uint64_t>(base);
@@ -43,14 +44,14 @@ __device__ __forceinline__ v4u raw_buffer(const void *base, uint32_t bytes)
 __device__ __forceinline__ void to_lds(const v4u &buffer, uint32_t offset, const int8_t *to)
 {
     const uint32_t lds = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) int8_t *)to;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer) : "memory");
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "{m0}"(lds) : "memory");
 }
 
 // The same of 64 numbers of 32 bits.
 __device__ __forceinline__ void words_to_lds(const v4u &buffer, uint32_t offset, const float *to)
 {
     const uint32_t lds = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) float *)to;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer) : "memory");
+    asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "{m0}"(lds) : "memory");
 }
 
 // 16 bytes of a row of `cols`, from k on; zero past the row.  Any alignment.
