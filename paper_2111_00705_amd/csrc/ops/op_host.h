@@ -9,6 +9,7 @@
 
 #include "../../../include/comp_ams_operators.h"
 #include "op_common.h"
+#include "op_sizes.h"
 
 namespace cams_ops {
 
@@ -47,10 +48,6 @@ void in_launches(int64_t blocks, int threads, F &&launch)
 }
 constexpr int64_t kMaxElements = (int64_t)1 << 60;    // rows * stride: offsets in bytes stay far below 2^63
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-inline size_t type_size(int32_t type) { return type == COMP_AMS_F32 ? 4 : 2; }
-inline bool known_type(int32_t type) { return type == COMP_AMS_F32 || type == COMP_AMS_BF16 || type == COMP_AMS_F16; }
 inline bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 // Calls f with a value of the element type.

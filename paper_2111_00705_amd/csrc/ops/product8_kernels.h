@@ -15,6 +15,7 @@
 // 16384 x 64 x 4096 40 us (48 before), 14704 x 576 x 2304 38 (43), where the results alone are 22 and 11.
 #pragma once
 #include "rows8.h"
+#include "rows8_shapes.h"
 
 namespace cams_ops {
 
@@ -29,7 +30,6 @@ struct ProductArgs {
     bool stream_out;             // y is stored as a stream
 };
 
-constexpr int kProductStep = 64;         // bytes of k in a stage of LDS
 constexpr int kXcds = 8;
 
 // Memory to LDS without registers, asynchronous: a lane's 16 bytes at `offset` of a buffer (base, size in bytes; zeros from its end on) go to `to` +

@@ -71,7 +71,7 @@ __device__ __forceinline__ void load_eight(float (&x)[8], const T *row, int c, i
     }
 }
 
-constexpr int kBiasCols = 256, kBiasParts = kPrepareThreads * 8 / kBiasCols;         // columns of a workgroup; threads that share eight
+constexpr int kBiasParts = kPrepareThreads * 8 / kBiasCols;         // threads that share eight columns
 
 // Sums of 256 columns of dy over a piece of a worker's rows, into sums[worker][piece][outs]: eight threads take every eighth row for the same
 // eight columns, and their sums are added in order.
@@ -218,8 +218,6 @@ struct WeightArgs {
     unsigned bias_chunks;
     int64_t grad_stride;
 };
-
-constexpr int kWeightStep = 32;          // rows in a stage of LDS
 
 // A tile of kI input channels x kO output channels by kWavesI x kWavesO wavefronts.  kInFirst: the result is [i][o], otherwise [o][i].
 //
