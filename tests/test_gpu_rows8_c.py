@@ -69,3 +69,43 @@ def test_linear_weight_grad_of_aligned_rows_that_nobody_promised(cols, outs):
     again = torch.zeros_like(w)
     P.linear_weight_grad(far, q.cuda(), scale.cuda(), again)
     assert R.same_bits(again, w)
+
+
+# rows that a team of lanes holds, of one wavefront and of several, with ends inside a lane's numbers, and rows of any length
+IN_PLACE = [(40, 100, F32), (33, 1000, BF16), (20, 2047, F32), (9, 8190, F16), (7, 9001, BF16), (5, 17_001, BF16), (3, 70_001, F32), (6, 5, BF16), (4500, 2049, F32)]
+
+
+@pytest.mark.parametrize("rows,cols,dtype", IN_PLACE, ids=str)
+def test_rms_norm_whose_sum_or_result_takes_the_place_of_an_input(rows, cols, dtype):
+    print(f"[case] in place {rows}x{cols} {dtype}", flush=True)
+    g = gen("in place", rows, cols)
+    x, res, gain = torch.randn(rows, cols, generator=g).to(dtype).cuda(), torch.randn(rows, cols, generator=g).to(dtype).cuda(), torch.randn(cols, generator=g).cuda()
+    want_y, want_h, want_r = P.rms_norm(x, gain, res)
+    want_q, want_s, _, _ = P.rms_norm_q8(x, gain, res)
+    alone, _, alone_r = P.rms_norm(x, gain)
+    rstd, scale = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+
+    def norm(y, h, a, b):
+        call("rms_norm", y, h, rstd, a, b, gain, rows, cols, cols, cols, cols, cols, 1e-5, CODE[dtype])
+
+    for which in (0, 1):                                                # h in the place of x, or of the residual; y in the other one's, or in its own
+        for both in (False, True):
+            ins = [x.clone(), res.clone()]
+            y = ins[1 - which] if both else torch.zeros_like(x)
+            norm(y, ins[which], *ins)
+            assert R.same_bits(y, want_y) and R.same_bits(ins[which], want_h) and R.same_bits(rstd, want_r)
+        ins = [x.clone(), res.clone()]                                  # y in an input's place, h not stored, or elsewhere
+        norm(ins[which], None, *ins)
+        assert R.same_bits(ins[which], want_y)
+        ins, h = [x.clone(), res.clone()], torch.zeros_like(x)
+        norm(ins[which], h, *ins)
+        assert R.same_bits(ins[which], want_y) and R.same_bits(h, want_h)
+        ins, q = [x.clone(), res.clone()], torch.zeros(rows, cols, dtype=torch.int8, device="cuda")
+        call("rms_norm_q8", q, scale, ins[which], rstd, *ins, gain, rows, cols, cols, cols, cols, cols, 1e-5, 0, CODE[dtype])
+        assert torch.equal(q, want_q) and R.same_bits(scale, want_s) and R.same_bits(ins[which], want_h) and R.same_bits(rstd, want_r)
+    again = x.clone()                                                   # no residual: y in the place of x
+    norm(again, None, again, None)
+    assert R.same_bits(again, alone) and R.same_bits(rstd, alone_r)
+    h = torch.zeros_like(x)
+    norm(h.clone(), h, x, None)
+    assert R.same_bits(h, x)
