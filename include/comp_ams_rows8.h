@@ -72,8 +72,8 @@ int comp_ams_rms_norm_work_bytes(int64_t rows, int64_t cols, int32_t n, uint64_t
  * applied in fp32 from left to right, y is rounded once to `type`.  0 <= rows, outs < 2^31, 0 <= cols < COMP_AMS_MAX_Q8_COLS.
  * With cols = 0 y is the bias.  The input's gradient is another such product: of dy in 8 bits with the transposed weight in 8 bits.
  * work: comp_ams_linear_q8_work_bytes() bytes of device memory, 16-byte aligned, which may be 0 (then NULL will do); fewer where, as q_aligned
- * and w_aligned != 0 promise, the array's address and stride are multiples of 16 and its stride is below 2^22.  (More than 64 rows are then read
- * where they stand, if cols is a multiple of 16 too.)
+ * and w_aligned != 0 promise, the array's address and stride are multiples of 16 and its stride is below 2^22.  (Rows are then read where
+ * they stand, if cols is a multiple of 16 too.  Few rows need no work memory; how many depends on the sizes.)
  */
 int comp_ams_linear_q8(void *y, const int8_t *q, const float *scale, const int8_t *w, const float *w_scale, const float *bias,
                        int64_t rows, int64_t cols, int64_t outs, int64_t y_stride, int64_t q_stride, int64_t w_stride, int32_t type,
@@ -92,7 +92,8 @@ int comp_ams_linear_q8_work_bytes(int64_t rows, int64_t cols, int64_t outs, int3
  * An infinity or a NaN in dy or a scale reaches the worker's gradients that it belongs to, as an infinity or a NaN.
  * rows >= 0 a multiple of n and below 2^32, a worker's below 2^29; 0 <= cols, outs <= 2^23.  With rows = 0 the gradients are zero.
  * work: comp_ams_linear_weight_grad_work_bytes() bytes, 16-byte aligned, not kept from one call to the next: q in 16 bits, and dy too
- * unless one product takes it, outs is a multiple of 8 and, as dy_aligned != 0 promises, dy and its stride are multiples of 16 bytes.
+ * unless one product takes it, outs is a multiple of 8 and, as dy_aligned != 0 promises, dy and its stride are multiples of 16 bytes; enough for
+ * gradients of either width.
  */
 int comp_ams_linear_weight_grad(void *dweight, void *dbias, const void *dy, const int8_t *q, const float *scale, int64_t rows,
                                 int64_t cols, int64_t outs, int64_t dy_stride, int64_t q_stride, int32_t n, int64_t grad_stride,

@@ -15,8 +15,8 @@ HEADERS = [os.path.join(CSRC, f) for f in ("device_utils.h", "blocksign_kernels.
     os.path.join(os.path.dirname(HERE), "include", "comp_ams_tuning.h"),
     os.path.join(os.path.dirname(HERE), "include", "comp_ams_operators.h"),
     os.path.join(os.path.dirname(HERE), "include", "comp_ams_rows8.h")] + [
-    os.path.join(OPS, f) for f in ("op_common.h", "norm_kernels.h", "bias_kernels.h", "vocab_kernels.h", "op_host.h", "op_sizes.h", "rows8.h", "rows8_shapes.h", "rms_kernels.h",
-                                    "product8_kernels.h", "weight_kernels.h")]
+    os.path.join(OPS, f) for f in ("op_common.h", "norm_kernels.h", "bias_kernels.h", "vocab_kernels.h", "op_host.h", "op_sizes.h", "rows8.h",
+                                    "rows8_shapes.h", "rms_kernels.h", "product8_kernels.h", "weight_kernels.h")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

@@ -6,7 +6,7 @@
 // Both operands lie along k, so a tile's rows go to LDS as they are.  The matrix instruction takes the channels as its rows: a lane then holds
 // four neighbouring channels of one token.
 //
-// 16384 x 4096 x 4096 to bfloat16 takes 222 to 230 us by the card, 2470 TOP/s at best: bound by power.  The matrix units are busy 59 % of the time at a clock that falls from 2.0
+// 16384 x 4096 x 4096 to bfloat16 takes 222 to 235 us by the card, 2470 TOP/s at best: bound by power.  The matrix units are busy 59 % of the time at a clock that falls from 2.0
 // to 1.7 GHz as that share rises, so what was left to gain was energy and the time that results take: read from LDS between barriers, two stages, results
 // stored as they are held, it took 309 us; four stages and fragments a step ahead 5 % less; results through LDS in whole lines and past the caches
 // 222.  The instruction of 32 x 32 results in place of 16 x 16 took 20 % more, four wavefronts of 128 x 128 in place of eight of 128 x 64 a quarter more.

@@ -6,7 +6,7 @@
 //   dy in bfloat16, scales powers of two     q scale and dy, both exact: one plane
 //   dy in float16, scales powers of two      dy scale in two planes: its 11 bits are 8 and 3, so nothing is lost.  (The matrix instruction of half precision
 //                                            would take both as they are, but it lines products up as if factors below 2^-14 were 2^-14 and cuts
-//                                            them 24 bits below the largest: gradients of 2^-20 were off by 2^-18 and more.)
+//                                            them 24 bits below the largest: gradients of 2^-24 were off by 5e-5.)
 //   dy in bfloat16, any scale                fl32(q scale) or fl32(dy scale), whichever makes less to write, in planes of 8 bits: three, all 24 bits, for
 //                                            gradients in fp32; for gradients in 16 bits, whose own rounding is 2^-9 or 2^-12, two: 2^-17 of
 //                                            each product is lost
@@ -18,9 +18,10 @@
 // values.
 //
 // 16384 rows, 4096 x 4096, four workers, bfloat16: 439 us with the first kernel, which takes 33 of them (HBM-bound, 6.1 TB/s); 1350 TFLOP/s for the
-// product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  Half precision, one worker, in two
-// planes: 806 us (13698 rows, 192 x 3914, two workers: 148, most of it the planes' bytes).  bfloat16 with any scales, 6168 rows, 183 x 4697, four workers: 80 us with two planes on q's side, 90 on dy's.  16384 rows, 768 x 2304, eight workers:
-// 66 us, 216 tiles for 256 compute units.
+// product alone, bound by power as product8 is.  Widened tile by tile on the way to LDS the whole took 1159 us.  Half precision,
+// 16000 rows, one worker, in two planes: 833 us (13698 rows, 192 x 3914, two workers: 148, most of it the planes' bytes).  bfloat16 with any scales, 6168
+// rows, 183 x 4697, four workers, gradients in 16 bits: 80 us with two planes on q's side, 90 on dy's.  16384 rows, 768 x 2304, eight workers: 66 us, 216
+// tiles for 256 compute units.
 #pragma once
 #include "product8_kernels.h"
 
