@@ -3,7 +3,7 @@
 each token and channel.  Conventions are those of operators.py.
 
 A row in 8 bits is q (int8) and one float32 scale: q = rint(x / scale), scale = absmax / 127, or with binary=True the least power of two
-not below that, which makes q * scale exact in every type.
+not below that, which makes q * scale exact in every type whose range holds it.
 
     q, scale, h, rstd = rms_norm_q8(x, gain, residual, binary=True)         # 8 bits for the product, and kept for the backward pass
     y = linear_q8(q, scale, wq, wscale)                                     # wq, wscale = quantize_rows(weight)
